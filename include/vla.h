@@ -306,6 +306,87 @@ int vla_policy_objective_noalloc(const float *logp_new, const float *logp_old, c
                                  int per_trajectory, float *objective, float *per_step, float *clip_frac,
                                  void *stream);
 
+/* ---- paged KV cache: append, attention, sampling (generation, section III-C, over ragged batches) ----------------------
+ * The rollout calls above serve batches of one prefix length on a cache of their own layout.  These serve sequences of any
+ * lengths on pages that the caller hands out, and decoders with grouped heads, norms of q and k, capped scores, biases by
+ * distance, prefix masks and windows.  Token ids and positions are whole numbers below 2^31; sizes below are per call.
+ *
+ * vla_paged_cache: one layer's cache.  k, v: DEVICE dtype [n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned;
+ *   page_size a power of two from 16 to 1024; head_dim a multiple of 16, at most 256.  Position p of a sequence lies in page
+ *   page_table[sequence][p / page_size], row p % page_size.
+ * vla_paged_batch: rows of n_seq sequences, one after the other: sequence s has rows row_start[s] .. row_start[s + 1] - 1
+ *   (row_start ascending from 0), the newest of its kv_len[s] positions: row i of its n_s rows is at position
+ *   kv_len[s] - n_s + i.  A sequence may have no rows.  Rows from row_start[n_seq] to n_rows - 1 are padding: neither read nor
+ *   written.  max_rows, max_len (HOST): bounds of n_s and kv_len that the launches are sized by; work beyond them is left out, and so are
+ *   pages whose id is not in [0, n_pages): the rows are not written, and read as zeros.  The arrays are read on the device, so a captured call follows them as they change.
+ *   table_stride: entries per sequence in page_table, at least max_len / page_size rounded up; entries of pages that hold no
+ *   visible position are never read.
+ *   page_table must not give one page to two sequences that both write to it (sequences may read shared pages).
+ *
+ * vla_paged_append: the new rows' q, k and v (outputs of a projection, in_dtype, row strides in elements, heads packed within
+ *   a row) -> K and V in their pages and q_out, in the cache's dtype.  Per head of q and of k: x / sqrt(mean(x^2) + eps) * gain
+ *   where a gain is given, then the rotation of the first rot_dim dims by position * inv_freq[i]: of the pairs (i, i + rot_dim / 2),
+ *   or (2 i, 2 i + 1) where interleaved; cos and sin times `scale`.  v is rounded alone.  fp32 arithmetic, angles in fp64,
+ *   one rounding at the end.  q and q_out may both be NULL (k and v alone), and q_out may be q itself (same dtype and stride).
+ *   Rows at negative positions (kv_len[s] < n_s) are left out.
+ *   vla_rotary: inv_freq DEVICE fp64 [rot_dim / 2] (scaled as the model has it; NULL with rot_dim 0), rot_dim even, at most
+ *   head_dim; q_gain, k_gain DEVICE fp32 [head_dim] or NULL.
+ *
+ * vla_paged_attention: rows q [n_rows, n_heads, head_dim] (the cache's dtype, row stride in elements; n_heads a multiple of
+ *   n_kv_heads, heads of a group consecutive) against the pages, which already hold the new rows' K and V.  With p the row's
+ *   position and j a key's:  s = scale q.k,  s = softcap tanh(s / softcap) (softcap > 0),  s -= slopes[head] |p - j| (slopes not
+ *   NULL);  visible are j < kv_len with  (j <= p and (window == 0 or j > p - window))  or  j < prefix_len[sequence];
+ *   out = sum softmax(s) v, fp32 sums; weights are rounded to the cache's dtype for the products with v.  lse (fp32 [n_rows, n_heads] or NULL) = ln sum exp(s).  A row that sees no
+ *   key gets zeros and -inf.  K and V of visible positions are taken to be finite where any row of the call masks them.
+ *   vla_paged_mask: scale > 0; softcap, window >= 0; slopes DEVICE fp32 [n_heads]; prefix_len DEVICE int32 [n_seq]; shared_len
+ *   (HOST): a multiple of page_size; the first shared_len positions of all sequences lie in the same pages, which are read once
+ *   for the whole batch, through sequence 0's table (every sequence with rows must hold shared_len positions or more).
+ *   ws: DEVICE, 16-byte aligned, of vla_paged_attention_workspace_bytes (from HOST numbers alone) bytes: partial sums of split key ranges; no state.
+ *   Sums are added in a fixed order: the same call gives the same bits; the split depends on the HOST numbers.
+ *
+ * vla_sample_logits: one token per row of logits (DEVICE dtype [n, vocab], row stride in elements), vocab at most 262,144.
+ *   With T = temperature[i] and w_k = exp((z_k - max z) / T):  of the tokens the top_k[i] largest are kept (ties: lowest id first;
+ *   <= 0: all), of these the shortest leading run, largest first, that holds top_p[i] of their mass (>= 1: all), of these those
+ *   with w_k >= min_p[i].  token[i] = the lowest id at which the kept tokens' running mass, in id order, exceeds u[i] times its
+ *   total; u in [0, 1).  T <= 0, or u NULL: the largest (lowest id).  The largest is always kept; NaN and -inf never are; where +inf occurs only
+ *   those are, at equal weights.  A row without any gets token -1, n_kept 0 and log-probabilities -inf.
+ *   temperature, top_p, min_p, u: DEVICE fp32 [n]; top_k DEVICE int32 [n]; each may be NULL (1, all, all, greedy, all).
+ *   logp (or NULL): log-probability under softmax(z / T), as the recompute gives it; logp_kept (or NULL): among the kept tokens;
+ *   n_kept (or NULL).  With T <= 0 or u NULL the cuts still apply to n_kept and logp_kept; T <= 0 counts as 1 in all of them.  Masses are summed as 64-bit fixed point numbers,
+ *   in any order the same, so equal inputs give equal tokens. */
+typedef struct vla_paged_cache {
+    void *k, *v;
+    int32_t dtype, n_pages, page_size, n_kv_heads, head_dim;
+} vla_paged_cache;
+typedef struct vla_paged_batch {
+    int32_t n_seq, n_rows, max_rows, max_len, table_stride;
+    const int32_t *row_start, *kv_len, *page_table;   /* DEVICE [n_seq + 1], [n_seq], [n_seq, table_stride] */
+} vla_paged_batch;
+typedef struct vla_rotary {
+    const double *inv_freq;
+    int32_t rot_dim, interleaved;
+    float scale, eps;
+    const float *q_gain, *k_gain;
+} vla_rotary;
+typedef struct vla_paged_mask {
+    float scale, softcap;
+    const float *slopes;
+    const int32_t *prefix_len;
+    int32_t window, shared_len;
+} vla_paged_mask;
+int vla_paged_append(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_rotary *rotary, const void *q,
+                     const void *k, const void *v, int in_dtype, int n_heads, int64_t q_stride, int64_t k_stride,
+                     int64_t v_stride, void *q_out, int64_t q_out_stride, void *stream);
+size_t vla_paged_attention_workspace_bytes(const vla_paged_cache *cache, const vla_paged_batch *batch,
+                                           const vla_paged_mask *mask, int n_heads);
+int vla_paged_attention(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, const void *q,
+                        int n_heads, int64_t q_stride, void *out, int64_t out_stride, float *lse, void *ws, size_t ws_bytes,
+                        void *stream);
+size_t vla_sample_logits_workspace_bytes(int n, int vocab);
+int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, int vocab, const float *temperature,
+                      const int32_t *top_k, const float *top_p, const float *min_p, const float *u, int32_t *token,
+                      float *logp, float *logp_kept, int32_t *n_kept, void *ws, size_t ws_bytes, void *stream);
+
 /* ---------------------------------------------------------------- GPU allocation modes (section IV-A)
  * Host-only arithmetic (no device work, all pointers HOST): the rollout-time model behind the
  * automatic placement.  One rollout epoch is m_chunks steps, each a Generation phase (t_gen for the

@@ -60,6 +60,26 @@ class vla_placement(C.Structure):
     _fields_ = [("k", C.c_int32), ("n_gen", C.c_int32), ("n_sim", C.c_int32), ("time", C.c_double)]
 
 
+class vla_paged_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class vla_paged_batch(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("n_rows", C.c_int32), ("max_rows", C.c_int32), ("max_len", C.c_int32), ("table_stride", C.c_int32),
+                ("row_start", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p)]
+
+
+class vla_rotary(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_float), ("eps", C.c_float),
+                ("q_gain", C.c_void_p), ("k_gain", C.c_void_p)]
+
+
+class vla_paged_mask(C.Structure):
+    _fields_ = [("scale", C.c_float), ("softcap", C.c_float), ("slopes", C.c_void_p), ("prefix_len", C.c_void_p), ("window", C.c_int32),
+                ("shared_len", C.c_int32)]
+
+
 class VlaError(RuntimeError):
     def __init__(self, code: int, message: str):
         super().__init__(f"libvla error {code}: {message}")
@@ -114,6 +134,14 @@ def lib() -> C.CDLL:
         L.vla_policy_objective_noalloc_max_traj.restype = C.c_int
         L.vla_policy_objective_noalloc.argtypes = [vp, vp, vp, i32, vp, i32, i32, f32, f32, i32, vp, vp, vp, vp]
         L.vla_logp_aggregate.argtypes = [vp, sz, i32, vp, vp]
+        i64, cache, batch = C.c_int64, C.POINTER(vla_paged_cache), C.POINTER(vla_paged_batch)
+        L.vla_paged_append.argtypes = [cache, batch, C.POINTER(vla_rotary), vp, vp, vp, i32, i32, i64, i64, i64, vp, i64, vp]
+        L.vla_paged_attention_workspace_bytes.argtypes = [cache, batch, C.POINTER(vla_paged_mask), i32]
+        L.vla_paged_attention_workspace_bytes.restype = sz
+        L.vla_paged_attention.argtypes = [cache, batch, C.POINTER(vla_paged_mask), vp, i32, i64, vp, i64, vp, vp, sz, vp]
+        L.vla_sample_logits_workspace_bytes.argtypes = [i32, i32]
+        L.vla_sample_logits_workspace_bytes.restype = sz
+        L.vla_sample_logits.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         dp = C.POINTER(C.c_double)
         L.vla_pipeline_time.argtypes = [C.c_double, C.c_double, i32, i32, dp]
         L.vla_profile_lookup.argtypes = [dp, i32, C.c_double, dp]
@@ -280,6 +308,133 @@ def vla_policy_objective_noalloc(logp_new, logp_old, adv, adv_per_step, mask, n_
 
 def vla_logp_aggregate(logp, n_out, inner, out, stream=None) -> None:
     _check(lib().vla_logp_aggregate(_ptr(logp), n_out, inner, _ptr(out), _stream(stream)))
+
+
+def _dtype(t) -> int:
+    import torch
+    code = {torch.float32: VLA_DTYPE_F32, torch.bfloat16: VLA_DTYPE_BF16}.get(t.dtype)
+    if code is None:
+        raise VlaError(VLA_EDTYPE, f"{t.dtype} is neither float32 nor bfloat16")
+    return code
+
+
+def _want(t, kind: str, name: str, shape=None):
+    """An array argument the library reads as packed values of one type: another type, shape or layout would be read wrongly."""
+    if t is None:
+        return None
+    if str(t.dtype) != "torch." + kind or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise VlaError(VLA_EINVAL, f"{name}: contiguous {kind}{'' if shape is None else ' ' + str(list(shape))} wanted, "
+                                   f"{t.dtype} {list(t.shape)} given")
+    return t.data_ptr()
+
+
+def _rows_of_heads(t, heads, dim, rows, name):
+    """Address and row stride of a [rows, heads, dim] view whose heads are packed within a row."""
+    if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
+        raise VlaError(VLA_ESHAPE, f"{name} is {list(t.shape)}, wanted [{rows}, {'heads' if heads is None else heads}, {dim}]")
+    if t.numel() and ((dim > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != dim)):
+        raise VlaError(VLA_EINVAL, f"{name}: the heads of a row are not packed (strides {t.stride()})")
+    width = t.shape[1] * dim
+    return t.data_ptr(), (t.stride(0) if rows > 1 else width)
+
+
+def make_paged_cache(k, v) -> vla_paged_cache:
+    """``k``, ``v``: device tensors [n_pages, n_kv_heads, page_size, head_dim]."""
+    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or not k.is_contiguous() or not v.is_contiguous():
+        raise VlaError(VLA_ESHAPE, "k and v are contiguous [n_pages, n_kv_heads, page_size, head_dim] tensors of one type")
+    n_pages, n_kv_heads, page_size, head_dim = k.shape
+    c = vla_paged_cache(k.data_ptr(), v.data_ptr(), _dtype(k), n_pages, page_size, n_kv_heads, head_dim)
+    c.keep = (k, v)
+    return c
+
+
+def make_paged_batch(row_start, kv_len, page_table, n_rows: int, max_rows: int, max_len: int) -> vla_paged_batch:
+    """``row_start`` [n_seq + 1], ``kv_len`` [n_seq], ``page_table`` [n_seq, entries]: int32 device tensors."""
+    n_seq = kv_len.shape[0]
+    if page_table.dim() != 2:
+        raise VlaError(VLA_ESHAPE, f"page_table is {list(page_table.shape)}, wanted [n_seq, entries]")
+    b = vla_paged_batch(n_seq, n_rows, max_rows, max_len, page_table.shape[1], _want(row_start, "int32", "row_start", (n_seq + 1,)),
+                        _want(kv_len, "int32", "kv_len", (n_seq,)), _want(page_table, "int32", "page_table", (n_seq, page_table.shape[1])))
+    b.keep = (row_start, kv_len, page_table)
+    return b
+
+
+def make_rotary(inv_freq=None, interleaved=False, scale=1.0, q_gain=None, k_gain=None, eps=1e-6) -> vla_rotary:
+    """``inv_freq``: fp64 device tensor [rot_dim / 2], or None for no rotation."""
+    r = vla_rotary(_want(inv_freq, "float64", "inv_freq"), 0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(interleaved)), scale, eps,
+                   _want(q_gain, "float32", "q_gain"), _want(k_gain, "float32", "k_gain"))
+    r.keep = (inv_freq, q_gain, k_gain)
+    return r
+
+
+def make_paged_mask(scale: float, softcap=0.0, slopes=None, prefix_len=None, window=0, shared_len=0) -> vla_paged_mask:
+    m = vla_paged_mask(scale, softcap, _want(slopes, "float32", "slopes"), _want(prefix_len, "int32", "prefix_len"), window, shared_len)
+    m.keep = (slopes, prefix_len)
+    return m
+
+
+def vla_paged_append(cache, batch, rotary, q, k, v, q_out=None, stream=None) -> None:
+    """``q`` [n_rows, n_heads, head_dim] (or None with ``q_out``), ``k``, ``v`` [n_rows, n_kv_heads, head_dim]: views with packed heads."""
+    d, rows = cache.head_dim, batch.n_rows
+    if (q is None) != (q_out is None):
+        raise VlaError(VLA_EINVAL, "paged_append: q and q_out come together")
+    for g, name in ((rotary.keep[1], "q_gain"), (rotary.keep[2], "k_gain")):
+        _want(g, "float32", name, (d,))
+    kp, ks = _rows_of_heads(k, cache.n_kv_heads, d, rows, "k")
+    vp_, vs = _rows_of_heads(v, cache.n_kv_heads, d, rows, "v")
+    qp = qs = op = os_ = 0
+    heads = cache.n_kv_heads
+    if q is not None:
+        heads = q.shape[1]
+        qp, qs = _rows_of_heads(q, None, d, rows, "q")
+        op, os_ = _rows_of_heads(q_out, heads, d, rows, "q_out")
+        if _dtype(q_out) != cache.dtype:
+            raise VlaError(VLA_EDTYPE, "paged_append: q_out has the cache's type")
+    if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+        raise VlaError(VLA_EDTYPE, "paged_append: q, k and v have one type")
+    _check(lib().vla_paged_append(C.byref(cache), C.byref(batch), C.byref(rotary), qp or None, kp, vp_, _dtype(k), heads, qs, ks, vs,
+                                  op or None, os_, _stream(stream)))
+
+
+def vla_paged_attention_workspace_bytes(cache, batch, mask, n_heads: int) -> int:
+    n = lib().vla_paged_attention_workspace_bytes(C.byref(cache), C.byref(batch), C.byref(mask), n_heads)
+    if n == 0:
+        raise VlaError(VLA_EINVAL, vla_last_error())
+    return n
+
+
+def vla_paged_attention(cache, batch, mask, q, out, lse=None, ws=None, stream=None) -> None:
+    heads, rows = q.shape[1], batch.n_rows
+    qp, qs = _rows_of_heads(q, None, cache.head_dim, rows, "q")
+    op, os_ = _rows_of_heads(out, heads, cache.head_dim, rows, "out")
+    if _dtype(q) != cache.dtype or _dtype(out) != cache.dtype:
+        raise VlaError(VLA_EDTYPE, "paged_attention: q and out have the cache's type")
+    _want(mask.keep[0], "float32", "slopes", (heads,))
+    _want(mask.keep[1], "int32", "prefix_len", (batch.n_seq,))
+    _check(lib().vla_paged_attention(C.byref(cache), C.byref(batch), C.byref(mask), qp, heads, qs, op, os_,
+                                     _want(lse, "float32", "lse", (rows, heads)), _ptr(ws),
+                                     0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def vla_sample_logits_workspace_bytes(n: int, vocab: int) -> int:
+    size = lib().vla_sample_logits_workspace_bytes(n, vocab)
+    if size == 0:
+        raise VlaError(VLA_EINVAL, vla_last_error())
+    return size
+
+
+def vla_sample_logits(logits, token, temperature=None, top_k=None, top_p=None, min_p=None, u=None, logp=None, logp_kept=None, n_kept=None,
+                      ws=None, stream=None) -> None:
+    """``logits`` [n, vocab] (rows may be apart); one value per row in everything else."""
+    if logits.dim() != 2 or (logits.numel() and logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise VlaError(VLA_ESHAPE, f"logits: rows of consecutive values wanted, {list(logits.shape)} with strides {logits.stride()} given")
+    n, vocab = logits.shape
+    f = lambda t, name: _want(t, "float32", name, (n,))
+    i = lambda t, name: _want(t, "int32", name, (n,))
+    _check(lib().vla_sample_logits(logits.data_ptr(), _dtype(logits), logits.stride(0) if n > 1 else vocab, n, vocab, f(temperature, "temperature"),
+                                   i(top_k, "top_k"), f(top_p, "top_p"), f(min_p, "min_p"), f(u, "u"), i(token, "token"), f(logp, "logp"),
+                                   f(logp_kept, "logp_kept"), i(n_kept, "n_kept"), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+                                   _stream(stream)))
 
 
 def _doubles(values):
