@@ -340,7 +340,8 @@ int vla_policy_objective_noalloc(const float *logp_new, const float *logp_old, c
  *   key gets zeros and -inf.  K and V of visible positions are taken to be finite where any row of the call masks them.
  *   vla_paged_mask: scale > 0; softcap, window >= 0; slopes DEVICE fp32 [n_heads]; prefix_len DEVICE int32 [n_seq]; shared_len
  *   (HOST): a multiple of page_size; the first shared_len positions of all sequences lie in the same pages, which are read once
- *   for the whole batch, through sequence 0's table (every sequence with rows must hold shared_len positions or more).
+ *   for the whole batch, through sequence 0's table (sequence 0 and every sequence with rows hold shared_len positions
+ *   or more); not together with a window.
  *   ws: DEVICE, 16-byte aligned, of vla_paged_attention_workspace_bytes (from HOST numbers alone) bytes: partial sums of split key ranges; no state.
  *   Sums are added in a fixed order: the same call gives the same bits; the split depends on the HOST numbers.
  *

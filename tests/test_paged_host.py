@@ -71,7 +71,7 @@ def test_attention_refuses():
         assert attend(**k) == code, k
     for mask, code in [(m(0.0, 0.0, None, None, 0, 0), vb.VLA_EINVAL), (m(float("nan"), 0.0, None, None, 0, 0), vb.VLA_EINVAL), (m(float("inf"), 0.0, None, None, 0, 0), vb.VLA_EINVAL),
                        (m(1.0, -1.0, None, None, 0, 0), vb.VLA_EINVAL), (m(1.0, 0.0, None, None, -1, 0), vb.VLA_EINVAL), (m(1.0, 0.0, None, None, 0, -16), vb.VLA_EINVAL),
-                       (m(1.0, 0.0, None, None, 0, 8), vb.VLA_ESHAPE), (m(1.0, 0.0, None, None, 0, 48), vb.VLA_ESHAPE)]:
+                       (m(1.0, 0.0, None, None, 0, 8), vb.VLA_ESHAPE), (m(1.0, 0.0, None, None, 0, 48), vb.VLA_ESHAPE), (m(1.0, 0.0, None, None, 5, 16), vb.VLA_EINVAL)]:
         assert attend(m=mask) == code
     assert attend(b=batch(n_rows=0)) == vb.VLA_OK
     q = lambda **k: vb.lib().vla_paged_attention_workspace_bytes(C.byref(cache(**k)), C.byref(batch()), C.byref(m(1.0, 0.0, None, None, 0, 0)), 4)
