@@ -4,12 +4,18 @@
 // larger number comes earlier.  Every cut keeps a leading run of that order, so the kept set is one threshold on that
 // number.  Masses are w = exp((z - max) / T) in fp64, rounded to multiples of 2^-44 and summed as whole numbers: the sums are exact,
 // in any order, and the border cases of top-p and of u fall alike every time (2^18 tokens of mass 1 stay below 2^63).
+//
+// One workgroup a row.  Up to LIST tokens (the whole row, or what a count over bins of the value leaves for top-k) are sorted in
+// LDS; the cuts are then places in a running sum.  Longer rows with top-p alone: masses over bins of 1/32 in log2 units find the
+// bin in which the cut falls, and the tokens of that bin are sorted.  The row is read again from the caches for each step:
+// its maximum; the bins; the tokens of the border bin and the kept mass of every 2048 ids; and the 2048 ids in which u falls.
 #include "vla_internal.h"
 
 namespace {
 
-constexpr int THREADS = 1024;
 constexpr double UNIT = 17592186044416.0;      // 2^44
+constexpr int LIST = 4096, BINS = 2048, SEGMENT = 2048, MAX_VOCAB = 262144;
+typedef unsigned long long u64;
 
 struct SampleArgs {
     const char *logits;
@@ -30,102 +36,198 @@ __device__ __forceinline__ unsigned order_of(float z) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(unsigned o) { return __builtin_bit_cast(float, o & 0x80000000u ? o & 0x7fffffffu : ~o); }
-__device__ __forceinline__ unsigned long long rank_key(unsigned order, int id) { return (unsigned long long)order << 32 | (unsigned)~id; }
+__device__ __forceinline__ u64 rank_key(unsigned order, int id) { return (u64)order << 32 | (unsigned)~id; }
+__device__ __forceinline__ int id_of(u64 key) { return (int)~(unsigned)key; }
+__device__ __forceinline__ float value_at(u64 key) { return value_of((unsigned)(key >> 32)); }
 
-__device__ __forceinline__ unsigned long long wave_sum(unsigned long long v) {
+__device__ __forceinline__ u64 wave_sum(u64 v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     return v;
 }
-__device__ __forceinline__ unsigned long long wave_max(unsigned long long v) {
+__device__ __forceinline__ u64 wave_max(u64 v) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) { const unsigned long long w = __shfl_xor(v, o, 64); v = w > v ? w : v; }
+    for (int o = 32; o > 0; o >>= 1) { const u64 w = __shfl_xor(v, o, 64); v = w > v ? w : v; }
     return v;
 }
-struct Both { unsigned long long count, mass; };
-// Sums (or the maximum of `count`) over the workgroup, to all threads.
-__device__ __forceinline__ Both block_both(Both v, bool largest, unsigned long long (*red)[THREADS / 64]) {
-    v.count = largest ? wave_max(v.count) : wave_sum(v.count);
-    v.mass = wave_sum(v.mass);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) { red[0][threadIdx.x >> 6] = v.count; red[1][threadIdx.x >> 6] = v.mass; }
-    __syncthreads();
-    Both r{0, 0};
-    for (int i = 0; i < THREADS / 64; i++) {
-        r.count = largest ? (red[0][i] > r.count ? red[0][i] : r.count) : r.count + red[0][i];
-        r.mass += red[1][i];
-    }
-    return r;
+__device__ __forceinline__ u64 wave_scan(u64 v) {            // inclusive
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const u64 w = __shfl_up(v, o, 64); if (lane >= o) v += w; }
+    return v;
 }
 
-// One workgroup per row; each cut by bisection of the order's 50 bits, a pass over the row a bit.
-template <typename T>
-__global__ void __launch_bounds__(THREADS) sample_rows_kernel(SampleArgs a) {
-    __shared__ unsigned long long red[2][THREADS / 64];
-    __shared__ unsigned long long scan[THREADS];
-    const int row = blockIdx.x, t = threadIdx.x, V = a.vocab;
-    const T *z = (const T *)a.logits + row * a.stride;
-    Both top{0, 0};
-    for (int i = t; i < V; i += THREADS) {
-        const unsigned o = order_of((float)z[i]);
-        if (o) { const unsigned long long k = rank_key(o, i); top.count = k > top.count ? k : top.count; }
-    }
-    const unsigned long long first = block_both(top, true, red).count;
-    if (first == 0) {
-        if (t == 0) {
-            a.token[row] = -1;
-            if (a.logp) a.logp[row] = -INFINITY;
-            if (a.logp_kept) a.logp_kept[row] = -INFINITY;
-            if (a.n_kept) a.n_kept[row] = 0;
+// 2^y for y <= 0, relative error below 1e-14: 2^f by its series in f ln 2 (|f ln 2| <= 0.347), the last term left out 6e-15.
+__device__ __forceinline__ double exp2_neg(double y) {
+    const double n = __builtin_rint(y), x = (y - n) * 0.69314718055994530942;
+    double p = 1.0 / 39916800.0;
+    p = __builtin_fma(p, x, 1.0 / 3628800.0);
+    p = __builtin_fma(p, x, 1.0 / 362880.0);
+    p = __builtin_fma(p, x, 1.0 / 40320.0);
+    p = __builtin_fma(p, x, 1.0 / 5040.0);
+    p = __builtin_fma(p, x, 1.0 / 720.0);
+    p = __builtin_fma(p, x, 1.0 / 120.0);
+    p = __builtin_fma(p, x, 1.0 / 24.0);
+    p = __builtin_fma(p, x, 1.0 / 6.0);
+    p = __builtin_fma(p, x, 0.5);
+    p = __builtin_fma(p, x, 1.0);
+    p = __builtin_fma(p, x, 1.0);
+    return __builtin_ldexp(p, n < -2000.0 ? -2000 : (int)n);
+}
+// w in [0, 1] to multiples of 2^-44: added to 2^52 its rounded multiple stands in the low bits.
+__device__ __forceinline__ u64 units_of(double w) { return __builtin_bit_cast(u64, __builtin_fma(w, UNIT, 4503599627370496.0)) & 0xfffffffffffffull; }
+
+// A row's masses: w = exp2((z - max) rate).
+struct Scale {
+    double zmax, rate;
+    __device__ __forceinline__ double weight(float z) const { return exp2_neg(((double)z - zmax) * rate); }
+    __device__ __forceinline__ u64 units(float z) const { return units_of(weight(z)); }
+    // bins of 1/32 in log2 units, never descending in -z; below 2^-63 all one
+    __device__ __forceinline__ int bin(float z) const { return (int)fmin((zmax - (double)z) * (rate * 32.0), (double)(BINS - 1)); }
+};
+
+struct Both { u64 count, mass; };
+template <int THREADS> struct Block {
+    u64 red[2][THREADS / 64];
+    // Sums (or the maximum of `count`) over the workgroup, to all threads.
+    __device__ Both both(Both v, bool largest = false) {
+        v.count = largest ? wave_max(v.count) : wave_sum(v.count);
+        v.mass = wave_sum(v.mass);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) { red[0][threadIdx.x >> 6] = v.count; red[1][threadIdx.x >> 6] = v.mass; }
+        __syncthreads();
+        Both r{0, 0};
+        for (int i = 0; i < THREADS / 64; i++) {
+            r.count = largest ? (red[0][i] > r.count ? red[0][i] : r.count) : r.count + red[0][i];
+            r.mass += red[1][i];
         }
-        return;
+        return r;
     }
-    const float zmax = value_of((unsigned)(first >> 32));
+    // What lies before this thread's value, in thread order.
+    __device__ u64 before(u64 v) {
+        const u64 in = wave_scan(v);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 63) red[0][threadIdx.x >> 6] = in;
+        __syncthreads();
+        u64 b = in - v;
+        for (int i = 0; i < (int)(threadIdx.x >> 6); i++) b += red[0][i];
+        return b;
+    }
+};
+
+// LDS of a workgroup.
+template <int THREADS> struct Room {
+    u64 keys[LIST];              // the list, sorted: largest key first; zeros behind it
+    union { u64 mass[BINS]; unsigned count[BINS]; u64 bucket[BINS]; };
+    u64 segment[MAX_VOCAB / SEGMENT];
+    Block<THREADS> block;
+    int n;                       // tokens that asked for a place in the list
+    int found, which;
+    u64 found_before;
+};
+
+// keys[0 .. P), P a power of two, from the largest to the smallest.  Pairs of a distance up to 64 lie in the 128 keys of one wave's
+// threads, whose LDS accesses take place in order: only longer distances need the workgroup's barrier.
+template <int THREADS> __device__ void sort_keys(u64 *keys, int P) {
+    __syncthreads();
+    for (int k = 2; k <= P; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            if (j >= 128 && j == k >> 1) __syncthreads();
+            for (int q = threadIdx.x; q < P / 2; q += THREADS) {
+                const int i = ((q & ~(j - 1)) << 1) | (q & (j - 1));
+                const u64 x = keys[i], y = keys[i + j];
+                if (((i & k) == 0) == (x < y)) { keys[i] = y; keys[i + j] = x; }
+            }
+            if (j >= 128) __syncthreads();
+            else asm volatile("" ::: "memory");
+        }
+    __syncthreads();
+}
+
+// Tokens of ids [segment * SEGMENT, ...) to f, by one wave: 16 bytes a load, all of the segment's asked for before the first is used.
+template <typename T, typename F> __device__ __forceinline__ void each_of_segment(const T *z, int V, int segment, F f) {
+    constexpr int W = 16 / (int)sizeof(T), STEPS = SEGMENT / (64 * W);
+    typedef T tw __attribute__((ext_vector_type(W), aligned(sizeof(T))));
+    const int i0 = segment * SEGMENT + (threadIdx.x & 63) * W;
+    if (segment * SEGMENT + SEGMENT <= V) {
+        tw v[STEPS];
+#pragma unroll
+        for (int s = 0; s < STEPS; s++) v[s] = *(const tw *)(z + i0 + s * 64 * W);
+#pragma unroll
+        for (int s = 0; s < STEPS; s++)
+#pragma unroll
+            for (int e = 0; e < W; e++) f((float)v[s][e], i0 + s * 64 * W + e);
+    } else
+        for (int s = 0; s < STEPS; s++)
+#pragma unroll
+            for (int e = 0; e < W; e++) {
+                const int i = i0 + s * 64 * W + e;
+                if (i < V) f((float)z[i], i);
+            }
+}
+template <int THREADS, typename T, typename F> __device__ __forceinline__ void each_token(const T *z, int V, F f) {
+    for (int s = threadIdx.x >> 6; s * SEGMENT < V; s += THREADS / 64) each_of_segment(z, V, s, f);
+}
+
+// Whether a token of mass w, with `run` before it in id order, is the one: the first whose sum exceeds `want`; the last with mass
+// should none (u that is no number below 1).
+__device__ __forceinline__ bool falls_in(u64 run, u64 w, double want, u64 total) {
+    const bool over = (double)(run + w) > want;
+    return w && (over ? run == 0 || !((double)run > want) : run + w == total);
+}
+
+// What the other ways decline (infinite logits; more than LIST tokens in one bin of a cut): each cut by bisection of the order's 50 bits, a pass
+// over the row a bit.
+template <int THREADS, typename T> __device__ void sample_by_bisection(const SampleArgs &a, const T *z, int row, u64 first, Room<THREADS> &room) {
+    const int t = threadIdx.x, V = a.vocab;
+    Block<THREADS> &block = room.block;
+    u64 *scan = room.mass;
+    const float zmax = value_at(first);
     const float T0 = a.temperature ? a.temperature[row] : 1.f;
-    const bool greedy = !(T0 > 0.f) || !a.u;
-    const double inv_t = T0 > 0.f ? (double)T0 : 1.0;
     const bool infinite = zmax == INFINITY;
-    auto weight = [&](float v) { return infinite ? (v == INFINITY ? 1.0 : 0.0) : exp(((double)v - (double)zmax) / inv_t); };
-    auto units = [&](float v) { return (unsigned long long)(weight(v) * UNIT + 0.5); };
+    const bool greedy = !(T0 > 0.f) || !a.u;
+    const Scale sc{infinite ? 0.0 : (double)zmax, 1.4426950408889634074 / (T0 > 0.f ? (double)T0 : 1.0)};
+    auto weight = [&](float v) { return infinite ? (v == INFINITY ? 1.0 : 0.0) : sc.weight(v); };
+    auto units = [&](float v) { return units_of(weight(v)); };
     // count and mass of what lies at or above a threshold
-    auto above = [&](unsigned long long least) {
+    auto above = [&](u64 least) {
         Both b{0, 0};
         for (int i = t; i < V; i += THREADS) {
             const float v = (float)z[i];
             const unsigned o = order_of(v);
             if (o && rank_key(o, i) >= least) { b.count++; b.mass += units(v); }
         }
-        return block_both(b, false, red);
+        return block.both(b);
     };
     // the largest threshold that holds at least what `enough` asks for; below it nothing changes what was asked
     auto bisect = [&](auto enough) {
-        unsigned long long lo = 1ull, hi = first;                    // enough(lo) by assumption
+        u64 lo = 1ull, hi = first;                    // enough(lo) by assumption
         while (lo < hi) {
-            const unsigned long long mid = lo + (hi - lo + 1) / 2;
+            const u64 mid = lo + (hi - lo + 1) / 2;
             if (enough(above(mid))) lo = mid; else hi = mid - 1;
         }
         return lo;
     };
     const Both all = above(1);
-    unsigned long long cut = 1, leading = all.mass;
-    if (infinite) cut = (unsigned long long)order_of(INFINITY) << 32;
+    u64 cut = 1, leading = all.mass;
+    if (infinite) cut = (u64)order_of(INFINITY) << 32;
     const int k = a.top_k ? a.top_k[row] : 0;
-    if (k > 0 && (unsigned long long)k < all.count) {
-        const unsigned long long c = bisect([&](Both b) { return b.count >= (unsigned long long)k; });
+    if (k > 0 && (u64)k < all.count) {
+        const u64 c = bisect([&](Both b) { return b.count >= (u64)k; });
         cut = c > cut ? c : cut;
         leading = above(cut).mass;
     }
     const float p = a.top_p ? a.top_p[row] : 1.f;
     if (p < 1.f) {
         const double want = (double)(p > 0.f ? p : 0.f) * (double)leading;
-        const unsigned long long c = bisect([&](Both b) { return (double)b.mass >= want; });
+        const u64 c = bisect([&](Both b) { return (double)b.mass >= want; });
         cut = c > cut ? c : cut;
     }
     const float least = a.min_p ? a.min_p[row] : 0.f;
     auto kept = [&](float v, int i) {
         const unsigned o = order_of(v);
         if (!o) return false;
-        const unsigned long long key = rank_key(o, i);
+        const u64 key = rank_key(o, i);
         return key == first || (key >= cut && weight(v) >= (double)least);
     };
     // ids in runs of consecutive ones per thread: running masses in id order
@@ -135,38 +237,281 @@ __global__ void __launch_bounds__(THREADS) sample_rows_kernel(SampleArgs a) {
         const float v = (float)z[i];
         if (kept(v, i)) { mine.count++; mine.mass += units(v); }
     }
-    const Both total = block_both(mine, false, red);
+    const Both total = block.both(mine);
     scan[t] = mine.mass;
     __syncthreads();
     if (t == 0) {
-        unsigned long long run = 0;
-        for (int i = 0; i < THREADS; i++) { const unsigned long long x = scan[i]; scan[i] = run; run += x; }
+        u64 run = 0;
+        for (int i = 0; i < THREADS; i++) { const u64 x = scan[i]; scan[i] = run; run += x; }
     }
     __syncthreads();
-    int token = (int)~(unsigned)first;
+    int token = id_of(first);
     if (!greedy) {
         const float u = a.u[row];
         const double want = (double)u * (double)total.mass;
-        // the first id whose running mass exceeds `want`; the last kept one with mass should rounding leave none
         Both pick{0, 0};
-        unsigned long long run = scan[t];
+        u64 run = scan[t];
         for (int i = i0; i < i1; i++) {
             const float v = (float)z[i];
             if (!kept(v, i)) continue;
-            const unsigned long long w = units(v);
-            const bool over = (double)(run + w) > want;
-            if (w && ((over && !((double)run > want)) || (!over && run + w == total.mass))) pick.count = (unsigned)i + 1ull;
+            const u64 w = units(v);
+            if (falls_in(run, w, want, total.mass)) pick.count = (unsigned)i + 1ull;
             run += w;
         }
-        token = (int)block_both(pick, true, red).count - 1;
+        token = (int)block.both(pick, true).count - 1;
     }
     if (t == 0) {
         const float v = (float)z[token];
-        const double y = infinite ? 0.0 : ((double)v - (double)zmax) / inv_t;
+        const double y = infinite ? 0.0 : ((double)v - sc.zmax) * sc.rate * 0.69314718055994530942;
         a.token[row] = token;
         if (a.logp) a.logp[row] = (float)(y - log((double)all.mass / UNIT));
         if (a.logp_kept) a.logp_kept[row] = (float)(y - log((double)total.mass / UNIT));
         if (a.n_kept) a.n_kept[row] = (int)total.count;
+    }
+}
+
+
+template <int THREADS, typename T> __global__ void __launch_bounds__(THREADS) sample_rows_kernel(SampleArgs a) {
+    __shared__ Room<THREADS> room;
+    Block<THREADS> &block = room.block;
+    const int row = blockIdx.x, t = threadIdx.x, V = a.vocab;
+    const T *z = (const T *)a.logits + row * a.stride;
+    const bool whole = THREADS < 1024 || V <= LIST;          // the row itself is the list
+    // ---- the largest, and how many there are
+    Both top{0, 0};
+    int P = 2;                             // places of the list, a power of two
+    if (whole) {
+        while (P < V) P <<= 1;
+        for (int i = t; i < P; i += THREADS) {
+            const unsigned o = i < V ? order_of((float)z[i]) : 0u;
+            const u64 key = o ? rank_key(o, i) : 0;
+            room.keys[i] = key;
+            top.count = key > top.count ? key : top.count;
+            top.mass += o != 0;
+        }
+    } else {
+        float best = -INFINITY;
+        int at = 0;
+        each_token<THREADS>(z, V, [&](float v, int i) {
+            if (v > best) { best = v; at = i; }              // (a lane's ids ascend: the lowest of equals stays)
+            top.mass += v > -INFINITY;
+        });
+        const unsigned o = order_of(best);
+        top.count = o ? rank_key(o, at) : 0;
+    }
+    top = block.both(top, true);
+    const u64 first = top.count;
+    const int valid = (int)top.mass;
+    if (first == 0) {
+        if (t == 0) {
+            a.token[row] = -1;
+            if (a.logp) a.logp[row] = -INFINITY;
+            if (a.logp_kept) a.logp_kept[row] = -INFINITY;
+            if (a.n_kept) a.n_kept[row] = 0;
+        }
+        return;
+    }
+    const float zmax = value_at(first), T0 = a.temperature ? a.temperature[row] : 1.f;
+    if (zmax == INFINITY) { sample_by_bisection<THREADS>(a, z, row, first, room); return; }
+    const bool greedy = !(T0 > 0.f) || !a.u;
+    const Scale sc{(double)zmax, 1.4426950408889634074 / (T0 > 0.f ? (double)T0 : 1.0)};
+    int k = a.top_k ? a.top_k[row] : 0;
+    if (k <= 0 || k >= valid) k = valid;
+    const float p = a.top_p ? a.top_p[row] : 1.f, least = a.min_p ? a.min_p[row] : 0.f;
+    const bool cut_k = k < valid, cut_p = p < 1.f;
+    const double share = p > 0.f ? (double)p : 0.0;
+    const bool ranked = whole || cut_k;    // the list holds all leading tokens (else: those of the bin in which the cut of top-p falls)
+
+    u64 all_mass = 0, kept_mass = 0, above = 0;      // of the row; of the kept tokens; of the bins before the border
+    int n_kept = 0, border = BINS;
+    double limit = 0.0;                              // mass before a token at which top-p ends
+    if (!whole) {
+        // ---- bins: where the cut falls
+        if (cut_k || cut_p) {
+            for (int i = t; i < BINS; i += THREADS) room.mass[i] = 0;
+            __syncthreads();
+            Both all{0, 0};
+            each_token<THREADS>(z, V, [&](float v, int) {
+                if (!(v > -INFINITY)) return;
+                const u64 w = sc.units(v);
+                if (cut_k) {
+                    all.mass += w;
+                    atomicAdd(&room.count[sc.bin(v)], 1u);
+                } else atomicAdd(&room.mass[sc.bin(v)], w);
+            });
+            if (cut_k) all_mass = block.both(all).mass;
+            __syncthreads();
+            constexpr int RUN = BINS / THREADS;
+            u64 mine[RUN], sum = 0;
+#pragma unroll
+            for (int e = 0; e < RUN; e++) { mine[e] = cut_k ? room.count[t * RUN + e] : room.mass[t * RUN + e]; sum += mine[e]; }
+            u64 run = block.before(sum);
+            if (!cut_k) {
+                all_mass = block.both(Both{0, sum}).mass;
+                limit = share * (double)all_mass;
+            }
+            auto reached = [&](u64 x) { return cut_k ? x >= (u64)k : (double)x >= limit; };
+#pragma unroll
+            for (int e = 0; e < RUN; e++) {          // (top-p of nothing: the first bin)
+                if (reached(run + mine[e]) && (!reached(run) || t + e == 0)) { room.found = t * RUN + e; room.found_before = run; }
+                run += mine[e];
+            }
+            __syncthreads();
+            border = room.found;
+            above = cut_k ? 0 : room.found_before;
+        }
+        // ---- the list; without top-k also the mass of the other kept tokens, by segment
+        if (t == 0) room.n = 0;
+        __syncthreads();
+        auto enlist = [&](float v, int i) {
+            const int at = atomicAdd(&room.n, 1);
+            if (at < LIST) room.keys[at] = rank_key(order_of(v), i);
+        };
+        if (cut_k) {
+            each_token<THREADS>(z, V, [&](float v, int i) {
+                if (v > -INFINITY && sc.bin(v) <= border) enlist(v, i);
+            });
+        } else {
+            u64 rest = 0;                            // not kept for min-p alone
+            for (int s = t >> 6; s * SEGMENT < V; s += THREADS / 64) {
+                u64 m = 0;
+                each_of_segment(z, V, s, [&](float v, int i) {
+                    if (!(v > -INFINITY)) return;
+                    if (cut_p) {
+                        const int b = sc.bin(v);
+                        if (b == border) enlist(v, i);
+                        if (b >= border) return;
+                    }
+                    const double w = sc.weight(v);
+                    if (w >= (double)least || (v == zmax && i == id_of(first))) { m += units_of(w); n_kept++; }
+                    else rest += units_of(w);
+                });
+                m = wave_sum(m);
+                if ((t & 63) == 0) room.segment[s] = m;
+            }
+            if (!cut_p) all_mass = block.both(Both{0, rest}).mass;          // (the kept ones' join below)
+        }
+        __syncthreads();
+        const int m = room.n;
+        if (m > LIST) { sample_by_bisection<THREADS>(a, z, row, first, room); return; }
+        while (P < m) P <<= 1;
+        for (int i = m + t; i < P; i += THREADS) room.keys[i] = 0;
+    }
+    // ---- sorted, the cuts are places in the running sum
+    int kept = 0;                          // of the list
+    if (ranked || cut_p) {
+        sort_keys<THREADS>(room.keys, P);
+        const int per = (P + THREADS - 1) / THREADS, i0 = t * per, i1 = min(P, i0 + per), leading = ranked ? k : P;
+        u64 all = 0, sum = 0;
+        for (int i = i0; i < i1; i++) {
+            const u64 key = room.keys[i], w = key ? sc.units(value_at(key)) : 0;
+            all += w;
+            if (i < leading) sum += w;
+        }
+        u64 run = above + block.before(sum);
+        const Both sums = block.both(Both{all, sum});
+        if (whole) all_mass = sums.count;
+        if (ranked) limit = share * (double)sums.mass;
+        Both c{0, 0};
+        for (int i = i0; i < min(i1, leading); i++) {
+            const u64 key = room.keys[i];
+            if (!key) break;
+            const double x = sc.weight(value_at(key));
+            const u64 w = units_of(x);
+            if (key == first || ((!cut_p || (double)run < limit) && x >= (double)least)) { c.count++; c.mass += w; }
+            run += w;
+        }
+        c = block.both(c);
+        kept = (int)c.count;
+        kept_mass = c.mass;
+    }
+    int token = id_of(first);
+    if (ranked) {
+        n_kept = kept;
+        // ---- in id order: masses of buckets of ids, then the ids of the bucket in which u falls
+        if (!greedy) {
+            int shift = 0;
+            while (((V - 1) >> shift) >= BINS) shift++;
+            for (int i = t; i < BINS; i += THREADS) room.bucket[i] = 0;
+            if (t == 0) room.n = 0;
+            __syncthreads();
+            for (int i = t; i < kept; i += THREADS) atomicAdd(&room.bucket[id_of(room.keys[i]) >> shift], sc.units(value_at(room.keys[i])));
+            __syncthreads();
+            const double want = (double)a.u[row] * (double)kept_mass;
+            constexpr int RUN = BINS / THREADS;
+            u64 mine[RUN], sum = 0;
+#pragma unroll
+            for (int e = 0; e < RUN; e++) { mine[e] = room.bucket[t * RUN + e]; sum += mine[e]; }
+            u64 run = block.before(sum);
+#pragma unroll
+            for (int e = 0; e < RUN; e++) {
+                if (falls_in(run, mine[e], want, kept_mass)) { room.found = t * RUN + e; room.found_before = run; }
+                run += mine[e];
+            }
+            __syncthreads();
+            const int bucket = room.found;
+            // its tokens, at most 2^shift <= 128, take the buckets' place
+            for (int i = t; i < kept; i += THREADS)
+                if (id_of(room.keys[i]) >> shift == bucket) room.bucket[atomicAdd(&room.n, 1)] = room.keys[i];
+            __syncthreads();
+            const int m = room.n;
+            Both pick{0, 0};
+            if (t < m) {
+                const u64 key = room.bucket[t];
+                u64 r = room.found_before;
+                for (int j = 0; j < m; j++)
+                    if (id_of(room.bucket[j]) < id_of(key)) r += sc.units(value_at(room.bucket[j]));
+                if (falls_in(r, sc.units(value_at(key)), want, kept_mass)) pick.count = (u64)id_of(key) + 1;
+            }
+            token = (int)block.both(pick, true).count - 1;
+        }
+    } else {
+        // ---- the list's kept tokens join their segments; the segment in which u falls is read once more
+        const u64 last = kept > 0 ? room.keys[kept - 1] : ~0ull;
+        for (int i = t; i < kept; i += THREADS) atomicAdd(&room.segment[id_of(room.keys[i]) / SEGMENT], sc.units(value_at(room.keys[i])));
+        __syncthreads();
+        const u64 mine = t * SEGMENT < V ? room.segment[t] : 0;
+        const u64 run = block.before(mine);
+        const Both sums = block.both(Both{(u64)n_kept, mine});
+        n_kept = (int)sums.count + kept;
+        kept_mass = sums.mass;
+        if (!cut_p) all_mass += kept_mass;
+        if (!greedy) {
+            const double want = (double)a.u[row] * (double)kept_mass;
+            if (falls_in(run, mine, want, kept_mass)) { room.found = t; room.found_before = run; }
+            __syncthreads();
+            const int i0 = room.found * SEGMENT;
+            constexpr int RUN = SEGMENT / THREADS;
+            u64 w[RUN], sum = 0;
+#pragma unroll
+            for (int e = 0; e < RUN; e++) {
+                const int i = i0 + t * RUN + e;
+                const float v = i < V ? (float)z[i] : -INFINITY;
+                w[e] = 0;
+                if (v > -INFINITY) {
+                    const u64 key = rank_key(order_of(v), i);
+                    const int b = cut_p ? sc.bin(v) : 0;
+                    const double x = sc.weight(v);
+                    if ((b < border || (b == border && key >= last)) && (x >= (double)least || key == first)) w[e] = units_of(x);
+                }
+                sum += w[e];
+            }
+            u64 r = room.found_before + block.before(sum);
+            Both pick{0, 0};
+#pragma unroll
+            for (int e = 0; e < RUN; e++) {
+                if (falls_in(r, w[e], want, kept_mass)) pick.count = (u64)(i0 + t * RUN + e) + 1;
+                r += w[e];
+            }
+            token = (int)block.both(pick, true).count - 1;
+        }
+    }
+    if (t == 0) {
+        const double y = ((double)(float)z[token] - sc.zmax) * sc.rate * 0.69314718055994530942;
+        a.token[row] = token;
+        if (a.logp) a.logp[row] = (float)(y - log((double)all_mass / UNIT));
+        if (a.logp_kept) a.logp_kept[row] = (float)(y - log((double)kept_mass / UNIT));
+        if (a.n_kept) a.n_kept[row] = n_kept;
     }
 }
 
@@ -192,8 +537,15 @@ int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, 
     const SampleArgs a{(const char *)logits, (long)row_stride, n, vocab, temperature, top_k, top_p, min_p, u, token, logp, logp_kept, n_kept};
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps("sample_logits", (double)n * vocab * (dtype == VLA_DTYPE_F32 ? 4.0 : 2.0), st);
-    if (dtype == VLA_DTYPE_F32) sample_rows_kernel<float><<<n, THREADS, 0, st>>>(a);
-    else sample_rows_kernel<bf16_t><<<n, THREADS, 0, st>>>(a);
+    const bool f32 = dtype == VLA_DTYPE_F32;
+    // (a row of up to 1024 tokens sorts in few steps of few waves: smaller workgroups, three a CU)
+    if (vocab <= 1024) {
+        if (f32) sample_rows_kernel<256, float><<<n, 256, 0, st>>>(a);
+        else sample_rows_kernel<256, bf16_t><<<n, 256, 0, st>>>(a);
+    } else {
+        if (f32) sample_rows_kernel<1024, float><<<n, 1024, 0, st>>>(a);
+        else sample_rows_kernel<1024, bf16_t><<<n, 1024, 0, st>>>(a);
+    }
     return vla_check_launch("sample_logits");
 }
 
