@@ -41,6 +41,7 @@ struct AttnArgs {
     const float *slopes;
     const int32_t *prefix_len;
     int window, shared_len;
+    float offset;            // what scores lack, in log2 units (see Rows::tile): lse alone knows it
     int aligned;             // rows of q and out start at multiples of 16 bytes
     // this launch
     int whole;               // packed rows of the whole batch against the shared positions
@@ -108,6 +109,8 @@ template <typename T, int DP> struct Tile {
     }
 };
 
+constexpr int CAPPED = 1, BIASED = 2;          // bits of MODE
+
 // What one lane knows of its query.
 struct Query {
     int row, head;           // of the call
@@ -116,7 +119,7 @@ struct Query {
     float slope;
 };
 
-template <bool PLAIN>
+template <int MODE>
 __device__ __forceinline__ Query make_query(const AttnArgs &a, int kvh, int s, int row, int i, const PagedSeq &sq, int hg, bool valid) {
     Query q;
     q.row = row;
@@ -128,12 +131,12 @@ __device__ __forceinline__ Query make_query(const AttnArgs &a, int kvh, int s, i
     q.lo = a.whole ? 0 : a.shared_len;
     if (a.window) q.lo = max(0, q.p + 1 - a.window);
     else { q.hi = max(q.hi, q.pre); q.pre = 0; }
-    q.slope = !PLAIN && a.slopes && valid ? a.slopes[q.head] : 0.f;
+    q.slope = (MODE & BIASED) && valid ? a.slopes[q.head] : 0.f;
     if (!valid) { q.hi = 0x7fffffff; q.lo = 0; }
     return q;
 }
 
-template <typename T, int DP, bool PLAIN> struct Rows {
+template <typename T, int DP, int MODE> struct Rows {
     typedef typename FragOf<T>::type frag;
     typedef Tile<T, DP> TL;
     static constexpr int KS = DP / 16, DB = DP / 32;
@@ -191,23 +194,33 @@ template <typename T, int DP, bool PLAIN> struct Rows {
                 x[n] = mma(k, q[kk], x[n]);
             }
         }
+        // scores in log2 units are x unit (+ AttnArgs::offset, which changes no weight)
         constexpr float LOG2E = 1.4426950408889634f;
-        float unit = a.scale * LOG2E;                        // scores -> log2 units
-        if (!PLAIN) {
-            unit = LOG2E;
-            const float back = a.cap > 0.f ? a.scale / a.cap : 0.f;
+        float unit = a.scale * LOG2E;
+        if (MODE & CAPPED) {
+            if constexpr (sizeof(T) == 4) {
+                const float back = a.scale / a.cap;
+                unit = a.cap * LOG2E;
+#pragma unroll
+                for (int n = 0; n < NB; n++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) x[n][i] = tanhf(x[n][i] * back);
+            } else {                                         // tanh t = 1 - 2 / (1 + e^2t); the 1 is the offset
+                const float twice = 2.f * LOG2E * a.scale / a.cap;
+                unit = 2.f * a.cap * LOG2E;
+#pragma unroll
+                for (int n = 0; n < NB; n++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) x[n][i] = -__builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[n][i] * twice));
+            }
+        }
+        if (MODE & BIASED) {
+            const float slope = -y.slope * LOG2E, away = (float)(y.p - key0 - 4 * hh);
 #pragma unroll
             for (int n = 0; n < NB; n++)
 #pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    float s = x[n][i] * a.scale;
-                    if (a.cap > 0.f) {
-                        if constexpr (sizeof(T) == 4) s = a.cap * tanhf(s / a.cap);
-                        else s = a.cap * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[n][i] * (back * 2.f * LOG2E))));
-                    }
-                    const int j = key0 + n * 32 + 8 * (i / 4) + 4 * hh + i % 4;
-                    x[n][i] = s - y.slope * (float)abs(y.p - j);
-                }
+                for (int i = 0; i < 16; i++) x[n][i] = __builtin_fmaf(slope, fabsf(away - (float)(n * 32 + 8 * (i / 4) + i % 4)), x[n][i] * unit);
+            unit = 1.f;
         }
         if (masked) {
 #pragma unroll
@@ -285,7 +298,7 @@ template <typename T, int DP, bool PLAIN> struct Rows {
             return;
         }
         const float f = sum > 0.f ? 1.f / sum : 0.f;
-        if (a.lse && hh == 0) a.lse[at] = sum > 0.f ? (m_ + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        if (a.lse && hh == 0) a.lse[at] = sum > 0.f ? (m_ + a.offset + log2f(sum)) * 0.6931471805599453f : -INFINITY;
         T *dst = (T *)a.out + y.row * a.o_stride + (size_t)y.head * d;
 #pragma unroll
         for (int b = 0; b < DB; b++)
@@ -337,10 +350,10 @@ __device__ __forceinline__ bool find_item(const AttnArgs &a, int id, int rows_pe
     return true;
 }
 
-template <bool PLAIN>
+template <int MODE>
 __device__ __forceinline__ Query find_query(const AttnArgs &a, const Item &it, int r) {
     const int i = r / a.group, hg = r - i * a.group;
-    if (!a.whole) return make_query<PLAIN>(a, it.kvh, it.s, it.sq.r0 + i, i, it.sq, hg, i < it.sq.rows);
+    if (!a.whole) return make_query<MODE>(a, it.kvh, it.s, it.sq.r0 + i, i, it.sq, hg, i < it.sq.rows);
     // row i of the batch: its sequence, by halving (row_start ascends)
     int lo = 0, hi = a.pv.n_seq;                              // row_start[lo] <= i < row_start[hi], if i is a row at all
     while (hi - lo > 1) {
@@ -349,7 +362,7 @@ __device__ __forceinline__ Query find_query(const AttnArgs &a, const Item &it, i
     }
     const PagedSeq sq = paged_seq(a.pv, lo);
     const int at = i - sq.r0;
-    Query q = make_query<PLAIN>(a, it.kvh, lo, i, at, sq, hg, at >= 0 && at < sq.rows);
+    Query q = make_query<MODE>(a, it.kvh, lo, i, at, sq, hg, at >= 0 && at < sq.rows);
     if (q.valid) { q.hi = min(q.hi, a.shared_len); q.pre = min(q.pre, a.shared_len); }
     return q;
 }
@@ -357,7 +370,7 @@ __device__ __forceinline__ Query find_query(const AttnArgs &a, const Item &it, i
 __device__ __forceinline__ bool sees_all(const Query &y, int k0, int k1) { return (k1 <= y.hi && k0 >= y.lo) || k1 <= y.pre; }
 __device__ __forceinline__ bool sees_none(const Query &y, int k0, int k1) { return !y.valid || ((k0 >= y.hi || k1 <= y.lo) && k0 >= y.pre); }
 
-template <typename T, int DP, bool PLAIN>
+template <typename T, int DP, int MODE>
 __global__ void __launch_bounds__(256) paged_prompt_kernel(AttnArgs a) {
     typedef Tile<T, DP> TL;
     constexpr int NB = sizeof(T) == 2 ? 2 : 1, KT = 32 * NB, BYTES = KT * TL::ROW, GROUPS = KT / 16;
@@ -366,9 +379,9 @@ __global__ void __launch_bounds__(256) paged_prompt_kernel(AttnArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Item it;
     if (!find_item(a, blockIdx.x, 128, &it)) return;
-    const Query y = find_query<PLAIN>(a, it, it.first + wave * 32 + (threadIdx.x & 31));
+    const Query y = find_query<MODE>(a, it, it.first + wave * 32 + (threadIdx.x & 31));
     const int part = a.part0 + blockIdx.y, base = it.lo & ~(KT - 1), lo = max(it.lo, base + (int)blockIdx.y * a.chunk), hi = min(it.hi, base + ((int)blockIdx.y + 1) * a.chunk);
-    Rows<T, DP, PLAIN> rows;
+    Rows<T, DP, MODE> rows;
     rows.start(a, y);
     if (lo < hi) {
         const int32_t *table = a.pv.table + (size_t)it.s * a.pv.table_stride;
@@ -400,7 +413,7 @@ __global__ void __launch_bounds__(256) paged_prompt_kernel(AttnArgs a) {
     rows.finish(a, y, part);
 }
 
-template <typename T, int DP, int NW, bool PLAIN>
+template <typename T, int DP, int NW, int MODE>
 __global__ void __launch_bounds__(64 * NW) paged_decode_kernel(AttnArgs a) {
     typedef Tile<T, DP> TL;
     constexpr int KT = 32, BYTES = KT * TL::ROW, STAGE = 2 * BYTES, LOADS = 4 * 16 / TL::RPI;
@@ -410,9 +423,9 @@ __global__ void __launch_bounds__(64 * NW) paged_decode_kernel(AttnArgs a) {
     const unsigned ring0 = (unsigned)(size_t)(lds_void *)ring;
     Item it;
     if (!find_item(a, blockIdx.x, 32, &it)) return;
-    const Query y = find_query<PLAIN>(a, it, it.first + (lane & 31));
+    const Query y = find_query<MODE>(a, it, it.first + (lane & 31));
     const int part = a.part0 + blockIdx.y, base = it.lo & ~(KT - 1), lo = max(it.lo, base + (int)blockIdx.y * a.chunk), hi = min(it.hi, base + ((int)blockIdx.y + 1) * a.chunk);
-    Rows<T, DP, PLAIN> rows;
+    Rows<T, DP, MODE> rows;
     rows.start(a, y);
     const int t0 = lo / KT, t1 = lo < hi ? (hi + KT - 1) / KT : t0;
     if (t0 + wave < t1) {
@@ -476,35 +489,50 @@ __global__ void __launch_bounds__(64 * NW) paged_decode_kernel(AttnArgs a) {
     } else rows.finish(a, y, part);
 }
 
-// The parts of one (row, head), joined in order by one wave.
-template <typename T>
+// The parts of one (row, head), joined by one workgroup: DP / 4 lanes a part, so 1024 / DP parts at a time, whose sums are added in one order.
+// (One wave a pair and part after part: 41 us for 64 parts of 32 pairs, a memory latency each.)
+template <typename T, int DP>
 __global__ void __launch_bounds__(256) paged_join_kernel(AttnArgs a) {
+    constexpr int LANES = DP / 4, AT_ONCE = 256 / LANES;
+    __shared__ f32x4_t sums[256];
     const PagedView &pv = a.pv;
-    const int row = blockIdx.x, lane = threadIdx.x & 63, d = pv.d;
+    const int row = blockIdx.x, h = blockIdx.y, t = threadIdx.x, lane = t & 63, d = pv.d;
     const int s = paged_seq_of_row(pv, row);
     if (s >= pv.n_seq) return;
     const PagedSeq sq = paged_seq(pv, s);
     if (row - sq.r0 < 0 || row - sq.r0 >= sq.rows) return;
-    for (int h = blockIdx.y * 4 + (threadIdx.x >> 6); h < a.n_heads; h += 4 * gridDim.y) {
-        const size_t step = (size_t)pv.n_rows * a.n_heads, at = (size_t)row * a.n_heads + h;
-        float top = -INFINITY, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int z = lane; z < a.parts; z += 64) top = fmaxf(top, a.ml[z * step + at].x);
-        top = vla_wave_fold(top, VlaMax());
-        for (int z = 0; z < a.parts; z++) {
-            const float2 v = a.ml[z * step + at];
-            if (v.x == -INFINITY || !(v.y > 0.f)) continue;
-            const float f = __builtin_amdgcn_exp2f(v.x - top);
-            sum += f * v.y;
+    const size_t step = (size_t)pv.n_rows * a.n_heads, at = (size_t)row * a.n_heads + h;
+    float top = -INFINITY, sum = 0.f;
+    for (int z = lane; z < a.parts; z += 64) top = fmaxf(top, a.ml[z * step + at].x);
+    top = vla_wave_fold(top, VlaMax());
+    auto share = [&](float2 v) { return v.y > 0.f ? __builtin_amdgcn_exp2f(v.x - top) : 0.f; };
+    for (int z = lane; z < a.parts; z += 64) { const float2 v = a.ml[z * step + at]; sum += share(v) * v.y; }
+    sum = vla_wave_sum(sum);
+    const int dim = (t % LANES) * 4;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    if (dim < d)
+#pragma unroll 4
+        for (int z = t / LANES; z < a.parts; z += AT_ONCE) {
+            const float f = share(a.ml[z * step + at]);
+            if (f > 0.f) {
+                const f32x4_t v = *(const f32x4_t *)(a.o_part + (z * step + at) * d + dim);
 #pragma unroll
-            for (int e = 0; e < 4; e++)
-                if (lane + 64 * e < d) o[e] += f * a.o_part[(z * step + at) * d + lane + 64 * e];
+                for (int e = 0; e < 4; e++) o[e] += f * v[e];
+            }
         }
-        const float f = sum > 0.f ? 1.f / sum : 0.f;
+    sums[t] = o;
+    __syncthreads();
+    if (t >= LANES || dim >= d) return;
+    for (int i = 1; i < AT_ONCE; i++) {
+        const f32x4_t v = sums[i * LANES + t];
 #pragma unroll
-        for (int e = 0; e < 4; e++)
-            if (lane + 64 * e < d) ((T *)a.out)[row * a.o_stride + (size_t)h * d + lane + 64 * e] = (T)(o[e] * f);
-        if (a.lse && lane == 0) a.lse[at] = sum > 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        for (int e = 0; e < 4; e++) o[e] += v[e];
     }
+    const float f = sum > 0.f ? 1.f / sum : 0.f;
+    T *dst = (T *)a.out + row * a.o_stride + (size_t)h * d + dim;
+#pragma unroll
+    for (int e = 0; e < 4; e++) dst[e] = (T)(o[e] * f);
+    if (a.lse && t == 0) a.lse[at] = sum > 0.f ? (top + a.offset + log2f(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
 int check(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, int n_heads, AttnArgs *a) {
@@ -575,35 +603,43 @@ size_t workspace(const AttnArgs &a, const Plan &p) {
     return p.parts > 1 ? ((slots * sizeof(float2) + 255) / 256 * 256) + slots * a.pv.d * sizeof(float) : 256;
 }
 
-template <typename T, int DP, bool PLAIN>
+template <typename T, int DP, int MODE>
 int launch_form(const AttnArgs &a, const Launch &p, hipStream_t st) {
     typedef Tile<T, DP> TL;
     const dim3 grid((unsigned)p.items, p.parts);
     if (p.prompt) {
         constexpr size_t bytes = 2 * 2 * (sizeof(T) == 2 ? 64 : 32) * TL::ROW;
-        if (int rc = vla_allow_lds((const void *)paged_prompt_kernel<T, DP, PLAIN>, bytes)) return rc;
-        paged_prompt_kernel<T, DP, PLAIN><<<grid, 256, bytes, st>>>(a);
+        if (int rc = vla_allow_lds((const void *)paged_prompt_kernel<T, DP, MODE>, bytes)) return rc;
+        paged_prompt_kernel<T, DP, MODE><<<grid, 256, bytes, st>>>(a);
     } else if (p.nw == 4) {
         if constexpr (TL::ROW <= 256) {
             constexpr size_t bytes = 4 * 2 * 2 * 32 * TL::ROW;
             static_assert(bytes >= 4 * 64 * 16 * 4 + 4 * 32 * 8, "the join's panel");
-            if (int rc = vla_allow_lds((const void *)paged_decode_kernel<T, DP, 4, PLAIN>, bytes)) return rc;
-            paged_decode_kernel<T, DP, 4, PLAIN><<<grid, 256, bytes, st>>>(a);
+            if (int rc = vla_allow_lds((const void *)paged_decode_kernel<T, DP, 4, MODE>, bytes)) return rc;
+            paged_decode_kernel<T, DP, 4, MODE><<<grid, 256, bytes, st>>>(a);
         }
     } else {
         constexpr size_t bytes = 2 * 2 * 32 * TL::ROW;
-        if (int rc = vla_allow_lds((const void *)paged_decode_kernel<T, DP, 1, PLAIN>, bytes)) return rc;
-        paged_decode_kernel<T, DP, 1, PLAIN><<<grid, 64, bytes, st>>>(a);
+        if (int rc = vla_allow_lds((const void *)paged_decode_kernel<T, DP, 1, MODE>, bytes)) return rc;
+        paged_decode_kernel<T, DP, 1, MODE><<<grid, 64, bytes, st>>>(a);
     }
     return vla_check_launch("paged_attention");
 }
+template <typename T, int MODE>
+int launch_sized(const AttnArgs &a, const Launch &p, hipStream_t st) {
+    switch (padded_dim(a.pv.d)) {
+        case 64: return launch_form<T, 64, MODE>(a, p, st);
+        case 128: return launch_form<T, 128, MODE>(a, p, st);
+        default: return launch_form<T, 256, MODE>(a, p, st);
+    }
+}
 template <typename T>
 int launch_typed(const AttnArgs &a, const Launch &p, hipStream_t st) {
-    const bool plain = a.cap == 0.f && !a.slopes;
-    switch (padded_dim(a.pv.d)) {
-        case 64: return plain ? launch_form<T, 64, true>(a, p, st) : launch_form<T, 64, false>(a, p, st);
-        case 128: return plain ? launch_form<T, 128, true>(a, p, st) : launch_form<T, 128, false>(a, p, st);
-        default: return plain ? launch_form<T, 256, true>(a, p, st) : launch_form<T, 256, false>(a, p, st);
+    switch ((a.cap > 0.f ? CAPPED : 0) | (a.slopes ? BIASED : 0)) {
+        case 0: return launch_sized<T, 0>(a, p, st);
+        case CAPPED: return launch_sized<T, CAPPED>(a, p, st);
+        case BIASED: return launch_sized<T, BIASED>(a, p, st);
+        default: return launch_sized<T, CAPPED | BIASED>(a, p, st);
     }
 }
 template <typename T>
@@ -621,7 +657,12 @@ int attend(AttnArgs a, const Plan &p, void *ws, hipStream_t st) {
     a.row_tiles = p.own.row_tiles; a.chunk = p.own.chunk;
     if ((rc = launch_typed<T>(a, p.own, st))) return rc;
     if (p.parts == 1) return VLA_OK;
-    paged_join_kernel<T><<<dim3(a.pv.n_rows, (a.n_heads + 3) / 4), 256, 0, st>>>(a);
+    const dim3 grid(a.pv.n_rows, a.n_heads);
+    switch (padded_dim(a.pv.d)) {
+        case 64: paged_join_kernel<T, 64><<<grid, 256, 0, st>>>(a); break;
+        case 128: paged_join_kernel<T, 128><<<grid, 256, 0, st>>>(a); break;
+        default: paged_join_kernel<T, 256><<<grid, 256, 0, st>>>(a);
+    }
     return vla_check_launch("paged_attention join");
 }
 
@@ -654,6 +695,7 @@ int vla_paged_attention(const vla_paged_cache *cache, const vla_paged_batch *bat
     const size_t es = f32 ? 4 : 2;
     a.q = (const char *)q; a.out = (char *)out; a.lse = lse; a.q_stride = q_stride; a.o_stride = out_stride;
     a.aligned = ((uintptr_t)q | (uintptr_t)out | (size_t)q_stride * es | (size_t)out_stride * es) % 16 == 0;
+    a.offset = !f32 ? a.cap * 1.4426950408889634f : 0.f;
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps("paged_attention", 0.0, st);
     return f32 ? attend<float>(a, p, ws, st) : attend<bf16_t>(a, p, ws, st);
