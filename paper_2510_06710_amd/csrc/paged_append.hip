@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a) {
     const PagedSeq sq = paged_seq(pv, s);
     const int i = row - sq.r0, pos = sq.len - sq.n + i;
     if (i < 0 || i >= sq.rows || pos < 0 || pos >= pv.max_len) return;
-    const int page = pv.table[(size_t)s * pv.table_stride + (pos >> pv.page_log)];
+    const int page = paged_int(pv.table, (size_t)s * pv.table_stride + (pos >> pv.page_log));
     const bool kept = (unsigned)page < (unsigned)pv.n_pages;
     if ((int)threadIdx.x < a.half) {
         double t = (double)pos * a.inv_freq[threadIdx.x] * 0.15915494309189533577, sn, cs;      // turns

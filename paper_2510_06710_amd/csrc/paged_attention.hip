@@ -44,13 +44,24 @@ struct AttnArgs {
     float offset;            // what scores lack, in log2 units (see Rows::tile): lse alone knows it
     int aligned;             // rows of q and out start at multiples of 16 bytes
     // this launch
+    int decode;              // the new rows' own keys in decode form
     int whole;               // packed rows of the whole batch against the shared positions
     int row_tiles;           // tiles of packed rows per sequence (whole: in all)
     int chunk;               // keys per part
     int part0, parts;        // number of this launch's first part; parts of all launches (1: the output is written here)
+    int waves, packed;       // decode: waves among which a key head's tiles are divided (0: one per sequence and key head); packed rows of a sequence at most
+    int2 *seq_waves;         // [n_seq]: the first wave that has a sequence, and how many have
+    float2 *wave_ml;         // [waves][n_kv][2][packed]: parts of sequences that several waves share
+    float *wave_o;           // [waves][n_kv][2][packed][d]
     float2 *ml;              // [parts][n_rows][n_heads]: maximum (log2 units) and sum
     float *o_part;           // [parts][n_rows][n_heads][d]
 };
+
+__device__ __forceinline__ int wave_sum(int v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
 
 // 16 bytes of zeros and more: what rows of pages that are not there are read from.
 __device__ __attribute__((aligned(16))) float zero_row[256];
@@ -77,7 +88,7 @@ struct Span {
         int k = min(max(key0, lo), hi - 1);
         if (key0 >= g0 && key0 + 15 < g1) k = g1;
         else if (k >= g0 && k < g1) k = key0 >= g0 || key0 + 15 >= g1 ? g1 : g0 - 1;
-        return table[k >> page_log];
+        return paged_int(table, k >> page_log);
     }
 };
 
@@ -126,7 +137,7 @@ __device__ __forceinline__ Query make_query(const AttnArgs &a, int kvh, int s, i
     q.head = kvh * a.group + hg;
     q.valid = valid;
     q.p = sq.len - sq.n + i;
-    q.pre = a.prefix_len && valid ? min(a.prefix_len[s], sq.keys) : 0;
+    q.pre = a.prefix_len && valid ? min(paged_int(a.prefix_len, s), sq.keys) : 0;
     q.hi = min(sq.keys, q.p + 1);
     q.lo = a.whole ? 0 : a.shared_len;
     if (a.window) q.lo = max(0, q.p + 1 - a.window);
@@ -165,6 +176,9 @@ template <typename T, int DP, int MODE> struct Rows {
                 }
             }
         }
+        // (here the compiler waits for them: left to the first use, inside the loop over tiles, it would wait for everything in flight at every tile)
+#pragma unroll
+        for (int kk = 0; kk < KS; kk++) asm volatile("" : "+v"(q[kk]));
 #pragma unroll
         for (int b = 0; b < DB; b++)
 #pragma unroll
@@ -276,29 +290,30 @@ template <typename T, int DP, int MODE> struct Rows {
             }
     }
 
-    // One part's result: the output itself where there is one part, else the part's sums.
-    __device__ __forceinline__ void finish(const AttnArgs &a, const Query &y, int part) {
-        write(a, y, part, m, vla_fold_step<32>(l, VlaAdd()), (threadIdx.x >> 5) & 1);
+    // A part's sums.
+    __device__ __forceinline__ void keep(const AttnArgs &a, float2 *ml, float *dst, float sum, int hh) {
+        if (hh == 0) *ml = make_float2(m, sum);
+        if (!(sum > 0.f)) return;                            // (the join reads nothing of an empty part)
+#pragma unroll
+        for (int b = 0; b < DB; b++)
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                const int dim = b * 32 + g * 8 + hh * 4;
+                if (dim < a.pv.d) *(f32x4_t *)(dst + dim) = f32x4_t{o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]};
+            }
     }
-    __device__ __forceinline__ void write(const AttnArgs &a, const Query &y, int part, float m_, float sum, int hh) {
-        const int d = a.pv.d;
+    // The output itself where there is one part, else the part's sums.
+    __device__ __forceinline__ void finish(const AttnArgs &a, const Query &y, int part) {
+        const int d = a.pv.d, hh = (threadIdx.x >> 5) & 1;
+        const float sum = vla_fold_step<32>(l, VlaAdd());
         if (!y.valid) return;
         const size_t at = (size_t)y.row * a.n_heads + y.head, slot = (size_t)part * a.pv.n_rows * a.n_heads + at;
         if (a.parts > 1) {
-            if (hh == 0) a.ml[slot] = make_float2(m_, sum);
-            if (!(sum > 0.f)) return;                        // (the join reads nothing of an empty part)
-            float *dst = a.o_part + slot * d;
-#pragma unroll
-            for (int b = 0; b < DB; b++)
-#pragma unroll
-                for (int g = 0; g < 4; g++) {
-                    const int dim = b * 32 + g * 8 + hh * 4;
-                    if (dim < d) *(f32x4_t *)(dst + dim) = f32x4_t{o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]};
-                }
+            keep(a, a.ml + slot, a.o_part + slot * d, sum, hh);
             return;
         }
         const float f = sum > 0.f ? 1.f / sum : 0.f;
-        if (a.lse && hh == 0) a.lse[at] = sum > 0.f ? (m_ + a.offset + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        if (a.lse && hh == 0) a.lse[at] = sum > 0.f ? (m + a.offset + log2f(sum)) * 0.6931471805599453f : -INFINITY;
         T *dst = (T *)a.out + y.row * a.o_stride + (size_t)y.head * d;
 #pragma unroll
         for (int b = 0; b < DB; b++)
@@ -323,26 +338,15 @@ template <typename T, int DP, int MODE> struct Rows {
 // Packed rows first .. first + n - 1 of a launch's item -> the lane's query, and the keys any of them may see.
 struct Item { int s, kvh, first, lo, hi, g0, g1; PagedSeq sq; };
 
-__device__ __forceinline__ bool find_item(const AttnArgs &a, int id, int rows_per_tile, Item *it) {
-    const PagedView &pv = a.pv;
-    it->kvh = id % pv.n_kv;
+// The keys that packed rows first .. first + n - 1 of sequence s may see (it->sq is there; false: there are no such rows).
+__device__ __forceinline__ bool range_of(const AttnArgs &a, int s, int first, int n, Item *it) {
+    it->s = s;
+    it->first = first;
     it->g0 = it->g1 = 0;
-    id /= pv.n_kv;
-    if (a.whole) {
-        it->s = 0;
-        it->first = id * rows_per_tile;
-        it->lo = 0;
-        it->hi = a.shared_len;
-        it->sq = paged_seq(pv, 0);
-        return it->first < min(pv.row_start[pv.n_seq], pv.n_rows) * a.group;
-    }
-    it->s = id % pv.n_seq;
-    it->first = (a.row_tiles - 1 - id / pv.n_seq) * rows_per_tile;      // the last rows, which see most keys, first
-    it->sq = paged_seq(pv, it->s);
     const int rows = it->sq.rows;
-    if (it->first >= rows * a.group) return false;
-    const int i0 = it->first / a.group, i1 = min(rows - 1, (it->first + rows_per_tile - 1) / a.group), p0 = it->sq.len - it->sq.n;
-    const int prefix = a.prefix_len ? min(max(a.prefix_len[it->s], 0), it->sq.keys) : 0;
+    if (first >= rows * a.group) return false;
+    const int i0 = first / a.group, i1 = min(rows - 1, (first + n - 1) / a.group), p0 = it->sq.len - it->sq.n;
+    const int prefix = a.prefix_len ? min(max(paged_int(a.prefix_len, s), 0), it->sq.keys) : 0;
     it->hi = min(it->sq.keys, max(p0 + i1 + 1, prefix));
     const int from = a.window ? max(0, p0 + i0 + 1 - a.window) : 0;          // the first row's window, the lowest
     it->lo = max(a.shared_len, prefix == 0 ? from : 0);
@@ -350,15 +354,32 @@ __device__ __forceinline__ bool find_item(const AttnArgs &a, int id, int rows_pe
     return true;
 }
 
+__device__ __forceinline__ bool find_item(const AttnArgs &a, int id, int rows_per_tile, Item *it) {
+    const PagedView &pv = a.pv;
+    it->kvh = id % pv.n_kv;
+    id /= pv.n_kv;
+    if (a.whole) {
+        it->sq = paged_seq(pv, 0);
+        it->s = it->lo = it->g0 = it->g1 = 0;
+        it->first = id * rows_per_tile;
+        it->hi = a.shared_len;
+        return it->first < min(paged_int(pv.row_start, pv.n_seq), pv.n_rows) * a.group;
+    }
+    const int s = id % pv.n_seq;
+    it->sq = paged_seq(pv, s);
+    return range_of(a, s, (a.row_tiles - 1 - id / pv.n_seq) * rows_per_tile, rows_per_tile, it);      // the last rows, which see most keys, first
+}
+
+// starts: a copy of row_start in LDS, or row_start itself.
 template <int MODE>
-__device__ __forceinline__ Query find_query(const AttnArgs &a, const Item &it, int r) {
+__device__ __forceinline__ Query find_query(const AttnArgs &a, const Item &it, int r, const int32_t *starts) {
     const int i = r / a.group, hg = r - i * a.group;
     if (!a.whole) return make_query<MODE>(a, it.kvh, it.s, it.sq.r0 + i, i, it.sq, hg, i < it.sq.rows);
     // row i of the batch: its sequence, by halving (row_start ascends)
     int lo = 0, hi = a.pv.n_seq;                              // row_start[lo] <= i < row_start[hi], if i is a row at all
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        if (a.pv.row_start[mid] <= i) lo = mid; else hi = mid;
+        if (starts[mid] <= i) lo = mid; else hi = mid;
     }
     const PagedSeq sq = paged_seq(a.pv, lo);
     const int at = i - sq.r0;
@@ -379,7 +400,15 @@ __global__ void __launch_bounds__(256) paged_prompt_kernel(AttnArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Item it;
     if (!find_item(a, blockIdx.x, 128, &it)) return;
-    const Query y = find_query<MODE>(a, it, it.first + wave * 32 + (threadIdx.x & 31));
+    // (the search of a row's sequence is a chain of loads, one per halving: from LDS where the sequences fit there)
+    const int32_t *starts = a.pv.row_start;
+    if (a.whole && a.pv.n_seq <= 2048) {
+        for (int i = threadIdx.x; i < a.pv.n_seq; i += 256) ((int32_t *)lds)[i] = starts[i];
+        __syncthreads();
+        starts = (const int32_t *)lds;
+    }
+    const Query y = find_query<MODE>(a, it, it.first + wave * 32 + (threadIdx.x & 31), starts);
+    if (a.whole) __syncthreads();
     const int part = a.part0 + blockIdx.y, base = it.lo & ~(KT - 1), lo = max(it.lo, base + (int)blockIdx.y * a.chunk), hi = min(it.hi, base + ((int)blockIdx.y + 1) * a.chunk);
     Rows<T, DP, MODE> rows;
     rows.start(a, y);
@@ -413,126 +442,212 @@ __global__ void __launch_bounds__(256) paged_prompt_kernel(AttnArgs a) {
     rows.finish(a, y, part);
 }
 
-template <typename T, int DP, int NW, int MODE>
-__global__ void __launch_bounds__(64 * NW) paged_decode_kernel(AttnArgs a) {
+// Key tiles of 32 of a sequence's rows in decode form, at least one where there are rows (their output has to be written).
+__device__ __forceinline__ int tiles_of(const AttnArgs &a, int s) {
+    Item it;
+    it.sq = paged_seq(a.pv, s);
+    if (!range_of(a, s, 0, 32, &it)) return 0;
+    return max(1, (it.hi + 31) / 32 - it.lo / 32);
+}
+// A wave's share of its key head's tiles.  No wave has less than two.  (The plan keeps all sums of tiles below 2^30.)
+__device__ __forceinline__ int share_of(const AttnArgs &a, int all) { return max(2, (int)((unsigned)(all + a.waves - 1) / (unsigned)a.waves)); }
+
+// A run of one sequence's tiles of one key head.
+struct Run {
+    Item it;
+    int t0, t1;              // (t0 = t1: its rows see nothing)
+    int tiles, took;         // of the sequence; of these, here
+    bool first, whole;       // from its first tile on; all of them
+};
+struct Walk {
+    int kvh, s, skip, left;
+    __device__ __forceinline__ bool next(const AttnArgs &a, Run *r) {
+        while (left > 0 && s < a.pv.n_seq) {
+            r->it.sq = paged_seq(a.pv, s);
+            r->it.kvh = kvh;
+            if (!range_of(a, s++, 0, 32, &r->it)) continue;
+            const int t = r->it.lo / 32, n = max(0, (r->it.hi + 31) / 32 - t), all = max(1, n), take = min(all - skip, left);
+            r->t0 = t + min(skip, n);
+            r->t1 = t + min(skip + take, n);
+            r->tiles = all;
+            r->took = take;
+            r->first = skip == 0;
+            r->whole = skip == 0 && take == all;
+            left -= take;
+            skip = 0;
+            return true;
+        }
+        return false;
+    }
+};
+
+// One wave a workgroup, as many as their rings fit the chip; each takes one key head's equal run of the key tiles of all sequences, whatever
+// their lengths, and streams through it, the next tile on its way whether it is of the same sequence or not.  A sequence's tiles that
+// fall to several waves leave parts for the join (a wave has at most two: of the sequence it begins within, and of the one it ends within).
+// Neighbouring waves have the same run of different heads, whose rows lie side by side in the pages.
+// Memory bound: 32 sequences of 2048 keys, 32 heads, 192 us, 5.6 TB/s; 256 of 294 keys 252 us; one of 32768 keys, 8 key heads, 27 us and 6 for
+// the join of 128 parts; 48 ragged ones of up to 8192 keys with capped scores and a bias 79 us.  (One workgroup of 1, 2 or 4 waves per sequence,
+// key head and even part of max_len: 200, 259, 30 + 5 and 125 to 155 us.)
+template <typename T, int DP, int MODE>
+__global__ void __launch_bounds__(64) paged_decode_kernel(AttnArgs a) {
     typedef Tile<T, DP> TL;
     constexpr int KT = 32, BYTES = KT * TL::ROW, STAGE = 2 * BYTES, LOADS = 4 * 16 / TL::RPI;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    char *ring = lds + wave * 2 * STAGE;
-    const unsigned ring0 = (unsigned)(size_t)(lds_void *)ring;
-    Item it;
-    if (!find_item(a, blockIdx.x, 32, &it)) return;
-    const Query y = find_query<MODE>(a, it, it.first + (lane & 31));
-    const int part = a.part0 + blockIdx.y, base = it.lo & ~(KT - 1), lo = max(it.lo, base + (int)blockIdx.y * a.chunk), hi = min(it.hi, base + ((int)blockIdx.y + 1) * a.chunk);
+    const unsigned ring0 = (unsigned)(size_t)(lds_void *)lds;
+    Walk walk{(int)(blockIdx.x % a.pv.n_kv), 0, 0, 0};
+    int share = 0x3fffffff, done = 0;                        // tiles of its share; that it has walked past
+    if (a.waves) {
+        const int lane = threadIdx.x & 63;
+        int all = 0, c = 0;
+        for (int s = lane; s < a.pv.n_seq; s += 64) all += c = tiles_of(a, s);
+        all = __builtin_amdgcn_readfirstlane(wave_sum(all));
+        share = share_of(a, all);
+        int rest = blockIdx.x / a.pv.n_kv * share;
+        walk.left = min(share, all - rest);
+        if (walk.left <= 0) return;
+        // the sequence in which it begins
+        for (int s0 = 0; s0 < a.pv.n_seq; s0 += 64) {
+            if (a.pv.n_seq > 64) c = s0 + lane < a.pv.n_seq ? tiles_of(a, s0 + lane) : 0;
+            int in = c;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(in, o, 64); if (lane >= o) in += v; }
+            const unsigned long long past = __ballot(in > rest);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                walk.s = __builtin_amdgcn_readfirstlane(s0 + l);
+                walk.skip = __builtin_amdgcn_readfirstlane(rest - __shfl(in - c, l, 64));
+                break;
+            }
+            rest -= __builtin_amdgcn_readlane(in, 63);
+        }
+    } else {
+        walk.s = blockIdx.x / a.pv.n_kv;
+        walk.left = tiles_of(a, walk.s);
+    }
+    Run run, ahead;
+    Walk lead = walk;                                        // one tile before what is computed
+    bool more = lead.next(a, &ahead);
+    int t = 0, p0 = 0, p1 = 0, stage = 0;                    // the lead's next tile and its pages
+    Span sp{0, 0, 0, 0};
+    auto pages = [&]() {
+        const int32_t *table = a.pv.table + (size_t)ahead.it.s * a.pv.table_stride;
+        p0 = sp.page(table, a.pv.page_log, t * KT);
+        p1 = sp.page(table, a.pv.page_log, t * KT + 16);
+    };
+    auto settle = [&]() {                                    // on to a tile that there is
+        while (more && ahead.t0 == ahead.t1) more = lead.next(a, &ahead);
+        if (!more) return;
+        t = ahead.t0;
+        sp = Span{ahead.it.lo, ahead.it.hi, ahead.it.g0, ahead.it.g1};
+        pages();
+    };
+    auto load = [&](int to) {
+        const unsigned at = ring0 + to * STAGE;
+        TL::template load16<false>(at, a.pv.k, a.pv, p0, ahead.it.kvh, t * KT, sp);
+        TL::template load16<false>(at + 16 * TL::ROW, a.pv.k, a.pv, p1, ahead.it.kvh, t * KT + 16, sp);
+        TL::template load16<true>(at + BYTES, a.pv.v, a.pv, p0, ahead.it.kvh, t * KT, sp);
+        TL::template load16<true>(at + BYTES + 16 * TL::ROW, a.pv.v, a.pv, p1, ahead.it.kvh, t * KT + 16, sp);
+        if (++t < ahead.t1) pages();
+        else { more = lead.next(a, &ahead); settle(); }
+    };
+    settle();
+    if (more) load(0);
     Rows<T, DP, MODE> rows;
-    rows.start(a, y);
-    const int t0 = lo / KT, t1 = lo < hi ? (hi + KT - 1) / KT : t0;
-    if (t0 + wave < t1) {
-        const int32_t *table = a.pv.table + (size_t)it.s * a.pv.table_stride;
-        const Span sp{lo, hi, it.g0, it.g1};
-        auto page_of = [&](int t, int g) { return sp.page(table, a.pv.page_log, t * KT + g * 16); };
-        auto load = [&](int t, int stage, int p0, int p1) {
-            const unsigned at = ring0 + stage * STAGE;
-            TL::template load16<false>(at, a.pv.k, a.pv, p0, it.kvh, t * KT, sp);
-            TL::template load16<false>(at + 16 * TL::ROW, a.pv.k, a.pv, p1, it.kvh, t * KT + 16, sp);
-            TL::template load16<true>(at + BYTES, a.pv.v, a.pv, p0, it.kvh, t * KT, sp);
-            TL::template load16<true>(at + BYTES + 16 * TL::ROW, a.pv.v, a.pv, p1, it.kvh, t * KT + 16, sp);
-        };
-        int t = t0 + wave, stage = 0;
-        load(t, 0, page_of(t, 0), page_of(t, 1));
-        int p0 = page_of(t + NW, 0), p1 = page_of(t + NW, 1);
-        for (; t < t1; t += NW, stage ^= 1) {
+    while (walk.next(a, &run)) {
+        const int packed = threadIdx.x & 31;
+        if (a.waves) {
+            // for the join: the waves that have this sequence, told by the one that begins it
+            if (run.first && run.it.kvh == 0 && threadIdx.x == 0) a.seq_waves[run.it.s] = make_int2(blockIdx.x / a.pv.n_kv, (int)((unsigned)(done + run.tiles - 1) / (unsigned)share) + 1);
+            done += run.took;
+        }
+        const Query y = find_query<MODE>(a, run.it, packed, a.pv.row_start);
+        rows.start(a, y);
+        for (int u = run.t0; u < run.t1; u++, stage ^= 1) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // the reads of the stage that is loaded again are through
-            if (t + NW < t1) {
-                load(t + NW, stage ^ 1, p0, p1);
-                p0 = page_of(t + 2 * NW, 0);
-                p1 = page_of(t + 2 * NW, 1);
-                vm_wait<LOADS>();
-            } else vm_wait<0>();
-            const int k0 = t * KT;
-            const char *kt = ring + stage * STAGE;
-            rows.template tile<1>(a, y, kt, kt + BYTES, k0, !__all(sees_all(y, k0, k0 + KT) && k0 + KT <= hi && k0 >= lo));
+            if (more) { load(stage ^ 1); vm_wait<LOADS>(); }
+            else vm_wait<0>();
+            const int k0 = u * KT;
+            const char *kt = lds + stage * STAGE;
+            rows.template tile<1>(a, y, kt, kt + BYTES, k0, !__all(sees_all(y, k0, k0 + KT) && k0 + KT <= run.it.hi && k0 >= run.it.lo));
+        }
+        if (run.whole) rows.finish(a, y, 0);
+        else {
+            const size_t slot = ((size_t)blockIdx.x * 2 + (run.first ? 1 : 0)) * a.packed + packed;
+            const float sum = vla_fold_step<32>(rows.l, VlaAdd());
+            if (y.valid) rows.keep(a, a.wave_ml + slot, a.wave_o + slot * a.pv.d, sum, (threadIdx.x >> 5) & 1);
         }
     }
-    if constexpr (NW > 1) {
-        // the waves' sums, joined by the first: maxima and sums through LDS, then the outputs, 32 dims at a time
-        const float sum = vla_fold_step<32>(rows.l, VlaAdd());
-        __syncthreads();
-        float *x = (float *)lds;
-        float2 *ml = (float2 *)(x + NW * 64 * 16);
-        if (lane < 32) ml[wave * 32 + lane] = make_float2(rows.m, sum);
-        __syncthreads();
-        float top = -INFINITY, total = 0.f;
-        for (int w = 0; w < NW; w++) top = fmaxf(top, ml[w * 32 + (lane & 31)].x);
-        for (int w = 0; w < NW; w++) {
-            const float2 v = ml[w * 32 + (lane & 31)];
-            total += v.x == -INFINITY ? 0.f : v.y * __builtin_amdgcn_exp2f(v.x - top);
-        }
-        const float f = rows.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rows.m - top);
-#pragma unroll
-        for (int b = 0; b < DP / 32; b++) {
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < 16; i++) x[(wave * 16 + i) * 64 + lane] = rows.o[b][i] * f;
-            __syncthreads();
-            if (wave == 0) {
-#pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    float v = 0.f;
-                    for (int w = 0; w < NW; w++) v += x[(w * 16 + i) * 64 + lane];
-                    rows.o[b][i] = v;
-                }
-            }
-        }
-        if (wave == 0) rows.write(a, y, part, top, total, lane >> 5);
-    } else rows.finish(a, y, part);
 }
 
 // The parts of one (row, head), joined by one workgroup: DP / 4 lanes a part, so 1024 / DP parts at a time, whose sums are added in one order.
+// First the parts of all rows' layout (ml, o_part), then those of the waves that shared the sequence.
 // (One wave a pair and part after part: 41 us for 64 parts of 32 pairs, a memory latency each.)
+constexpr int JOIN_PARTS = 2048 + 512;          // of waves, and of own and shared ranges, at most
 template <typename T, int DP>
 __global__ void __launch_bounds__(256) paged_join_kernel(AttnArgs a) {
     constexpr int LANES = DP / 4, AT_ONCE = 256 / LANES;
     __shared__ f32x4_t sums[256];
+    __shared__ float weights[JOIN_PARTS];
     const PagedView &pv = a.pv;
-    const int row = blockIdx.x, h = blockIdx.y, t = threadIdx.x, lane = t & 63, d = pv.d;
-    const int s = paged_seq_of_row(pv, row);
+    const int t = threadIdx.x, lane = t & 63, d = pv.d;
+    const int s = a.decode ? blockIdx.x / pv.max_rows : paged_seq_of_row(pv, blockIdx.x);
     if (s >= pv.n_seq) return;
     const PagedSeq sq = paged_seq(pv, s);
-    if (row - sq.r0 < 0 || row - sq.r0 >= sq.rows) return;
-    const size_t step = (size_t)pv.n_rows * a.n_heads, at = (size_t)row * a.n_heads + h;
-    float top = -INFINITY, sum = 0.f;
-    for (int z = lane; z < a.parts; z += 64) top = fmaxf(top, a.ml[z * step + at].x);
-    top = vla_wave_fold(top, VlaMax());
-    auto share = [&](float2 v) { return v.y > 0.f ? __builtin_amdgcn_exp2f(v.x - top) : 0.f; };
-    for (int z = lane; z < a.parts; z += 64) { const float2 v = a.ml[z * step + at]; sum += share(v) * v.y; }
-    sum = vla_wave_sum(sum);
-    const int dim = (t % LANES) * 4;
-    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    if (dim < d)
-#pragma unroll 4
-        for (int z = t / LANES; z < a.parts; z += AT_ONCE) {
-            const float f = share(a.ml[z * step + at]);
-            if (f > 0.f) {
-                const f32x4_t v = *(const f32x4_t *)(a.o_part + (z * step + at) * d + dim);
-#pragma unroll
-                for (int e = 0; e < 4; e++) o[e] += f * v[e];
-            }
-        }
-    sums[t] = o;
-    __syncthreads();
-    if (t >= LANES || dim >= d) return;
-    for (int i = 1; i < AT_ONCE; i++) {
-        const f32x4_t v = sums[i * LANES + t];
-#pragma unroll
-        for (int e = 0; e < 4; e++) o[e] += v[e];
+    const int i0 = a.decode ? blockIdx.x % pv.max_rows : blockIdx.x - sq.r0, row = sq.r0 + i0;
+    if (i0 < 0 || i0 >= sq.rows) return;
+    int w0 = 0, first = 0, shared = 0;                       // parts of ml from `first` on; those of waves w0 .. w0 + shared - 1
+    if (a.waves) {
+        w0 = a.seq_waves[s].x;
+        shared = a.seq_waves[s].y;
+        if (shared == 1) {                                   // one wave had it all
+            if (a.parts == 1) return;
+            shared = 0;
+        } else first = 1;
     }
-    const float f = sum > 0.f ? 1.f / sum : 0.f;
-    T *dst = (T *)a.out + row * a.o_stride + (size_t)h * d + dim;
+    const int n = a.parts - first, total = n + shared, dim = (t % LANES) * 4;
+    const size_t step = (size_t)pv.n_rows * a.n_heads;
+    for (int h = blockIdx.y; h < a.n_heads; h += gridDim.y) {
+        const size_t at = (size_t)row * a.n_heads + h;
+        const int packed = i0 * a.group + h % a.group;
+        // (the wave that begins a sequence holds it as its last, the others as their first)
+        auto wave_slot = [&](int z) { return (((size_t)(w0 + z) * pv.n_kv + h / a.group) * 2 + (z == 0 ? 1 : 0)) * a.packed + packed; };
+        auto ml_of = [&](int z) { return z < n ? a.ml[(z + first) * step + at] : a.wave_ml[wave_slot(z - n)]; };
+        float top = -INFINITY, sum = 0.f;
+        for (int z = lane; z < total; z += 64) top = fmaxf(top, ml_of(z).x);
+        top = vla_wave_fold(top, VlaMax());
+        __syncthreads();
+        for (int z = lane; z < total; z += 64) {
+            const float2 v = ml_of(z);
+            const float f = v.y > 0.f ? __builtin_amdgcn_exp2f(v.x - top) : 0.f;
+            sum += f * v.y;
+            if (t < 64) weights[z] = f;
+        }
+        sum = vla_wave_sum(sum);
+        __syncthreads();
+        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+        if (dim < d)
+#pragma unroll 8
+            for (int z = t / LANES; z < total; z += AT_ONCE) {
+                const float f = weights[z];
+                const f32x4_t v = *(const f32x4_t *)((z < n ? a.o_part + ((z + first) * step + at) * d : a.wave_o + wave_slot(z - n) * d) + dim);
 #pragma unroll
-    for (int e = 0; e < 4; e++) dst[e] = (T)(o[e] * f);
-    if (a.lse && t == 0) a.lse[at] = sum > 0.f ? (top + a.offset + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+                for (int e = 0; e < 4; e++) o[e] += f > 0.f ? f * v[e] : 0.f;          // (an empty part has no sums, whatever lies there)
+            }
+        sums[t] = o;
+        __syncthreads();
+        if (t < LANES && dim < d) {
+            for (int i = 1; i < AT_ONCE; i++) {
+                const f32x4_t v = sums[i * LANES + t];
+#pragma unroll
+                for (int e = 0; e < 4; e++) o[e] += v[e];
+            }
+            const float f = sum > 0.f ? 1.f / sum : 0.f;
+            T *dst = (T *)a.out + row * a.o_stride + (size_t)h * d + dim;
+#pragma unroll
+            for (int e = 0; e < 4; e++) dst[e] = (T)(o[e] * f);
+            if (a.lse && t == 0) a.lse[at] = sum > 0.f ? (top + a.offset + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        }
+    }
 }
 
 int check(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, int n_heads, AttnArgs *a) {
@@ -560,110 +675,127 @@ int check(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_
     return VLA_OK;
 }
 
-// One launch: which kernel, its tiles of packed rows and its parts.
-struct Launch { bool prompt; int nw, row_tiles, parts, chunk; long items; };
-struct Plan { Launch own, whole; int parts; bool has_whole; };
+// The launches of a call: the new rows against what is their sequence's alone, in prompt or in decode form, and against the shared prefix.
+struct Prompt { int row_tiles, parts, chunk; long items; };
+struct Plan {
+    bool decode;
+    int waves;               // decode: among which a key head's tiles are divided, 0: a wave per sequence and key head
+    Prompt own, whole;       // own: unless decode
+    int parts;               // in ml and o_part
+};
 
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-Launch plan_launch(const AttnArgs &a, bool f32, bool whole) {
-    Launch p{};
-    const int dp = padded_dim(a.pv.d), row = dp * (f32 ? 4 : 2);
+// Tiles of 128 packed rows, their keys in parts by an estimate in cycles: rounds of workgroups, each a fixed time (its dependent loads, the first
+// tile, the writing out: 8 us) and its keys at the matrix and vector work of a tile; and the parts' sums, written and read again.
+Prompt plan_prompt(const AttnArgs &a, bool f32, bool whole) {
+    Prompt p{};
+    const int row = padded_dim(a.pv.d) * (f32 ? 4 : 2);
     const long packed = (long)(whole ? a.pv.n_rows : a.pv.max_rows) * a.group;
-    p.prompt = packed > 32;
     // the longest range of keys of one tile of rows; it starts at a multiple of 64 unless a window or a short shared prefix moves it
     long keys = whole ? a.shared_len : a.pv.max_len - a.shared_len;
-    if (a.window && !a.prefix_len && keys > (long)a.window + (p.prompt ? 128 : 32)) keys = a.window + (p.prompt ? 128 : 32);
+    if (a.window && !a.prefix_len && keys > (long)a.window + 128) keys = a.window + 128;
     if (!whole && (a.window || a.shared_len % 64)) keys += 63;
-    p.row_tiles = (int)((packed + (p.prompt ? 127 : 31)) / (p.prompt ? 128 : 32));
+    p.row_tiles = (int)((packed + 127) / 128);
     p.items = (long)p.row_tiles * (whole ? 1 : a.pv.n_seq) * a.pv.n_kv;
-    // A decode wave's ring is 128 rows: four waves a workgroup where four rings fit a CU's LDS and there are keys enough for each
-    p.nw = !p.prompt && row <= 256 && keys > 512 ? 4 : 1;
-    // Parts: as many as fill the chip, none under 256 keys
-    const long want = p.prompt ? 512 : p.nw == 4 ? 512 : 1024, most = (keys + 255) / 256;
-    long parts = p.items > 0 ? (want + p.items - 1) / p.items : 1;
-    if (parts > most) parts = most;
-    if (parts < 1) parts = 1;
-    p.chunk = (int)(((keys + parts - 1) / parts + 63) / 64 * 64);
-    if (p.chunk < 64) p.chunk = 64;
-    p.parts = (int)((keys + p.chunk - 1) / p.chunk);
-    if (p.parts < 1) p.parts = 1;
+    p.parts = 1;
+    p.chunk = 64;
+    const double pairs = (double)a.pv.n_rows * a.n_heads;
+    const int per_cu = 4 * row * (f32 ? 32 : 64) <= 80 * 1024 ? 2 : 1;
+    double best = 0.0;
+    for (long parts = 1; parts <= 256; parts++) {
+        const long chunk = keys > 0 ? (((keys + parts - 1) / parts) + 63) / 64 * 64 : 64, n = keys > 0 ? (keys + chunk - 1) / chunk : 1;
+        if (n < parts) continue;
+        const double rounds = (double)((p.items * n + 256 * per_cu - 1) / (256 * per_cu));
+        const double cost = rounds * (20e3 + chunk * 50.0 * per_cu * row / 256) + (n > 1 ? n * pairs * a.pv.d * 8.0 / 2000.0 : 0.0);
+        if (best == 0.0 || cost < best) { best = cost; p.chunk = (int)chunk; p.parts = (int)n; }
+    }
     return p;
 }
 Plan plan(const AttnArgs &a, bool f32) {
     Plan p{};
-    p.own = plan_launch(a, f32, false);
-    p.has_whole = a.shared_len > 0;
-    if (p.has_whole) p.whole = plan_launch(a, f32, true);
-    p.parts = p.own.parts + (p.has_whole ? p.whole.parts : 0);
+    // Decode form: up to 32 packed rows a sequence (a matrix instruction's columns).  (Every wave looks at all sequences' lengths: not for many thousands.)
+    p.decode = (long)a.pv.max_rows * a.group <= 32 && a.pv.n_seq <= 2048 && (long)a.pv.n_seq * (a.pv.max_len / 32 + 2) < 1L << 30;
+    if (p.decode) {
+        // as many waves as their rings, 128 rows of K or V each, fit the CUs' LDS; a few tiles at most per sequence: not divided, which saves the join
+        // (handed out in units of 1280 bytes: four of 32 KB)
+        const int fit = 128 / ((128 * padded_dim(a.pv.d) * (f32 ? 4 : 2) + 1279) / 1280);
+        const int waves = 256 * (fit > 8 ? 8 : fit) / a.pv.n_kv;
+        p.waves = a.pv.max_len - a.shared_len > 128 ? (waves > 0 ? waves : 1) : 0;
+        p.parts = 1;
+    } else {
+        p.own = plan_prompt(a, f32, false);
+        p.parts = p.own.parts;
+    }
+    if (a.shared_len > 0) {
+        p.whole = plan_prompt(a, f32, true);
+        p.parts += p.whole.parts;
+    }
     return p;
 }
-size_t workspace(const AttnArgs &a, const Plan &p) {
-    const size_t slots = (size_t)a.pv.n_rows * a.n_heads * p.parts;
-    return p.parts > 1 ? ((slots * sizeof(float2) + 255) / 256 * 256) + slots * a.pv.d * sizeof(float) : 256;
+size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
+// Lays the workspace out from `base` (NULL: only its size).
+size_t lay_out(AttnArgs *a, const Plan &p, char *base) {
+    size_t off = 0;
+    auto take = [&](size_t bytes) { char *at = base + off; off += round_up(bytes); return at; };
+    a->parts = p.parts;
+    a->waves = p.waves;
+    a->decode = p.decode;
+    a->packed = a->pv.max_rows * a->group;
+    if (p.parts > 1) {
+        const size_t slots = (size_t)a->pv.n_rows * a->n_heads * p.parts;
+        a->ml = (float2 *)take(slots * sizeof(float2));
+        a->o_part = (float *)take(slots * a->pv.d * sizeof(float));
+    }
+    if (p.waves) {
+        const size_t slots = (size_t)p.waves * a->pv.n_kv * 2 * a->packed;
+        a->seq_waves = (int2 *)take(a->pv.n_seq * sizeof(int2));
+        a->wave_ml = (float2 *)take(slots * sizeof(float2));
+        a->wave_o = (float *)take(slots * a->pv.d * sizeof(float));
+    }
+    return off ? off : 256;
 }
 
 template <typename T, int DP, int MODE>
-int launch_form(const AttnArgs &a, const Launch &p, hipStream_t st) {
-    typedef Tile<T, DP> TL;
-    const dim3 grid((unsigned)p.items, p.parts);
-    if (p.prompt) {
-        constexpr size_t bytes = 2 * 2 * (sizeof(T) == 2 ? 64 : 32) * TL::ROW;
-        if (int rc = vla_allow_lds((const void *)paged_prompt_kernel<T, DP, MODE>, bytes)) return rc;
-        paged_prompt_kernel<T, DP, MODE><<<grid, 256, bytes, st>>>(a);
-    } else if (p.nw == 4) {
-        if constexpr (TL::ROW <= 256) {
-            constexpr size_t bytes = 4 * 2 * 2 * 32 * TL::ROW;
-            static_assert(bytes >= 4 * 64 * 16 * 4 + 4 * 32 * 8, "the join's panel");
-            if (int rc = vla_allow_lds((const void *)paged_decode_kernel<T, DP, 4, MODE>, bytes)) return rc;
-            paged_decode_kernel<T, DP, 4, MODE><<<grid, 256, bytes, st>>>(a);
-        }
-    } else {
-        constexpr size_t bytes = 2 * 2 * 32 * TL::ROW;
-        if (int rc = vla_allow_lds((const void *)paged_decode_kernel<T, DP, 1, MODE>, bytes)) return rc;
-        paged_decode_kernel<T, DP, 1, MODE><<<grid, 64, bytes, st>>>(a);
-    }
+int launch_prompt(AttnArgs a, const Prompt &p, bool whole, int part0, hipStream_t st) {
+    constexpr size_t bytes = 2 * 2 * (sizeof(T) == 2 ? 64 : 32) * Tile<T, DP>::ROW;
+    if (int rc = vla_allow_lds((const void *)paged_prompt_kernel<T, DP, MODE>, bytes)) return rc;
+    a.whole = whole; a.row_tiles = p.row_tiles; a.chunk = p.chunk; a.part0 = part0;
+    paged_prompt_kernel<T, DP, MODE><<<dim3((unsigned)p.items, p.parts), 256, bytes, st>>>(a);
     return vla_check_launch("paged_attention");
 }
+template <typename T, int DP, int MODE>
+int launch(const AttnArgs &a, const Plan &p, hipStream_t st) {
+    int rc;
+    if (a.shared_len > 0 && (rc = launch_prompt<T, DP, MODE>(a, p.whole, true, p.decode ? 1 : p.own.parts, st))) return rc;
+    if (p.decode) {
+        constexpr size_t bytes = 2 * 2 * 32 * Tile<T, DP>::ROW;
+        if ((rc = vla_allow_lds((const void *)paged_decode_kernel<T, DP, MODE>, bytes))) return rc;
+        paged_decode_kernel<T, DP, MODE><<<(p.waves ? p.waves : a.pv.n_seq) * a.pv.n_kv, 64, bytes, st>>>(a);
+        rc = vla_check_launch("paged_attention");
+    } else rc = launch_prompt<T, DP, MODE>(a, p.own, false, 0, st);
+    if (rc || (p.parts == 1 && !p.waves)) return rc;
+    const int rows = p.decode ? a.pv.n_seq * a.pv.max_rows : a.pv.n_rows;
+    const int heads = (2048 + rows - 1) / rows;              // of a row, that get a workgroup of their own
+    paged_join_kernel<T, DP><<<dim3(rows, heads < a.n_heads ? heads : a.n_heads), 256, 0, st>>>(a);
+    return vla_check_launch("paged_attention join");
+}
 template <typename T, int MODE>
-int launch_sized(const AttnArgs &a, const Launch &p, hipStream_t st) {
+int launch_sized(const AttnArgs &a, const Plan &p, hipStream_t st) {
     switch (padded_dim(a.pv.d)) {
-        case 64: return launch_form<T, 64, MODE>(a, p, st);
-        case 128: return launch_form<T, 128, MODE>(a, p, st);
-        default: return launch_form<T, 256, MODE>(a, p, st);
+        case 64: return launch<T, 64, MODE>(a, p, st);
+        case 128: return launch<T, 128, MODE>(a, p, st);
+        default: return launch<T, 256, MODE>(a, p, st);
     }
 }
 template <typename T>
-int launch_typed(const AttnArgs &a, const Launch &p, hipStream_t st) {
+int launch_typed(const AttnArgs &a, const Plan &p, hipStream_t st) {
     switch ((a.cap > 0.f ? CAPPED : 0) | (a.slopes ? BIASED : 0)) {
         case 0: return launch_sized<T, 0>(a, p, st);
         case CAPPED: return launch_sized<T, CAPPED>(a, p, st);
         case BIASED: return launch_sized<T, BIASED>(a, p, st);
         default: return launch_sized<T, CAPPED | BIASED>(a, p, st);
     }
-}
-template <typename T>
-int attend(AttnArgs a, const Plan &p, void *ws, hipStream_t st) {
-    a.parts = p.parts;
-    const size_t slots = (size_t)a.pv.n_rows * a.n_heads * p.parts;
-    a.ml = (float2 *)ws;
-    a.o_part = (float *)((char *)ws + (slots * sizeof(float2) + 255) / 256 * 256);
-    int rc;
-    if (p.has_whole) {
-        AttnArgs w = a;
-        w.whole = 1; w.row_tiles = p.whole.row_tiles; w.chunk = p.whole.chunk; w.part0 = p.own.parts;
-        if ((rc = launch_typed<T>(w, p.whole, st))) return rc;
-    }
-    a.row_tiles = p.own.row_tiles; a.chunk = p.own.chunk;
-    if ((rc = launch_typed<T>(a, p.own, st))) return rc;
-    if (p.parts == 1) return VLA_OK;
-    const dim3 grid(a.pv.n_rows, a.n_heads);
-    switch (padded_dim(a.pv.d)) {
-        case 64: paged_join_kernel<T, 64><<<grid, 256, 0, st>>>(a); break;
-        case 128: paged_join_kernel<T, 128><<<grid, 256, 0, st>>>(a); break;
-        default: paged_join_kernel<T, 256><<<grid, 256, 0, st>>>(a);
-    }
-    return vla_check_launch("paged_attention join");
 }
 
 }  // namespace
@@ -673,7 +805,7 @@ extern "C" {
 size_t vla_paged_attention_workspace_bytes(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, int n_heads) {
     AttnArgs a{};
     if (check(cache, batch, mask, n_heads, &a)) return 0;
-    return workspace(a, plan(a, cache->dtype == VLA_DTYPE_F32));
+    return lay_out(&a, plan(a, cache->dtype == VLA_DTYPE_F32), nullptr);
 }
 
 int vla_paged_attention(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, const void *q, int n_heads,
@@ -688,7 +820,7 @@ int vla_paged_attention(const vla_paged_cache *cache, const vla_paged_batch *bat
     }
     const bool f32 = cache->dtype == VLA_DTYPE_F32;
     const Plan p = plan(a, f32);
-    const size_t need = workspace(a, p);
+    const size_t need = lay_out(&a, p, (char *)ws);
     if (ws_bytes < need) { vla_set_error("paged_attention: workspace %zu bytes, need %zu", ws_bytes, need); return VLA_EWORKSPACE; }
     if (batch->n_rows == 0 || batch->max_rows == 0) return VLA_OK;
     if (p.own.items > 0x7fffffffL) { vla_set_error("paged_attention: %ld tiles of rows are too many: split the batch", p.own.items); return VLA_ESHAPE; }
@@ -698,7 +830,7 @@ int vla_paged_attention(const vla_paged_cache *cache, const vla_paged_batch *bat
     a.offset = !f32 ? a.cap * 1.4426950408889634f : 0.f;
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps("paged_attention", 0.0, st);
-    return f32 ? attend<float>(a, p, ws, st) : attend<bf16_t>(a, p, ws, st);
+    return f32 ? launch_typed<float>(a, p, st) : launch_typed<bf16_t>(a, p, st);
 }
 
 }  // extern "C"
