@@ -355,6 +355,15 @@ int vla_policy_objective_noalloc(const float *logp_new, const float *logp_old, c
  *   logp (or NULL): log-probability under softmax(z / T), as the recompute gives it; logp_kept (or NULL): among the kept tokens;
  *   n_kept (or NULL).  With T <= 0 or u NULL the cuts still apply to n_kept and logp_kept; T <= 0 counts as 1 in all of them.  Masses are summed as 64-bit fixed point numbers,
  *   in any order the same, so equal inputs give equal tokens. */
+/* vla_forward_paged: the decoder over a ragged batch's new rows: a prefill of prefixes of any lengths, a decode step, or both at once.
+ *   Row r is the embedding of token ids[r], or, where ids[r] < 0, row -1 - ids[r] of patch (DEVICE dtype [n_patch, hidden]; ids and rows out of
+ *   range are clamped).  Every layer appends its K and V to its cache, layer l at cache->k, v + l * layer_stride elements, and attends:
+ *   causally, but for positions below prefix_len[sequence] (or NULL), which every row sees; shared_len as in vla_paged_mask.  The cache
+ *   has the model's dtype, heads and head_dim; any max_len (the model's max_batch and max_seq do not bind it).
+ *   h_last  DEVICE fp32 [n_seq, hidden] out: final-norm output of each sequence's last new row (zeros' where it has none)
+ *   logits  DEVICE fp32 [n_seq, 256] out or NULL: the action bins' (token id vocab - 256 + bin), what vla_sample_logits takes
+ *   value   DEVICE fp32 [n_seq, value_dim] out or NULL
+ *   ws      DEVICE, of vla_forward_paged_workspace_bytes bytes.  n_rows within one pass (see vla_prefill). */
 typedef struct vla_paged_cache {
     void *k, *v;
     int32_t dtype, n_pages, page_size, n_kv_heads, head_dim;
@@ -384,6 +393,11 @@ int vla_paged_attention(const vla_paged_cache *cache, const vla_paged_batch *bat
                         int n_heads, int64_t q_stride, void *out, int64_t out_stride, float *lse, void *ws, size_t ws_bytes,
                         void *stream);
 size_t vla_sample_logits_workspace_bytes(int n, int vocab);
+size_t vla_forward_paged_workspace_bytes(const vla_config *cfg, const vla_paged_cache *cache, const vla_paged_batch *batch,
+                                         int shared_len);
+int vla_forward_paged(vla_model *model, const vla_paged_cache *cache, size_t layer_stride, const vla_paged_batch *batch,
+                      const int32_t *ids, const void *patch, int n_patch, const int32_t *prefix_len, int shared_len, void *ws,
+                      size_t ws_bytes, float *h_last, float *logits, float *value, void *stream);
 int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, int vocab, const float *temperature,
                       const int32_t *top_k, const float *top_p, const float *min_p, const float *u, int32_t *token,
                       float *logp, float *logp_kept, int32_t *n_kept, void *ws, size_t ws_bytes, void *stream);

@@ -139,6 +139,9 @@ def lib() -> C.CDLL:
         L.vla_paged_attention_workspace_bytes.argtypes = [cache, batch, C.POINTER(vla_paged_mask), i32]
         L.vla_paged_attention_workspace_bytes.restype = sz
         L.vla_paged_attention.argtypes = [cache, batch, C.POINTER(vla_paged_mask), vp, i32, i64, vp, i64, vp, vp, sz, vp]
+        L.vla_forward_paged_workspace_bytes.argtypes = [C.POINTER(vla_config), cache, batch, i32]
+        L.vla_forward_paged_workspace_bytes.restype = sz
+        L.vla_forward_paged.argtypes = [vp, cache, sz, batch, vp, vp, i32, vp, i32, vp, sz, vp, vp, vp, vp]
         L.vla_sample_logits_workspace_bytes.argtypes = [i32, i32]
         L.vla_sample_logits_workspace_bytes.restype = sz
         L.vla_sample_logits.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -414,6 +417,23 @@ def vla_paged_attention(cache, batch, mask, q, out, lse=None, ws=None, stream=No
     _check(lib().vla_paged_attention(C.byref(cache), C.byref(batch), C.byref(mask), qp, heads, qs, op, os_,
                                      _want(lse, "float32", "lse", (rows, heads)), _ptr(ws),
                                      0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def vla_forward_paged_workspace_bytes(cfg: vla_config, cache, batch, shared_len: int = 0) -> int:
+    n = lib().vla_forward_paged_workspace_bytes(C.byref(cfg), C.byref(cache), C.byref(batch), shared_len)
+    if n == 0:
+        raise VlaError(VLA_EINVAL, vla_last_error())
+    return n
+
+
+def vla_forward_paged(model, cache, layer_stride: int, batch, ids, ws, h_last, patch=None, prefix_len=None, shared_len=0, logits=None, value=None, stream=None) -> None:
+    """``ids`` int32 [n_rows]; ``patch`` [n_patch, hidden] in the model's type: the rows that negative ids name."""
+    if patch is not None and not patch.is_contiguous():
+        raise VlaError(VLA_EINVAL, "forward_paged: patch is not contiguous")
+    _check(lib().vla_forward_paged(model, C.byref(cache), layer_stride, C.byref(batch), _want(ids, "int32", "ids", (batch.n_rows,)), _ptr(patch),
+                                   0 if patch is None else patch.shape[0], _want(prefix_len, "int32", "prefix_len", (batch.n_seq,)), shared_len, _ptr(ws),
+                                   ws.numel() * ws.element_size(), _want(h_last, "float32", "h_last"), _want(logits, "float32", "logits", (batch.n_seq, VLA_N_BINS)),
+                                   _want(value, "float32", "value"), _stream(stream)))
 
 
 def vla_sample_logits_workspace_bytes(n: int, vocab: int) -> int:

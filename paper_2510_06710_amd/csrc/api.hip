@@ -8,7 +8,7 @@
 #include <new>
 #include <vector>
 
-#include "vla_internal.h"
+#include "paged.h"
 
 // ------------------------------------------------------------------------------------------ errors
 static thread_local char g_err[512] = "";
@@ -712,8 +712,126 @@ int vla_forward_streams(vla_model *m, void *fw_ws, int n_max, const void *patch,
                : forward_streams_impl<bf16_t>(m, fw_ws, n_max, patch, ids, bins, n, P, T, A, mode, slot_embed, n_layers, keep, st);
 }
 
+// ------------------------------------------------------------------------------------------ ragged batches on pages
+// Workspace of vla_forward_paged: that of a forward of as many rows, one row per sequence (a decode step) or all of one, and the paged attention's.
+struct PagedWorkspace {
+    Workspace w;
+    float *last;             // [n_seq, H]
+    double *freq;            // [d / 2]
+    int32_t *bins;           // of the head, which samples too: [n_seq]
+    float *logp, *ent;
+    void *attn;
+    size_t attn_bytes, total;
+};
+static PagedWorkspace plan_paged(const vla_config &c, char *base, const vla_paged_batch &b, size_t attn_bytes) {
+    PagedWorkspace p;
+    const bool step = b.max_rows <= 1;
+    p.w = plan_workspace(c, base, step ? b.n_rows : 1, step ? 1 : b.n_rows, 1, b.n_seq, false);
+    size_t off = p.w.total;
+    auto take = [&](size_t bytes) { char *at = base ? base + off : nullptr; off += align_up(bytes); return (void *)at; };
+    p.last = (float *)take((size_t)b.n_seq * c.hidden * 4);
+    p.freq = (double *)take((size_t)c.hidden / c.n_heads / 2 * sizeof(double));
+    p.bins = (int32_t *)take((size_t)b.n_seq * 4);
+    p.logp = (float *)take((size_t)b.n_seq * 4);
+    p.ent = (float *)take((size_t)b.n_seq * 4);
+    p.attn = take(attn_bytes);
+    p.attn_bytes = attn_bytes;
+    p.total = off;
+    return p;
+}
+
+static vla_paged_mask paged_mask(const vla_config &c, const int32_t *prefix_len, int shared_len) {
+    return vla_paged_mask{1.0f / sqrtf((float)(c.hidden / c.n_heads)), 0.f, nullptr, prefix_len, 0, shared_len};
+}
+
+// Layer by layer as run_layers has it, on row-major activations; rotation and K, V by the paged append, attention on the pages.
+template <typename T>
+static int forward_paged_impl(vla_model *m, const vla_paged_cache &cache, size_t layer_stride, const vla_paged_batch &b, const int32_t *ids,
+                              const void *patch, int n_patch, const vla_paged_mask &mask, const PagedWorkspace &pw, float *h_last,
+                              float *logits, float *value, void *stream) {
+    const vla_config &c = m->cfg;
+    const Workspace &ws = pw.w;
+    const int H = c.hidden, F = c.ffn, M = b.n_rows, d = H / c.n_heads;
+    const bool step = b.max_rows <= 1;
+    hipStream_t st = (hipStream_t)stream;
+    int rc;
+    const vla_rotary rotary{pw.freq, d, 0, 1.0f, 0.f, nullptr, nullptr};
+    if ((rc = launch_rotary_freq(pw.freq, d, c.rope_theta, st))) return rc;
+    if ((rc = launch_paged_embed<T>(ws.X, ids, (const T *)patch, n_patch, (const T *)m->w.embed, M, H, c.vocab, st))) return rc;
+    for (int l = 0; l < c.n_layers; l++) {
+        const vla_layer_weights &lw = m->layers[l];
+        const vla_layer_weights *pk = (step && !m->packed.empty() && kblocked_shape_ok(c)) ? &m->packed[l] : nullptr;
+        vla_paged_cache layer = cache;
+        layer.k = (char *)cache.k + l * layer_stride * elt_size(c);
+        layer.v = (char *)cache.v + l * layer_stride * elt_size(c);
+        auto product = [&](const void *A, int K, const void *const *W, const void *const *Wkb, int n_seg, int segN, void *C, int epilogue) {
+            GemmArgs g{};
+            g.A = A; g.K = K; g.n_seg = n_seg; g.segN = segN; g.C = C; g.M = M; g.epilogue = epilogue; g.a_rows = ws.a_rows; g.step = step;
+            for (int i = 0; i < n_seg; i++) { g.W[i] = W[i]; if (Wkb) g.Wkb[i] = Wkb[i]; }
+            return run_gemm<T>(c, g, ws.skinny, st);
+        };
+        const void *qkv[3] = {lw.wq, lw.wk, lw.wv}, *qkv_kb[3] = {pk ? pk->wq : nullptr, pk ? pk->wk : nullptr, pk ? pk->wv : nullptr};
+        const void *ffn[2] = {lw.w_gate, lw.w_up}, *ffn_kb[2] = {pk ? pk->w_gate : nullptr, pk ? pk->w_up : nullptr};
+        const void *o_kb = pk ? pk->wo : nullptr, *down_kb = pk ? pk->w_down : nullptr;
+        if ((rc = run_rmsnorm<T>(c, ws.Nrm, ws.X, lw.attn_norm, M, 0, st))) return rc;
+        if ((rc = product(ws.Nrm, H, qkv, pk ? qkv_kb : nullptr, 3, H, ws.QKV, EPI_STORE))) return rc;
+        if ((rc = vla_paged_append(&layer, &b, &rotary, ws.QKV, ws.QKV + H, ws.QKV + 2 * H, VLA_DTYPE_F32, c.n_heads, 3L * H, 3L * H, 3L * H, ws.Q, H, stream))) return rc;
+        if ((rc = vla_paged_attention(&layer, &b, &mask, ws.Q, c.n_heads, H, ws.AO, H, nullptr, pw.attn, pw.attn_bytes, stream))) return rc;
+        if ((rc = product(ws.AO, H, &lw.wo, pk ? &o_kb : nullptr, 1, H, ws.X, EPI_RESIDUAL))) return rc;
+        if ((rc = run_rmsnorm<T>(c, ws.Nrm, ws.X, lw.ffn_norm, M, 0, st))) return rc;
+        if ((rc = product(ws.Nrm, H, ffn, pk ? ffn_kb : nullptr, 2, F, ws.ACT, EPI_SWIGLU))) return rc;
+        if ((rc = product(ws.ACT, F, &lw.w_down, pk ? &down_kb : nullptr, 1, H, ws.X, EPI_RESIDUAL))) return rc;
+    }
+    if ((rc = launch_paged_last_rows(pw.last, ws.X, b.row_start, b.n_seq, M, H, st))) return rc;
+    if ((rc = launch_final_norm_rows(h_last, pw.last, (const float *)m->w.final_norm, b.n_seq, 1, 0, 1, H, c.rms_eps, st))) return rc;
+    if (logits && (rc = launch_head_sample<T>(h_last, (const T *)m->w.lm_head + (size_t)(c.vocab - VLA_N_BINS) * H, b.n_seq, H, 1.0f, nullptr, nullptr,
+                                              pw.bins, pw.logp, pw.ent, logits, 1, 0, nullptr, (const T *)nullptr, c.vocab, ws.QKV, st))) return rc;
+    if (value && (rc = launch_value_head(value, h_last, (const float *)m->w.value_w, m->w.value_b, (const float *)m->w.value_bias, value_dim(c), b.n_seq, H, H, st))) return rc;
+    return 0;
+}
+
+// The checks that the size query and the call share; the attention's workspace in *attn_bytes.
+static int check_forward_paged(const vla_config &c, const vla_paged_cache *cache, const vla_paged_batch *b, const vla_paged_mask &mask, size_t *attn_bytes) {
+    PagedView view;
+    if (int rc = vla_check_paged("forward_paged", cache, b, &view)) return rc;
+    if (cache->dtype != c.dtype || cache->n_kv_heads != c.n_heads || cache->head_dim != c.hidden / c.n_heads) {
+        vla_set_error("forward_paged: the cache has %d heads of %d, the model %d of %d, or another dtype", cache->n_kv_heads, cache->head_dim, c.n_heads, c.hidden / c.n_heads);
+        return VLA_ESHAPE;
+    }
+    if (b->n_rows < 1 || b->max_rows < 1) { vla_set_error("forward_paged: n_rows and max_rows must be positive"); return VLA_EINVAL; }
+    if (int rc = check_rows_per_pass(c, 1, b->n_rows)) return rc;
+    *attn_bytes = vla_paged_attention_workspace_bytes(cache, b, &mask, c.n_heads);
+    return *attn_bytes ? VLA_OK : VLA_EINVAL;
+}
+
 // ------------------------------------------------------------------------------------------ C ABI
 extern "C" {
+
+size_t vla_forward_paged_workspace_bytes(const vla_config *cfg, const vla_paged_cache *cache, const vla_paged_batch *batch, int shared_len) {
+    size_t attn = 0;
+    if (check_config(cfg) || check_forward_paged(*cfg, cache, batch, paged_mask(*cfg, nullptr, shared_len), &attn)) return 0;
+    return plan_paged(*cfg, nullptr, *batch, attn).total;
+}
+
+int vla_forward_paged(vla_model *m, const vla_paged_cache *cache, size_t layer_stride, const vla_paged_batch *batch, const int32_t *ids,
+                      const void *patch, int n_patch, const int32_t *prefix_len, int shared_len, void *ws, size_t ws_bytes, float *h_last,
+                      float *logits, float *value, void *stream) {
+    if (!m || !ids || !ws || !h_last) { vla_set_error("forward_paged: model, ids, ws or h_last is NULL"); return VLA_EINVAL; }
+    if (n_patch < 0 || (n_patch > 0 && !patch)) { vla_set_error("forward_paged: n_patch is negative or patch is NULL"); return VLA_EINVAL; }
+    if (value && !m->w.value_w) { vla_set_error("value requested but the model has no value head"); return VLA_EINVAL; }
+    const vla_config &c = m->cfg;
+    const vla_paged_mask mask = paged_mask(c, prefix_len, shared_len);
+    size_t attn = 0;
+    if (int rc = check_forward_paged(c, cache, batch, mask, &attn)) return rc;
+    const size_t layer = (size_t)cache->n_pages * cache->n_kv_heads * cache->page_size * cache->head_dim;
+    if (c.n_layers > 1 && layer_stride < layer) { vla_set_error("forward_paged: layer stride of %zu elements, a layer has %zu", layer_stride, layer); return VLA_ESHAPE; }
+    if (layer_stride * elt_size(c) % 16) { vla_set_error("forward_paged: the layers are not 16-byte aligned"); return VLA_EINVAL; }
+    if ((uintptr_t)ws % 16) { vla_set_error("forward_paged: ws is not 16-byte aligned"); return VLA_EINVAL; }
+    const PagedWorkspace p = plan_paged(c, (char *)ws, *batch, attn);
+    if (ws_bytes < p.total) { vla_set_error("workspace %zu bytes, need %zu", ws_bytes, p.total); return VLA_EWORKSPACE; }
+    return c.dtype == VLA_DTYPE_F32 ? forward_paged_impl<float>(m, *cache, layer_stride, *batch, ids, patch, n_patch, mask, p, h_last, logits, value, stream)
+                                    : forward_paged_impl<bf16_t>(m, *cache, layer_stride, *batch, ids, patch, n_patch, mask, p, h_last, logits, value, stream);
+}
 
 int vla_version(void) { return VLA_VERSION; }
 

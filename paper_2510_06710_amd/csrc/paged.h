@@ -13,6 +13,12 @@ struct PagedView {
 // Host: 0 or an error code with the message set.  `what` names the entry point.
 int vla_check_paged(const char *what, const vla_paged_cache *cache, const vla_paged_batch *batch, PagedView *out);
 
+// Rows of a ragged batch as the decoder takes and gives them (vla_forward_paged).
+template <typename T>
+int launch_paged_embed(float *X, const int32_t *ids, const T *patch, int n_patch, const T *embed, int n_rows, int H, int vocab, hipStream_t st);
+int launch_paged_last_rows(float *out, const float *X, const int32_t *row_start, int n_seq, int n_rows, int H, hipStream_t st);
+int launch_rotary_freq(double *freq, int d, float theta, hipStream_t st);
+
 // The batch's arrays do not change while a kernel runs: read as constants, uniform indexes through the scalar cache (behind the
 // kernels' assembler text the compiler would otherwise take vector loads, and wait for everything in flight).
 typedef const __attribute__((address_space(4))) int32_t *const_ints;

@@ -148,7 +148,41 @@ __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a) {
     }
 }
 
+template <typename T>
+__global__ void __launch_bounds__(256) paged_embed_kernel(float *X, const int32_t *ids, const T *patch, int n_patch, const T *embed, int H, int vocab) {
+    const int id = ids[blockIdx.x];
+    const T *src = id < 0 && n_patch > 0 ? patch + (size_t)min(-(id + 1), n_patch - 1) * H : embed + (size_t)min(max(id, 0), vocab - 1) * H;
+    for (int i = threadIdx.x; i < H; i += 256) X[(size_t)blockIdx.x * H + i] = (float)src[i];
+}
+
+// The last of each sequence's rows; zeros for a sequence without rows.
+__global__ void __launch_bounds__(256) paged_last_rows_kernel(float *out, const float *X, const int32_t *row_start, int n_rows, int H) {
+    const int s = blockIdx.x, r0 = min(max(row_start[s], 0), n_rows), r1 = min(max(row_start[s + 1], r0), n_rows);
+    for (int i = threadIdx.x; i < H; i += 256) out[(size_t)s * H + i] = r1 > r0 ? X[(size_t)(r1 - 1) * H + i] : 0.f;
+}
+
+// theta^(-2 i / d), as vla_rope_entry has it
+__global__ void rotary_freq_kernel(double *freq, int d, float theta) {
+    if ((int)threadIdx.x < d / 2) freq[threadIdx.x] = pow((double)theta, -2.0 * (double)threadIdx.x / (double)d);
+}
+
 }  // namespace
+
+template <typename T>
+int launch_paged_embed(float *X, const int32_t *ids, const T *patch, int n_patch, const T *embed, int n_rows, int H, int vocab, hipStream_t st) {
+    paged_embed_kernel<T><<<n_rows, 256, 0, st>>>(X, ids, patch, n_patch, embed, H, vocab);
+    return vla_check_launch("paged_embed");
+}
+template int launch_paged_embed<float>(float *, const int32_t *, const float *, int, const float *, int, int, int, hipStream_t);
+template int launch_paged_embed<bf16_t>(float *, const int32_t *, const bf16_t *, int, const bf16_t *, int, int, int, hipStream_t);
+int launch_paged_last_rows(float *out, const float *X, const int32_t *row_start, int n_seq, int n_rows, int H, hipStream_t st) {
+    paged_last_rows_kernel<<<n_seq, 256, 0, st>>>(out, X, row_start, n_rows, H);
+    return vla_check_launch("paged_last_rows");
+}
+int launch_rotary_freq(double *freq, int d, float theta, hipStream_t st) {
+    rotary_freq_kernel<<<1, 128, 0, st>>>(freq, d, theta);
+    return vla_check_launch("rotary_freq");
+}
 
 int vla_check_paged(const char *what, const vla_paged_cache *c, const vla_paged_batch *b, PagedView *out) {
     if (!c || !b) { vla_set_error("%s: cache or batch is NULL", what); return VLA_EINVAL; }

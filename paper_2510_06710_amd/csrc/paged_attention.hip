@@ -733,6 +733,11 @@ Plan plan(const AttnArgs &a, bool f32) {
     }
     return p;
 }
+int check_plan(const Plan &p) {
+    const long most = p.own.items > p.whole.items ? p.own.items : p.whole.items;
+    if (most > 0x7fffffffL / 256) { vla_set_error("paged_attention: %ld tiles of rows are too many: split the batch", most); return VLA_ESHAPE; }
+    return VLA_OK;
+}
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 // Lays the workspace out from `base` (NULL: only its size).
 size_t lay_out(AttnArgs *a, const Plan &p, char *base) {
@@ -805,7 +810,8 @@ extern "C" {
 size_t vla_paged_attention_workspace_bytes(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, int n_heads) {
     AttnArgs a{};
     if (check(cache, batch, mask, n_heads, &a)) return 0;
-    return lay_out(&a, plan(a, cache->dtype == VLA_DTYPE_F32), nullptr);
+    const Plan p = plan(a, cache->dtype == VLA_DTYPE_F32);
+    return check_plan(p) ? 0 : lay_out(&a, p, nullptr);
 }
 
 int vla_paged_attention(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, const void *q, int n_heads,
@@ -820,10 +826,10 @@ int vla_paged_attention(const vla_paged_cache *cache, const vla_paged_batch *bat
     }
     const bool f32 = cache->dtype == VLA_DTYPE_F32;
     const Plan p = plan(a, f32);
+    if (int rc = check_plan(p)) return rc;
     const size_t need = lay_out(&a, p, (char *)ws);
     if (ws_bytes < need) { vla_set_error("paged_attention: workspace %zu bytes, need %zu", ws_bytes, need); return VLA_EWORKSPACE; }
     if (batch->n_rows == 0 || batch->max_rows == 0) return VLA_OK;
-    if (p.own.items > 0x7fffffffL) { vla_set_error("paged_attention: %ld tiles of rows are too many: split the batch", p.own.items); return VLA_ESHAPE; }
     const size_t es = f32 ? 4 : 2;
     a.q = (const char *)q; a.out = (char *)out; a.lse = lse; a.q_stride = q_stride; a.o_stride = out_stride;
     a.aligned = ((uintptr_t)q | (uintptr_t)out | (size_t)q_stride * es | (size_t)out_stride * es) % 16 == 0;

@@ -1,0 +1,140 @@
+"""The paged operators together: rollouts of ragged batches through vla_forward_paged and vla_sample_logits against the oracle's, environment by environment
+(its caches are contiguous and its batches uniform), a group that shares its observation's pages, and a decode step in a captured graph."""
+import numpy as np
+import pytest
+import torch
+
+import vla_inputs as vi
+from oracle import vla_oracle as vo
+from oracle.from_inputs import oracle_config, oracle_weights, to_f64
+from paged_ref import sample
+from paper_2510_06710_amd import binding as vb
+from paper_2510_06710_amd.harness import PagedRollout, Rollout
+from parity import TOL
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+SHAPES = {"f32": vi.TINY, "bf16": vi.ModelShape(n_layers=1, hidden=256, n_heads=2, ffn=512, vocab=1024, dtype="bf16"),
+          "bf16_wide": vi.ModelShape(n_layers=1, hidden=1024, n_heads=8, ffn=1024, vocab=1024, dtype="bf16")}
+
+
+def setup(name, lengths, seed=3):
+    """Environments of lengths [(patches, instruction ids)], their observations, model and weights."""
+    shape = SHAPES[name]
+    synth = vi.SynthModel(shape, seed, device=DEV)
+    run = Rollout(synth, 4, 16, value_b=vi.VALUE_BIAS)
+    obs = [vi.observation(vi.Workload("w", shape, 1, p, t, 4), seed + i, device=DEV) for i, (p, t) in enumerate(lengths)]
+    cfg = oracle_config(shape, "bf16" if shape.dtype == "bf16" else "exact")
+    return run, [(p[0], t[0]) for p, t in obs], cfg, oracle_weights(vi.SynthModel(shape, seed), vi.VALUE_BIAS)
+
+
+def follow(cfg, w, patch, ids, bins):
+    """Oracle logits of each token of one environment whose sampled bins are given, and its value."""
+    kv, h, value = vo.ovla_prefill(cfg, w, to_f64(patch.cpu())[None], ids.cpu().numpy().astype(np.int64)[None])
+    logp, ent, v, logits = vo.ovla_logprob_recompute(cfg, w, to_f64(patch.cpu())[None], ids.cpu().numpy().astype(np.int64)[None], bins[None], len(bins), 0, None, 1.0)
+    return logits[0], value[0]
+
+
+LENGTHS = [(5, 3), (0, 1), (48, 16), (16, 0), (31, 2), (100, 29)]
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16", "bf16_wide"])
+@pytest.mark.parametrize("page", [16, 64])
+def test_ragged_rollout(name, page):
+    lengths = [l if l[1] else (l[0], 1) for l in LENGTHS]
+    run, obs, cfg, w = setup(name, lengths)
+    paged = PagedRollout(run, 64, page)
+    u = torch.rand(4, len(obs), generator=torch.Generator().manual_seed(1)).to(DEV)
+    _, logits, value = paged.prefill([p for p, _ in obs], [t for _, t in obs])
+    bins, logp, kept, z = paged.decode(logits, 4, temperature=1.6, top_k=40, top_p=0.9, min_p=0.01, u=u)
+    torch.cuda.synchronize()
+    tol = TOL["f32" if name == "f32" else "bf16"]
+    for i, (patch, ids) in enumerate(obs):
+        got = bins[i].cpu().numpy()
+        ref, v = follow(cfg, w, patch, ids, got)
+        assert np.abs(z[i].double().cpu().numpy() - ref).max() <= tol["logits"], i
+        assert abs(value[i].item() - np.ravel(v)[0]) <= tol["value"]
+        for j in range(4):                                   # what was sampled is what these logits give
+            want = sample(z[i, j].double().cpu().numpy(), torch.tensor(1.6).item(), 40, torch.tensor(0.9).item(), torch.tensor(0.01).item(), u[j, i].item())
+            assert got[j] == want[0] and abs(logp[i, j].item() - want[2]) < 1e-5 and abs(kept[i, j].item() - want[3]) < 1e-5
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_patches_that_see_each_other(name):
+    run, obs, cfg, w = setup(name, [(33, 5), (7, 2)])
+    paged = PagedRollout(run, 32)
+    _, logits, _ = paged.prefill([p for p, _ in obs], [t for _, t in obs], see_patches=True)
+    torch.cuda.synchronize()
+    causal = [follow(cfg, w, p, t, np.zeros(1, np.int64))[0][0] for p, t in obs]
+    assert min(np.abs(l.double().cpu().numpy() - c).max() for l, c in zip(logits, causal)) > 1e-3          # the mask does change the logits
+    # ... and with every prefix of length 1 it is the causal mask again
+    ones = [o[0][:1] for o in obs]
+    _, a, _ = PagedRollout(run, 32).prefill(ones, [t for _, t in obs], see_patches=True)
+    _, b, _ = PagedRollout(run, 32).prefill(ones, [t for _, t in obs])
+    assert (a - b).abs().max().item() <= TOL["f32" if name == "f32" else "bf16"]["logits"]
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("group", [1, 3, 9])
+def test_group_shares_its_observation(name, group):
+    run, obs, cfg, w = setup(name, [(48, 21)])
+    paged = PagedRollout(run, 64)
+    u = torch.rand(3, group, generator=torch.Generator().manual_seed(2)).to(DEV)
+    _, logits, _ = paged.prefill_group(*obs[0], group)
+    if group > 1:
+        assert paged.pages[1][:4] == paged.pages[0][:4] and paged.pages[1][4] != paged.pages[0][4] and paged.shared_len == 64
+    bins, _, _, z = paged.decode(logits, 3, u=u)
+    torch.cuda.synchronize()
+    for i in range(group):
+        ref, _ = follow(cfg, w, *obs[0], bins[i].cpu().numpy())
+        assert np.abs(z[i].double().cpu().numpy() - ref).max() <= TOL["f32" if name == "f32" else "bf16"]["logits"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_captured_step_follows_its_arrays(dtype):
+    """Append, attention and sampling of one token per sequence in a graph: replayed with other lengths, tables and inputs it gives what eager calls give."""
+    kind = torch.bfloat16 if dtype == "bf16" else torch.float32
+    n, heads, kv, d, page, entries, vocab = 5, 4, 2, 64, 16, 40, 1000
+    g = torch.Generator().manual_seed(9)
+    pools = [torch.randn(n * entries, kv, page, d, generator=g).to(kind).to(DEV) for _ in range(2)]
+    start, lens = torch.arange(n + 1, dtype=torch.int32, device=DEV), torch.zeros(n, dtype=torch.int32, device=DEV)
+    table = torch.zeros(n, entries, dtype=torch.int32, device=DEV)
+    qkv, z, u = torch.zeros(n, heads + 2 * kv, d, device=DEV), torch.zeros(n, vocab, device=DEV), torch.zeros(n, device=DEV)
+    q, out = (torch.zeros(n, heads, d, dtype=kind, device=DEV) for _ in range(2))
+    token, top_k = torch.zeros(n, dtype=torch.int32, device=DEV), torch.full((n,), 50, dtype=torch.int32, device=DEV)
+    freq = (10000.0 ** (-torch.arange(d // 2, dtype=torch.float64) / (d // 2))).to(DEV)
+    cache, batch, mask = vb.make_paged_cache(*pools), vb.make_paged_batch(start, lens, table, n, 1, entries * page), vb.make_paged_mask(d ** -0.5)
+    ws = torch.empty(vb.vla_paged_attention_workspace_bytes(cache, batch, mask, heads), dtype=torch.uint8, device=DEV)
+    ws2 = torch.empty(vb.vla_sample_logits_workspace_bytes(n, vocab), dtype=torch.uint8, device=DEV)
+
+    def step():
+        vb.vla_paged_append(cache, batch, vb.make_rotary(freq), qkv[:, :heads], qkv[:, heads:heads + kv], qkv[:, heads + kv:], q)
+        vb.vla_paged_attention(cache, batch, mask, q, out, None, ws)
+        vb.vla_sample_logits(z, token, top_k=top_k, u=u, ws=ws2)
+
+    def inputs(seed):
+        r = torch.Generator().manual_seed(seed)
+        lens.copy_(torch.randint(1, entries * page, (n,), generator=r))
+        table.copy_(torch.randperm(n * entries, generator=r).view(n, entries))
+        qkv.copy_(torch.randn(qkv.shape, generator=r))
+        z.copy_(torch.randn(z.shape, generator=r) * 3)
+        u.copy_(torch.rand(n, generator=r))
+
+    inputs(0)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (1, 2, 3, 1):
+        inputs(seed)
+        saved = [p.clone() for p in pools]
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (q, out, token, *pools)]
+        for p, s in zip(pools, saved):
+            p.copy_(s)
+        ws.fill_(255)
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (q, out, token, *pools)))

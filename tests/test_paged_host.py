@@ -106,3 +106,24 @@ def test_binding_refuses_arrays_that_would_be_read_wrongly():
                 lambda: vb.vla_sample_logits(z(4, 9).T, z(9, dtype=i32)), lambda: vb.vla_sample_logits(z(4, 9), z(4)), lambda: vb.vla_sample_logits(z(4, 9), z(4, dtype=i32), top_k=z(4))):
         with pytest.raises(vb.VlaError):
             bad()
+
+
+def test_forward_paged_refuses():
+    import vla_inputs as vi
+    from test_abi_host import fake_model
+    cfg = vb.make_config(vi.TINY, 8, 80)
+    h, keep = fake_model(cfg)
+    L = vb.lib()
+    good = dict(dtype=vb.VLA_DTYPE_F32, n_kv_heads=4, head_dim=64)
+
+    def f(c=good, b={}, model=h, stride=1 << 20, ids=P, patch=P, n_patch=4, shared=0, ws=P, size=1 << 40, hl=P, value=None):
+        cc, bb = cache(**c), batch(**b)
+        return L.vla_forward_paged(model, C.byref(cc), stride, C.byref(bb), ids, patch, n_patch, None, shared, ws, size, hl, None, value, None)
+
+    assert f(model=None) == f(ids=None) == f(ws=None) == f(hl=None) == f(patch=None) == f(n_patch=-1) == f(value=P) == vb.VLA_EINVAL
+    assert f(ws=P + 4) == f(stride=(1 << 20) + 1) == f(b=dict(n_rows=0)) == f(b=dict(max_rows=0)) == vb.VLA_EINVAL
+    assert f(c=dict(good, dtype=vb.VLA_DTYPE_BF16)) == f(c=dict(good, n_kv_heads=2)) == f(c=dict(good, head_dim=48)) == f(stride=100) == vb.VLA_ESHAPE
+    assert f(c=dict(good, page_size=24)) == f(b=dict(n_rows=1 << 30)) == vb.VLA_ESHAPE and f(size=1000) == vb.VLA_EWORKSPACE
+    q = lambda **k: L.vla_forward_paged_workspace_bytes(C.byref(cfg), C.byref(cache(**dict(good, **k))), C.byref(batch()), 0)
+    assert q() > 5 * 256 * 4 and q(head_dim=48) == 0
+    vb.vla_destroy(h)
