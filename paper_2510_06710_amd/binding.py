@@ -313,9 +313,20 @@ def vla_logp_aggregate(logp, n_out, inner, out, stream=None) -> None:
     _check(lib().vla_logp_aggregate(_ptr(logp), n_out, inner, _ptr(out), _stream(stream)))
 
 
+_codes = {}
+
+
+def _known() -> dict:
+    """torch's types: VLA_DTYPE_* of those that storage has, and by name."""
+    if not _codes:
+        import torch
+        _codes.update({torch.float32: VLA_DTYPE_F32, torch.bfloat16: VLA_DTYPE_BF16, "float32": torch.float32, "int32": torch.int32,
+                       "float64": torch.float64})
+    return _codes
+
+
 def _dtype(t) -> int:
-    import torch
-    code = {torch.float32: VLA_DTYPE_F32, torch.bfloat16: VLA_DTYPE_BF16}.get(t.dtype)
+    code = _known().get(t.dtype)
     if code is None:
         raise VlaError(VLA_EDTYPE, f"{t.dtype} is neither float32 nor bfloat16")
     return code
@@ -325,7 +336,7 @@ def _want(t, kind: str, name: str, shape=None):
     """An array argument the library reads as packed values of one type: another type, shape or layout would be read wrongly."""
     if t is None:
         return None
-    if str(t.dtype) != "torch." + kind or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+    if t.dtype is not _known()[kind] or not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise VlaError(VLA_EINVAL, f"{name}: contiguous {kind}{'' if shape is None else ' ' + str(list(shape))} wanted, "
                                    f"{t.dtype} {list(t.shape)} given")
     return t.data_ptr()

@@ -218,7 +218,7 @@ extern "C" int vla_paged_append(const vla_paged_cache *cache, const vla_paged_ba
     AppendArgs a{};
     if (int rc = vla_check_paged("paged_append", cache, batch, &a.pv)) return rc;
     if (in_dtype != VLA_DTYPE_F32 && in_dtype != VLA_DTYPE_BF16) { vla_set_error("paged_append: unknown dtype %d", in_dtype); return VLA_EDTYPE; }
-    if (!rotary || !k || !v) { vla_set_error("paged_append: rotary, k or v is NULL"); return VLA_EINVAL; }
+    if (!rotary || (batch->n_rows > 0 && (!k || !v))) { vla_set_error("paged_append: rotary, k or v is NULL"); return VLA_EINVAL; }
     if (!q != !q_out) { vla_set_error("paged_append: q and q_out come together"); return VLA_EINVAL; }
     const int d = cache->head_dim, kv = cache->n_kv_heads;
     if (q && (n_heads <= 0 || n_heads > 65536)) { vla_set_error("paged_append: n_heads %d unsupported (1 .. 65,536)", n_heads); return VLA_ESHAPE; }

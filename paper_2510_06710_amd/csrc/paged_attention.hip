@@ -818,7 +818,7 @@ int vla_paged_attention(const vla_paged_cache *cache, const vla_paged_batch *bat
                         int64_t q_stride, void *out, int64_t out_stride, float *lse, void *ws, size_t ws_bytes, void *stream) {
     AttnArgs a{};
     if (int rc = check(cache, batch, mask, n_heads, &a)) return rc;
-    if (!q || !out || !ws) { vla_set_error("paged_attention: q, out or ws is NULL"); return VLA_EINVAL; }
+    if (batch->n_rows > 0 && (!q || !out || !ws)) { vla_set_error("paged_attention: q, out or ws is NULL"); return VLA_EINVAL; }
     if ((uintptr_t)ws % 16) { vla_set_error("paged_attention: ws is not 16-byte aligned"); return VLA_EINVAL; }
     if (q_stride < (int64_t)n_heads * cache->head_dim || out_stride < (int64_t)n_heads * cache->head_dim) {
         vla_set_error("paged_attention: a row stride is shorter than its heads");
@@ -828,7 +828,7 @@ int vla_paged_attention(const vla_paged_cache *cache, const vla_paged_batch *bat
     const Plan p = plan(a, f32);
     if (int rc = check_plan(p)) return rc;
     const size_t need = lay_out(&a, p, (char *)ws);
-    if (ws_bytes < need) { vla_set_error("paged_attention: workspace %zu bytes, need %zu", ws_bytes, need); return VLA_EWORKSPACE; }
+    if (batch->n_rows > 0 && ws_bytes < need) { vla_set_error("paged_attention: workspace %zu bytes, need %zu", ws_bytes, need); return VLA_EWORKSPACE; }
     if (batch->n_rows == 0 || batch->max_rows == 0) return VLA_OK;
     const size_t es = f32 ? 4 : 2;
     a.q = (const char *)q; a.out = (char *)out; a.lse = lse; a.q_stride = q_stride; a.o_stride = out_stride;
