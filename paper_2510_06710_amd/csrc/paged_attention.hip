@@ -57,6 +57,11 @@ struct AttnArgs {
     float *o_part;           // [parts][n_rows][n_heads][d]
 };
 
+__device__ __forceinline__ int wave_min(int v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+    return __builtin_amdgcn_readfirstlane(v);
+}
 __device__ __forceinline__ int wave_sum(int v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -101,25 +106,54 @@ template <typename T, int DP> struct Tile {
         if constexpr (sizeof(T) == 4) return 0;
         return 2 * (CPR < 16 ? r & 3 : (r & 3) | (r & 1) << 2);
     }
-    // 16 rows from key0 on (a multiple of 16: one page) of K or V.  Keys that no query of the tile sees are not read: outside [lo, hi)
+    // ROWS rows from row r0 on of the 16 keys from key0 on (a multiple of 16: one page), of K or V.  Keys that no query of the tile sees are not read: outside [lo, hi)
     // the nearest one inside takes their place, in [g0, g1) the nearest one outside.
-    template <bool V>
-    __device__ static void load16(unsigned at, const char *pool, const PagedView &pv, int page, int kvh, int key0, const Span &sp) {
+    template <bool V, int ROWS>
+    __device__ static void load(unsigned at, const char *pool, const PagedView &pv, int page, int kvh, int key0, const Span &sp, int r0 = 0) {
         const int lane = threadIdx.x & 63, row_bytes = pv.d * (int)sizeof(T), chunks = row_bytes >> 4;
         const bool ok = (unsigned)page < (unsigned)pv.n_pages;
         const char *base = ok ? pool + (((size_t)page * pv.n_kv + kvh) << pv.page_log) * row_bytes : (const char *)zero_row;
         const int in_page = ok ? (1 << pv.page_log) - 1 : 0;
 #pragma unroll
-        for (int i = 0; i < 16 / RPI; i++) {
-            const int r = i * RPI + lane / CPR;
+        for (int i = 0; i < ROWS / RPI; i++) {
+            const int r = r0 + i * RPI + lane / CPR;
             int key = min(max(key0 + r, sp.lo), sp.hi - 1);
             if (key >= sp.g0 && key < sp.g1) key = key0 >= sp.g0 || key0 + 15 >= sp.g1 ? sp.g1 : sp.g0 - 1;
             const int c = min((lane % CPR) ^ (V ? fv(r) : fk(r)), chunks - 1);
             dma16(at + i * 1024, (unsigned)((key & in_page) * row_bytes + c * 16), base);
         }
     }
+    // The same where all of the rows are read and their page is there: a lane's offsets do not change from tile to tile.
+    template <bool V, int ROWS> struct Offsets {
+        unsigned off[ROWS / RPI];
+        __device__ __forceinline__ void start(const PagedView &pv, int r0) {
+            const int lane = threadIdx.x & 63, row_bytes = pv.d * (int)sizeof(T), chunks = row_bytes >> 4;
+#pragma unroll
+            for (int i = 0; i < ROWS / RPI; i++) {
+                const int r = r0 + i * RPI + lane / CPR;
+                off[i] = r * row_bytes + min((lane % CPR) ^ (V ? fv(r) : fk(r)), chunks - 1) * 16;
+            }
+        }
+        __device__ __forceinline__ void load(unsigned at, const char *rows) const {
+#pragma unroll
+            for (int i = 0; i < ROWS / RPI; i++) dma16(at + i * 1024, off[i], rows);
+        }
+    };
+};
+// Where the 16 keys from key0 on begin in k and in v.
+struct Place {
+    unsigned page_bytes, head_bytes, row_bytes;
+    __device__ __forceinline__ Place(const PagedView &pv, int kvh, int size) {
+        row_bytes = pv.d * size;
+        head_bytes = ((unsigned)kvh << pv.page_log) * row_bytes;
+        page_bytes = ((unsigned)pv.n_kv << pv.page_log) * row_bytes;
+    }
+    __device__ __forceinline__ size_t at(const PagedView &pv, int page, int key0) const {
+        return (size_t)(unsigned)page * page_bytes + head_bytes + (key0 & ((1 << pv.page_log) - 1)) * row_bytes;
+    }
 };
 
+constexpr float LOG2E = 1.4426950408889634f;
 constexpr int CAPPED = 1, BIASED = 2;          // bits of MODE
 
 // What one lane knows of its query.
@@ -187,70 +221,108 @@ template <typename T, int DP, int MODE> struct Rows {
         l = 0.f;
     }
 
-    // 32 NB keys from key0 on, K and V at kt and vt in LDS.  masked: some query may not see some key.
-    template <int NB>
-    __device__ __forceinline__ void tile(const AttnArgs &a, const Query &y, const char *kt, const char *vt, int key0, bool masked) {
+    // The steps of a tile of 32 keys from key0 on, K and V at kt and vt in LDS.  Scores: a lane's query against 16 of the keys,
+    // register i is key 8 (i / 4) + 4 hh + i % 4.
+    __device__ __forceinline__ static frag key(const char *kt, int kk) {
         const int lane = threadIdx.x & 63, col = lane & 31, hh = lane >> 5;
-        f32x16_t x[NB];
+        const char *row = kt + col * TL::ROW;
+        if constexpr (sizeof(T) == 2) return *(const frag *)(row + ((2 * kk + hh) ^ TL::fk(col)) * 16);
+        else {
+            const f32x4_t u = *(const f32x4_t *)(row + ((4 * kk + 2 * hh) ^ TL::fk(col)) * 16), w = *(const f32x4_t *)(row + ((4 * kk + 2 * hh + 1) ^ TL::fk(col)) * 16);
+            return __builtin_shufflevector(u, w, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+    __device__ __forceinline__ void scores(f32x16_t &x, const char *kt) const {
 #pragma unroll
-        for (int n = 0; n < NB; n++) {
+        for (int i = 0; i < 16; i++) x[i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; i++) x[n][i] = 0.f;
+        for (int kk = 0; kk < KS; kk++) x = mma(key(kt, kk), q[kk], x);
+    }
+    // scores(next, kt) and weights(p, x) in turn: a matrix instruction, then the vector work it covers (left to itself the compiler
+    // puts all of the one before all of the other).  The operands come out of LDS three instructions ahead.
+    __device__ __forceinline__ void scores_and_weights(f32x16_t &next, const char *kt, frag (&p)[2], const f32x16_t &x, float unit) {
+        constexpr int EACH = 16 / KS, AHEAD = KS < 3 ? KS : 3;
+        const float ref = m == -INFINITY ? 0.f : m;
+        frag k[AHEAD];
 #pragma unroll
-            for (int kk = 0; kk < KS; kk++) {
-                const char *row = kt + (n * 32 + col) * TL::ROW;
-                frag k;
-                if constexpr (sizeof(T) == 2) k = *(const frag *)(row + ((2 * kk + hh) ^ TL::fk(col)) * 16);
-                else {
-                    const f32x4_t u = *(const f32x4_t *)(row + ((4 * kk + 2 * hh) ^ TL::fk(col)) * 16), w = *(const f32x4_t *)(row + ((4 * kk + 2 * hh + 1) ^ TL::fk(col)) * 16);
-                    k = __builtin_shufflevector(u, w, 0, 1, 2, 3, 4, 5, 6, 7);
-                }
-                x[n] = mma(k, q[kk], x[n]);
+        for (int kk = 0; kk < AHEAD; kk++) k[kk] = key(kt, kk);
+#pragma unroll
+        for (int i = 0; i < 16; i++) next[i] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KS; kk++) {
+            __builtin_amdgcn_sched_barrier(0);
+            next = mma(k[kk % AHEAD], q[kk], next);
+            if (kk + AHEAD < KS) k[kk % AHEAD] = key(kt, kk + AHEAD);
+#pragma unroll
+            for (int i = kk * EACH; i < (kk + 1) * EACH; i++) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, -ref));
+                l += w;
+                p[i / 8][i % 8] = (T)w;
             }
         }
-        // scores in log2 units are x unit (+ AttnArgs::offset, which changes no weight)
-        constexpr float LOG2E = 1.4426950408889634f;
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // values(p, vt), and in its cover shape and the largest of `next`.
+    __device__ __forceinline__ float values_and_largest(const frag (&p)[2], const char *vt, f32x16_t &next, const AttnArgs &a, const Query &y, int key0) {
+        constexpr int N = 2 * DB, EACH = (16 + N - 1) / N, AHEAD = 3;
+        frag v[AHEAD];
+        float top = -INFINITY;
+#pragma unroll
+        for (int s = 0; s < AHEAD; s++) v[s] = value(vt, s / DB, s % DB);
+#pragma unroll
+        for (int s = 0; s < N; s++) {
+            __builtin_amdgcn_sched_barrier(0);
+            o[s % DB] = mma(v[s % AHEAD], p[s / DB], o[s % DB]);
+            if (s + AHEAD < N) v[s % AHEAD] = value(vt, (s + AHEAD) / DB, (s + AHEAD) % DB);
+#pragma unroll
+            for (int i = s * EACH; i < (s + 1) * EACH && i < 16; i++) {
+                next[i] = shaped(next[i], a, y, key0, i);
+                top = fmaxf(top, next[i]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        return vla_fold_step<32>(top, VlaMax()) * unit_of(a);
+    }
+    // Scores in log2 units are x unit (+ AttnArgs::offset, which changes no weight).
+    __device__ __forceinline__ static float unit_of(const AttnArgs &a) {
+        if (MODE & BIASED) return 1.f;
+        if (MODE & CAPPED) return (sizeof(T) == 4 ? 1.f : 2.f) * a.cap * LOG2E;
+        return a.scale * LOG2E;
+    }
+    // One score of the tile from key0 on; i as in scores.
+    __device__ __forceinline__ static float shaped(float x, const AttnArgs &a, const Query &y, int key0, int i) {
         float unit = a.scale * LOG2E;
         if (MODE & CAPPED) {
             if constexpr (sizeof(T) == 4) {
-                const float back = a.scale / a.cap;
                 unit = a.cap * LOG2E;
-#pragma unroll
-                for (int n = 0; n < NB; n++)
-#pragma unroll
-                    for (int i = 0; i < 16; i++) x[n][i] = tanhf(x[n][i] * back);
+                x = tanhf(x * (a.scale / a.cap));
             } else {                                         // tanh t = 1 - 2 / (1 + e^2t); the 1 is the offset
-                const float twice = 2.f * LOG2E * a.scale / a.cap;
                 unit = 2.f * a.cap * LOG2E;
-#pragma unroll
-                for (int n = 0; n < NB; n++)
-#pragma unroll
-                    for (int i = 0; i < 16; i++) x[n][i] = -__builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[n][i] * twice));
+                x = -__builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * LOG2E * a.scale / a.cap)));
             }
         }
         if (MODE & BIASED) {
-            const float slope = -y.slope * LOG2E, away = (float)(y.p - key0 - 4 * hh);
-#pragma unroll
-            for (int n = 0; n < NB; n++)
-#pragma unroll
-                for (int i = 0; i < 16; i++) x[n][i] = __builtin_fmaf(slope, fabsf(away - (float)(n * 32 + 8 * (i / 4) + i % 4)), x[n][i] * unit);
-            unit = 1.f;
+            const float away = (float)(y.p - key0 - 4 * (int)((threadIdx.x >> 5) & 1));
+            x = __builtin_fmaf(-y.slope * LOG2E, fabsf(away - (float)(8 * (i / 4) + i % 4)), x * unit);
         }
-        if (masked) {
+        return x;
+    }
+    __device__ __forceinline__ static void hide(f32x16_t &x, const Query &y, int key0) {
+        const int j0 = key0 + 4 * (int)((threadIdx.x >> 5) & 1);
 #pragma unroll
-            for (int n = 0; n < NB; n++)
-#pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    const int j = key0 + n * 32 + 8 * (i / 4) + 4 * hh + i % 4;
-                    if (!((j < y.hi && j >= y.lo) || j < y.pre)) x[n][i] = -INFINITY;
-                }
+        for (int i = 0; i < 16; i++) {
+            const int j = j0 + 8 * (i / 4) + i % 4;
+            if (!((j < y.hi && j >= y.lo) || j < y.pre)) x[i] = -INFINITY;
         }
-        float top = x[0][0];
+    }
+    // The largest of a query's scores, in log2 units.
+    __device__ __forceinline__ static float largest(const f32x16_t &x, float unit) {
+        float top = x[0];
 #pragma unroll
-        for (int n = 0; n < NB; n++)
-#pragma unroll
-            for (int i = 0; i < 16; i++) top = fmaxf(top, x[n][i]);
-        top = vla_fold_step<32>(top, VlaMax()) * unit;
+        for (int i = 1; i < 16; i++) top = fmaxf(top, x[i]);
+        return vla_fold_step<32>(top, VlaMax()) * unit;
+    }
+    __device__ __forceinline__ void move_to(float top) {
         if (__any(top > m + 8.f)) {                          // (m = -inf at first: any visible key)
             const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - to);
             l *= f;
@@ -260,34 +332,49 @@ template <typename T, int DP, int MODE> struct Rows {
                 for (int i = 0; i < 16; i++) o[b][i] *= f;
             m = to;
         }
+    }
+    __device__ __forceinline__ void weights(frag (&p)[2], const f32x16_t &x, float unit) {
         const float ref = m == -INFINITY ? 0.f : m;
-        frag p[2 * NB];
 #pragma unroll
-        for (int n = 0; n < NB; n++)
+        for (int i = 0; i < 16; i++) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, -ref));
+            l += w;
+            p[i / 8][i % 8] = (T)w;
+        }
+    }
+    __device__ __forceinline__ static frag value(const char *vt, int u, int b) {
+        const int lane = threadIdx.x & 63, col = lane & 31, hh = lane >> 5;
+        frag v;
+        if constexpr (sizeof(T) == 2) {
+            const int l16 = lane & 15, r = u * 16 + 4 * hh + (l16 >> 2);
+            const int c = (b * 4 + ((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1)) ^ TL::fv(l16 >> 2);
+            const char *at = vt + r * TL::ROW + c * 16 + (l16 & 1) * 8;
+            const auto v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)at), v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(at + 8 * TL::ROW));
+            v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 16; i++) {
-                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][i], unit, -ref));
-                l += w;
-                p[2 * n + i / 8][i % 8] = (T)w;
-            }
+            for (int e = 0; e < 8; e++)
+                v[e] = *(const float *)(vt + (u * 16 + 8 * (e / 4) + 4 * hh + e % 4) * TL::ROW + (b * 32 + col) * 4);
+        }
+        return v;
+    }
+    __device__ __forceinline__ void values(const frag (&p)[2], const char *vt) {
 #pragma unroll
-        for (int u = 0; u < 2 * NB; u++)
+        for (int u = 0; u < 2; u++)
 #pragma unroll
-            for (int b = 0; b < DB; b++) {
-                frag v;
-                if constexpr (sizeof(T) == 2) {
-                    const int l16 = lane & 15, r = u * 16 + 4 * hh + (l16 >> 2);
-                    const int c = (b * 4 + ((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1)) ^ TL::fv(l16 >> 2);
-                    const char *at = vt + r * TL::ROW + c * 16 + (l16 & 1) * 8;
-                    const auto v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)at), v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(at + 8 * TL::ROW));
-                    v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-                } else {
+            for (int b = 0; b < DB; b++) o[b] = mma(value(vt, u, b), p[u], o[b]);
+    }
+    // masked: some query may not see some key.
+    __device__ __forceinline__ void tile(const AttnArgs &a, const Query &y, const char *kt, const char *vt, int key0, bool masked) {
+        f32x16_t x;
+        frag p[2];
+        scores(x, kt);
 #pragma unroll
-                    for (int e = 0; e < 8; e++)
-                        v[e] = *(const float *)(vt + (u * 16 + 8 * (e / 4) + 4 * hh + e % 4) * TL::ROW + (b * 32 + col) * 4);
-                }
-                o[b] = mma(v, p[u], o[b]);
-            }
+        for (int i = 0; i < 16; i++) x[i] = shaped(x[i], a, y, key0, i);
+        if (masked) hide(x, y, key0);
+        move_to(largest(x, unit_of(a)));
+        weights(p, x, unit_of(a));
+        values(p, vt);
     }
 
     // A part's sums.
@@ -389,12 +476,16 @@ __device__ __forceinline__ Query find_query(const AttnArgs &a, const Item &it, i
 }
 
 __device__ __forceinline__ bool sees_all(const Query &y, int k0, int k1) { return (k1 <= y.hi && k0 >= y.lo) || k1 <= y.pre; }
-__device__ __forceinline__ bool sees_none(const Query &y, int k0, int k1) { return !y.valid || ((k0 >= y.hi || k1 <= y.lo) && k0 >= y.pre); }
 
+// Four waves of 32 packed rows each, all walking the same keys, 32 at a time.  K and V move through rings of RING tiles, K one tile before V: while
+// tile t's weights are formed on the vector units its successor's scores are on the matrix pipe, instruction by instruction in turn,
+// and while its values are summed the successor's largest is found.
+template <typename T, int DP> constexpr int RING = 32 * Tile<T, DP>::ROW * 6 <= 160 * 1024 ? 3 : 2;
 template <typename T, int DP, int MODE>
-__global__ void __launch_bounds__(256) paged_prompt_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_prompt_kernel(AttnArgs a) {
     typedef Tile<T, DP> TL;
-    constexpr int NB = sizeof(T) == 2 ? 2 : 1, KT = 32 * NB, BYTES = KT * TL::ROW, GROUPS = KT / 16;
+    typedef Rows<T, DP, MODE> R;
+    constexpr int KT = 32, BYTES = KT * TL::ROW, RG = RING<T, DP>, LOADS = 2 * 8 / TL::RPI;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const unsigned lds0 = (unsigned)(size_t)(lds_void *)lds;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -409,34 +500,76 @@ __global__ void __launch_bounds__(256) paged_prompt_kernel(AttnArgs a) {
     }
     const Query y = find_query<MODE>(a, it, it.first + wave * 32 + (threadIdx.x & 31), starts);
     if (a.whole) __syncthreads();
-    const int part = a.part0 + blockIdx.y, base = it.lo & ~(KT - 1), lo = max(it.lo, base + (int)blockIdx.y * a.chunk), hi = min(it.hi, base + ((int)blockIdx.y + 1) * a.chunk);
-    Rows<T, DP, MODE> rows;
+    const int part = a.part0 + blockIdx.y, base = it.lo & ~63, lo = max(it.lo, base + (int)blockIdx.y * a.chunk), hi = min(it.hi, base + ((int)blockIdx.y + 1) * a.chunk);
+    R rows;
     rows.start(a, y);
     if (lo < hi) {
         const int32_t *table = a.pv.table + (size_t)it.s * a.pv.table_stride;
         const int t0 = lo / KT, t1 = (hi + KT - 1) / KT;
         const Span sp{lo, hi, it.g0, it.g1};
-        auto page_of = [&](int t, int g) { return sp.page(table, a.pv.page_log, t * KT + g * 16); };
-        // a wave's share of a tile: 16 rows of K and the same of V, or (GROUPS = 2) of one of them
-        const int g = wave % GROUPS;
-        auto load = [&](int t, int page) {
-            const unsigned at = lds0 + (t & 1) * 2 * BYTES + g * 16 * TL::ROW;
-            if (GROUPS == 4 || wave < 2) TL::template load16<false>(at, a.pv.k, a.pv, page, it.kvh, t * KT + g * 16, sp);
-            if (GROUPS == 4 || wave >= 2) TL::template load16<true>(at + BYTES, a.pv.v, a.pv, page, it.kvh, t * KT + g * 16, sp);
+        // a wave's share of a tile: eight rows of K and of V
+        const int g = wave / 2, r0 = wave % 2 * 8;
+        const unsigned lds_k = lds0 + wave * 8 * TL::ROW, lds_v = lds_k + RG * BYTES;
+        typename TL::template Offsets<false, 8> off_k;
+        typename TL::template Offsets<true, 8> off_v;
+        off_k.start(a.pv, r0);
+        off_v.start(a.pv, r0);
+        const Place place(a.pv, it.kvh, sizeof(T));
+        // tiles that are read whole, and whose keys all of the wave's queries see: [in0, in1); [seen0, seen1) and [pre0, pre1)
+        const int in0 = (lo + KT - 1) / KT, in1 = it.g0 == it.g1 ? hi / KT : 0;
+        const int seen0 = (max(-wave_min(-y.lo), lo) + KT - 1) / KT, seen1 = min(wave_min(y.hi), hi) / KT;
+        const int pre1 = max(0, min(wave_min(y.valid ? y.pre : 0x7fffffff), hi)) / KT;
+        auto masked = [&](int t) { return !((t >= seen0 && t < seen1) || (t >= in0 && t < pre1)); };
+        auto page_of = [&](int t) { return sp.page(table, a.pv.page_log, t * KT + g * 16); };
+        auto whole = [&](int t, int page) { return t >= in0 && t < in1 && (unsigned)page < (unsigned)a.pv.n_pages; };
+        auto load_k = [&](int t, unsigned stage_at, int page) {
+            if (whole(t, page)) off_k.load(lds_k + stage_at, a.pv.k + place.at(a.pv, page, t * KT + g * 16));
+            else TL::template load<false, 8>(lds_k + stage_at, a.pv.k, a.pv, page, it.kvh, t * KT + g * 16, sp, r0);
         };
-        load(t0, page_of(t0, g));
-        int page = page_of(min(t0 + 1, t1 - 1), g);
-        for (int t = t0; t < t1; t++) {
-            // this tile has landed and everyone is through with the one before, whose place the next one takes
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if (t + 1 < t1) {
-                load(t + 1, page);
-                page = page_of(min(t + 2, t1 - 1), g);
+        auto load_v = [&](int t, unsigned stage_at, int page) {
+            if (whole(t, page)) off_v.load(lds_v + stage_at, a.pv.v + place.at(a.pv, page, t * KT + g * 16));
+            else TL::template load<true, 8>(lds_v + stage_at, a.pv.v, a.pv, page, it.kvh, t * KT + g * 16, sp, r0);
+        };
+        const float unit = R::unit_of(a);
+        // Tile t lies in stage (t - t0) % RG of either ring.  In order: K0 V0 K1 V1 K2 (two stages: K0 V0 K1), then one V and one K a step.
+#pragma unroll
+        for (int i = 0; i < RG; i++)
+            if (t0 + i < t1) {
+                const int page = page_of(t0 + i);
+                load_k(t0 + i, i * BYTES, page);
+                if (i < RG - 1) load_v(t0 + i, i * BYTES, page);
             }
-            const int k0 = t * KT;
-            if (__all(sees_none(y, k0, k0 + KT))) continue;
-            const char *kt = lds + (t & 1) * 2 * BYTES;
-            rows.template tile<NB>(a, y, kt, kt + BYTES, k0, !__all(sees_all(y, max(k0, lo), k0 + KT) && k0 + KT <= hi && k0 >= lo));
+        int page_v = page_of(t0 + RG - 1), page_k = page_of(t0 + RG);          // (clamped to pages that there are)
+        if (t0 + RG - 1 < t1) vm_wait<(RG - 1) * LOADS>();
+        else vm_wait<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        f32x16_t x, next;
+        rows.scores(x, lds);
+#pragma unroll
+        for (int i = 0; i < 16; i++) x[i] = R::shaped(x[i], a, y, t0 * KT, i);
+        if (masked(t0)) R::hide(x, y, t0 * KT);
+        float top = R::largest(x, unit);
+        unsigned stage = 0;                                          // where tile t's lies, in bytes
+        for (int t = t0; t < t1; t++) {
+            const unsigned after = stage == (RG - 1) * BYTES ? 0 : stage + BYTES, before = stage == 0 ? (RG - 1) * BYTES : stage - BYTES;
+            // K of t + 1 and V of t have landed, and everyone is through with K of t and V of t - 1, whose places are loaded again
+            if (RG == 3 && t + RG - 1 < t1) vm_wait<LOADS>();
+            else vm_wait<0>();
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (t + RG - 1 < t1) load_v(t + RG - 1, before, page_v);
+            if (t + RG < t1) load_k(t + RG, stage, page_k);
+            page_v = page_k;
+            page_k = page_of(t + 1 + RG);
+            typename R::frag p[2];
+            rows.move_to(top);
+            rows.scores_and_weights(next, lds + after, p, x, unit);
+            top = rows.values_and_largest(p, lds + RG * BYTES + stage, next, a, y, (t + 1) * KT);
+            if (masked(t + 1)) {                                 // (behind the last tile `next` is of no use to anyone)
+                R::hide(next, y, (t + 1) * KT);
+                top = R::largest(next, unit);
+            }
+            x = next;
+            stage = after;
         }
     }
     rows.finish(a, y, part);
@@ -541,12 +674,25 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(AttnArgs a) {
         sp = Span{ahead.it.lo, ahead.it.hi, ahead.it.g0, ahead.it.g1};
         pages();
     };
+    typename TL::template Offsets<false, 16> off_k;
+    typename TL::template Offsets<true, 16> off_v;
+    off_k.start(a.pv, 0);
+    off_v.start(a.pv, 0);
+    const Place place(a.pv, walk.kvh, sizeof(T));
     auto load = [&](int to) {
         const unsigned at = ring0 + to * STAGE;
-        TL::template load16<false>(at, a.pv.k, a.pv, p0, ahead.it.kvh, t * KT, sp);
-        TL::template load16<false>(at + 16 * TL::ROW, a.pv.k, a.pv, p1, ahead.it.kvh, t * KT + 16, sp);
-        TL::template load16<true>(at + BYTES, a.pv.v, a.pv, p0, ahead.it.kvh, t * KT, sp);
-        TL::template load16<true>(at + BYTES + 16 * TL::ROW, a.pv.v, a.pv, p1, ahead.it.kvh, t * KT + 16, sp);
+        if (t * KT >= sp.lo && (t + 1) * KT <= sp.hi && sp.g0 == sp.g1 && (unsigned)p0 < (unsigned)a.pv.n_pages && (unsigned)p1 < (unsigned)a.pv.n_pages) {
+            const size_t x = place.at(a.pv, p0, t * KT), z = place.at(a.pv, p1, t * KT + 16);
+            off_k.load(at, a.pv.k + x);
+            off_k.load(at + 16 * TL::ROW, a.pv.k + z);
+            off_v.load(at + BYTES, a.pv.v + x);
+            off_v.load(at + BYTES + 16 * TL::ROW, a.pv.v + z);
+        } else {
+        TL::template load<false, 16>(at, a.pv.k, a.pv, p0, ahead.it.kvh, t * KT, sp);
+        TL::template load<false, 16>(at + 16 * TL::ROW, a.pv.k, a.pv, p1, ahead.it.kvh, t * KT + 16, sp);
+        TL::template load<true, 16>(at + BYTES, a.pv.v, a.pv, p0, ahead.it.kvh, t * KT, sp);
+        TL::template load<true, 16>(at + BYTES + 16 * TL::ROW, a.pv.v, a.pv, p1, ahead.it.kvh, t * KT + 16, sp);
+        }
         if (++t < ahead.t1) pages();
         else { more = lead.next(a, &ahead); settle(); }
     };
@@ -568,7 +714,7 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(AttnArgs a) {
             else vm_wait<0>();
             const int k0 = u * KT;
             const char *kt = lds + stage * STAGE;
-            rows.template tile<1>(a, y, kt, kt + BYTES, k0, !__all(sees_all(y, k0, k0 + KT) && k0 + KT <= run.it.hi && k0 >= run.it.lo));
+            rows.tile(a, y, kt, kt + BYTES, k0, !__all(sees_all(y, k0, k0 + KT) && k0 + KT <= run.it.hi && k0 >= run.it.lo));
         }
         if (run.whole) rows.finish(a, y, 0);
         else {
@@ -701,7 +847,7 @@ Prompt plan_prompt(const AttnArgs &a, bool f32, bool whole) {
     p.parts = 1;
     p.chunk = 64;
     const double pairs = (double)a.pv.n_rows * a.n_heads;
-    const int per_cu = 4 * row * (f32 ? 32 : 64) <= 80 * 1024 ? 2 : 1;
+    const int per_cu = row <= 256 ? 2 : 1;
     double best = 0.0;
     for (long parts = 1; parts <= 256; parts++) {
         const long chunk = keys > 0 ? (((keys + parts - 1) / parts) + 63) / 64 * 64 : 64, n = keys > 0 ? (keys + chunk - 1) / chunk : 1;
@@ -763,7 +909,7 @@ size_t lay_out(AttnArgs *a, const Plan &p, char *base) {
 
 template <typename T, int DP, int MODE>
 int launch_prompt(AttnArgs a, const Prompt &p, bool whole, int part0, hipStream_t st) {
-    constexpr size_t bytes = 2 * 2 * (sizeof(T) == 2 ? 64 : 32) * Tile<T, DP>::ROW;
+    constexpr size_t bytes = 2 * RING<T, DP> * 32 * Tile<T, DP>::ROW > 8192 ? 2 * RING<T, DP> * 32 * Tile<T, DP>::ROW : 8192;
     if (int rc = vla_allow_lds((const void *)paged_prompt_kernel<T, DP, MODE>, bytes)) return rc;
     a.whole = whole; a.row_tiles = p.row_tiles; a.chunk = p.chunk; a.part0 = part0;
     paged_prompt_kernel<T, DP, MODE><<<dim3((unsigned)p.items, p.parts), 256, bytes, st>>>(a);
