@@ -68,8 +68,8 @@ __device__ __forceinline__ int wave_sum(int v) {
     return v;
 }
 
-// 16 bytes of zeros and more: what rows of pages that are not there are read from.
-__device__ __attribute__((aligned(16))) float zero_row[256];
+// What rows of pages that are not there are read from: 16 of the longest.
+__device__ __attribute__((aligned(16))) float zero_rows[16 * 256];
 
 __device__ __forceinline__ f32x16_t mma(const bf16x8_t &x, const bf16x8_t &y, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16_t mma(const f32x8_t &x, const f32x8_t &y, f32x16_t c) {
@@ -112,7 +112,7 @@ template <typename T, int DP> struct Tile {
     __device__ static void load(unsigned at, const char *pool, const PagedView &pv, int page, int kvh, int key0, const Span &sp, int r0 = 0) {
         const int lane = threadIdx.x & 63, row_bytes = pv.d * (int)sizeof(T), chunks = row_bytes >> 4;
         const bool ok = (unsigned)page < (unsigned)pv.n_pages;
-        const char *base = ok ? pool + (((size_t)page * pv.n_kv + kvh) << pv.page_log) * row_bytes : (const char *)zero_row;
+        const char *base = ok ? pool + (((size_t)page * pv.n_kv + kvh) << pv.page_log) * row_bytes : (const char *)zero_rows;
         const int in_page = ok ? (1 << pv.page_log) - 1 : 0;
 #pragma unroll
         for (int i = 0; i < ROWS / RPI; i++) {
@@ -123,7 +123,7 @@ template <typename T, int DP> struct Tile {
             dma16(at + i * 1024, (unsigned)((key & in_page) * row_bytes + c * 16), base);
         }
     }
-    // The same where all of the rows are read and their page is there: a lane's offsets do not change from tile to tile.
+    // The same where all of the rows are read: a lane's offsets do not change from tile to tile.
     template <bool V, int ROWS> struct Offsets {
         unsigned off[ROWS / RPI];
         __device__ __forceinline__ void start(const PagedView &pv, int r0) {
@@ -150,6 +150,9 @@ struct Place {
     }
     __device__ __forceinline__ size_t at(const PagedView &pv, int page, int key0) const {
         return (size_t)(unsigned)page * page_bytes + head_bytes + (key0 & ((1 << pv.page_log) - 1)) * row_bytes;
+    }
+    __device__ __forceinline__ const char *in(const PagedView &pv, const char *pool, int page, size_t at) const {
+        return (unsigned)page < (unsigned)pv.n_pages ? pool + at : (const char *)zero_rows;
     }
 };
 
@@ -521,13 +524,12 @@ __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_prom
         const int pre1 = max(0, min(wave_min(y.valid ? y.pre : 0x7fffffff), hi)) / KT;
         auto masked = [&](int t) { return !((t >= seen0 && t < seen1) || (t >= in0 && t < pre1)); };
         auto page_of = [&](int t) { return sp.page(table, a.pv.page_log, t * KT + g * 16); };
-        auto whole = [&](int t, int page) { return t >= in0 && t < in1 && (unsigned)page < (unsigned)a.pv.n_pages; };
         auto load_k = [&](int t, unsigned stage_at, int page) {
-            if (whole(t, page)) off_k.load(lds_k + stage_at, a.pv.k + place.at(a.pv, page, t * KT + g * 16));
+            if (t >= in0 && t < in1) off_k.load(lds_k + stage_at, place.in(a.pv, a.pv.k, page, place.at(a.pv, page, t * KT + g * 16)));
             else TL::template load<false, 8>(lds_k + stage_at, a.pv.k, a.pv, page, it.kvh, t * KT + g * 16, sp, r0);
         };
         auto load_v = [&](int t, unsigned stage_at, int page) {
-            if (whole(t, page)) off_v.load(lds_v + stage_at, a.pv.v + place.at(a.pv, page, t * KT + g * 16));
+            if (t >= in0 && t < in1) off_v.load(lds_v + stage_at, place.in(a.pv, a.pv.v, page, place.at(a.pv, page, t * KT + g * 16)));
             else TL::template load<true, 8>(lds_v + stage_at, a.pv.v, a.pv, page, it.kvh, t * KT + g * 16, sp, r0);
         };
         const float unit = R::unit_of(a);
@@ -550,27 +552,49 @@ __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_prom
         if (masked(t0)) R::hide(x, y, t0 * KT);
         float top = R::largest(x, unit);
         unsigned stage = 0;                                          // where tile t's lies, in bytes
-        for (int t = t0; t < t1; t++) {
+        int t = t0;
+        size_t at_v = 0;                                             // of the 16 keys whose V comes next
+        typename R::frag p[2];
+        // plain: everything is there to load, whole, and all see all of tile t + 1
+        auto step = [&](auto plain) {
+            constexpr bool PLAIN = decltype(plain)::value;
             const unsigned after = stage == (RG - 1) * BYTES ? 0 : stage + BYTES, before = stage == 0 ? (RG - 1) * BYTES : stage - BYTES;
             // K of t + 1 and V of t have landed, and everyone is through with K of t and V of t - 1, whose places are loaded again
-            if (RG == 3 && t + RG - 1 < t1) vm_wait<LOADS>();
+            if (RG == 3 && (PLAIN || t + RG - 1 < t1)) vm_wait<LOADS>();
             else vm_wait<0>();
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if (t + RG - 1 < t1) load_v(t + RG - 1, before, page_v);
-            if (t + RG < t1) load_k(t + RG, stage, page_k);
-            page_v = page_k;
-            page_k = page_of(t + 1 + RG);
-            typename R::frag p[2];
+            if constexpr (PLAIN) {
+                off_v.load(lds_v + before, place.in(a.pv, a.pv.v, page_v, at_v));
+                at_v = place.at(a.pv, page_k, (t + RG) * KT + g * 16);
+                off_k.load(lds_k + stage, place.in(a.pv, a.pv.k, page_k, at_v));
+                page_v = page_k;
+                page_k = paged_int(table, ((t + 1 + RG) * KT + g * 16) >> a.pv.page_log);
+            } else {
+                if (t + RG - 1 < t1) load_v(t + RG - 1, before, page_v);
+                if (t + RG < t1) load_k(t + RG, stage, page_k);
+                page_v = page_k;
+                page_k = page_of(t + 1 + RG);
+            }
             rows.move_to(top);
             rows.scores_and_weights(next, lds + after, p, x, unit);
             top = rows.values_and_largest(p, lds + RG * BYTES + stage, next, a, y, (t + 1) * KT);
-            if (masked(t + 1)) {                                 // (behind the last tile `next` is of no use to anyone)
+            if (!PLAIN && masked(t + 1)) {                           // (behind the last tile `next` is of no use to anyone)
                 R::hide(next, y, (t + 1) * KT);
                 top = R::largest(next, unit);
             }
             x = next;
             stage = after;
+            t++;
+        };
+        // plain steps: from `from` to before `upto`
+        const int from = max(max(in0, seen0), t0), upto = min(min(in1, t1) - RG - 1, seen1 - 1);
+        while (t < from && t < t1) step(std::integral_constant<bool, false>());
+        if (t < upto) {
+            at_v = place.at(a.pv, page_v, (t + RG - 1) * KT + g * 16);
+            do step(std::integral_constant<bool, true>());
+            while (t < upto);
         }
+        while (t < t1) step(std::integral_constant<bool, false>());
     }
     rows.finish(a, y, part);
 }
@@ -681,12 +705,12 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(AttnArgs a) {
     const Place place(a.pv, walk.kvh, sizeof(T));
     auto load = [&](int to) {
         const unsigned at = ring0 + to * STAGE;
-        if (t * KT >= sp.lo && (t + 1) * KT <= sp.hi && sp.g0 == sp.g1 && (unsigned)p0 < (unsigned)a.pv.n_pages && (unsigned)p1 < (unsigned)a.pv.n_pages) {
+        if (t * KT >= sp.lo && (t + 1) * KT <= sp.hi && sp.g0 == sp.g1) {
             const size_t x = place.at(a.pv, p0, t * KT), z = place.at(a.pv, p1, t * KT + 16);
-            off_k.load(at, a.pv.k + x);
-            off_k.load(at + 16 * TL::ROW, a.pv.k + z);
-            off_v.load(at + BYTES, a.pv.v + x);
-            off_v.load(at + BYTES + 16 * TL::ROW, a.pv.v + z);
+            off_k.load(at, place.in(a.pv, a.pv.k, p0, x));
+            off_k.load(at + 16 * TL::ROW, place.in(a.pv, a.pv.k, p1, z));
+            off_v.load(at + BYTES, place.in(a.pv, a.pv.v, p0, x));
+            off_v.load(at + BYTES + 16 * TL::ROW, place.in(a.pv, a.pv.v, p1, z));
         } else {
         TL::template load<false, 16>(at, a.pv.k, a.pv, p0, ahead.it.kvh, t * KT, sp);
         TL::template load<false, 16>(at + 16 * TL::ROW, a.pv.k, a.pv, p1, ahead.it.kvh, t * KT + 16, sp);
