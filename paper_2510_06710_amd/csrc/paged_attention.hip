@@ -483,7 +483,8 @@ __device__ __forceinline__ bool sees_all(const Query &y, int k0, int k1) { retur
 // Four waves of 32 packed rows each, all walking the same keys, 32 at a time.  K and V move through rings of RING tiles, K one tile before V: while
 // tile t's weights are formed on the vector units its successor's scores are on the matrix pipe, instruction by instruction in turn,
 // and while its values are summed the successor's largest is found.
-template <typename T, int DP> constexpr int RING = 32 * Tile<T, DP>::ROW * 6 <= 160 * 1024 ? 3 : 2;
+constexpr int LDS_STARTS = 2048;
+template <typename T, int DP> constexpr int RING = 32 * Tile<T, DP>::ROW * 8 <= 64 * 1024 ? 4 : 2;
 template <typename T, int DP, int MODE>
 __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_prompt_kernel(AttnArgs a) {
     typedef Tile<T, DP> TL;
@@ -494,53 +495,54 @@ __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_prom
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Item it;
     if (!find_item(a, blockIdx.x, 128, &it)) return;
-    // (the search of a row's sequence is a chain of loads, one per halving: from LDS where the sequences fit there)
+    const int part = a.part0 + blockIdx.y, base = it.lo & ~63, lo = max(it.lo, base + (int)blockIdx.y * a.chunk), hi = min(it.hi, base + ((int)blockIdx.y + 1) * a.chunk);
+    const int32_t *table = a.pv.table + (size_t)it.s * a.pv.table_stride;
+    const int t0 = lo / KT, t1 = lo < hi ? (hi + KT - 1) / KT : t0;
+    const Span sp{lo, hi, it.g0, it.g1};
+    // a wave's share of a tile: eight rows of K and of V
+    const int g = wave / 2, r0 = wave % 2 * 8;
+    const unsigned lds_k = lds0 + wave * 8 * TL::ROW, lds_v = lds_k + RG * BYTES;
+    typename TL::template Offsets<false, 8> off_k;
+    typename TL::template Offsets<true, 8> off_v;
+    off_k.start(a.pv, r0);
+    off_v.start(a.pv, r0);
+    const Place place(a.pv, it.kvh, sizeof(T));
+    const int in0 = (lo + KT - 1) / KT, in1 = it.g0 == it.g1 ? hi / KT : 0;          // tiles that are read whole: [in0, in1)
+    auto page_of = [&](int t) { return sp.page(table, a.pv.page_log, t * KT + g * 16); };
+    auto load_k = [&](int t, unsigned stage_at, int page) {
+        if (t >= in0 && t < in1) off_k.load(lds_k + stage_at, place.in(a.pv, a.pv.k, page, place.at(a.pv, page, t * KT + g * 16)));
+        else TL::template load<false, 8>(lds_k + stage_at, a.pv.k, a.pv, page, it.kvh, t * KT + g * 16, sp, r0);
+    };
+    auto load_v = [&](int t, unsigned stage_at, int page) {
+        if (t >= in0 && t < in1) off_v.load(lds_v + stage_at, place.in(a.pv, a.pv.v, page, place.at(a.pv, page, t * KT + g * 16)));
+        else TL::template load<true, 8>(lds_v + stage_at, a.pv.v, a.pv, page, it.kvh, t * KT + g * 16, sp, r0);
+    };
+    // Tile t lies in stage (t - t0) % RG of either ring.  In order: K0 V0 K1 V1 K2 V2 K3 (two stages: K0 V0 K1), then one V and one K a step.
+    // The first are on their way before the queries are looked for.
+#pragma unroll
+    for (int i = 0; i < RG; i++)
+        if (t0 + i < t1) {
+            const int page = page_of(t0 + i);
+            load_k(t0 + i, i * BYTES, page);
+            if (i < RG - 1) load_v(t0 + i, i * BYTES, page);
+        }
+    // (the search of a row's sequence is a chain of loads, one per halving: from LDS, behind the rings)
     const int32_t *starts = a.pv.row_start;
-    if (a.whole && a.pv.n_seq <= 2048) {
-        for (int i = threadIdx.x; i < a.pv.n_seq; i += 256) ((int32_t *)lds)[i] = starts[i];
+    if (a.whole && a.pv.n_seq <= LDS_STARTS) {
+        int32_t *copy = (int32_t *)(lds + 2 * RG * BYTES);
+        for (int i = threadIdx.x; i < a.pv.n_seq; i += 256) copy[i] = starts[i];
         __syncthreads();
-        starts = (const int32_t *)lds;
+        starts = copy;
     }
     const Query y = find_query<MODE>(a, it, it.first + wave * 32 + (threadIdx.x & 31), starts);
-    if (a.whole) __syncthreads();
-    const int part = a.part0 + blockIdx.y, base = it.lo & ~63, lo = max(it.lo, base + (int)blockIdx.y * a.chunk), hi = min(it.hi, base + ((int)blockIdx.y + 1) * a.chunk);
     R rows;
     rows.start(a, y);
     if (lo < hi) {
-        const int32_t *table = a.pv.table + (size_t)it.s * a.pv.table_stride;
-        const int t0 = lo / KT, t1 = (hi + KT - 1) / KT;
-        const Span sp{lo, hi, it.g0, it.g1};
-        // a wave's share of a tile: eight rows of K and of V
-        const int g = wave / 2, r0 = wave % 2 * 8;
-        const unsigned lds_k = lds0 + wave * 8 * TL::ROW, lds_v = lds_k + RG * BYTES;
-        typename TL::template Offsets<false, 8> off_k;
-        typename TL::template Offsets<true, 8> off_v;
-        off_k.start(a.pv, r0);
-        off_v.start(a.pv, r0);
-        const Place place(a.pv, it.kvh, sizeof(T));
-        // tiles that are read whole, and whose keys all of the wave's queries see: [in0, in1); [seen0, seen1) and [pre0, pre1)
-        const int in0 = (lo + KT - 1) / KT, in1 = it.g0 == it.g1 ? hi / KT : 0;
+        // tiles whose keys all of the wave's queries see: [seen0, seen1) and [in0, pre1)
         const int seen0 = (max(-wave_min(-y.lo), lo) + KT - 1) / KT, seen1 = min(wave_min(y.hi), hi) / KT;
         const int pre1 = max(0, min(wave_min(y.valid ? y.pre : 0x7fffffff), hi)) / KT;
         auto masked = [&](int t) { return !((t >= seen0 && t < seen1) || (t >= in0 && t < pre1)); };
-        auto page_of = [&](int t) { return sp.page(table, a.pv.page_log, t * KT + g * 16); };
-        auto load_k = [&](int t, unsigned stage_at, int page) {
-            if (t >= in0 && t < in1) off_k.load(lds_k + stage_at, place.in(a.pv, a.pv.k, page, place.at(a.pv, page, t * KT + g * 16)));
-            else TL::template load<false, 8>(lds_k + stage_at, a.pv.k, a.pv, page, it.kvh, t * KT + g * 16, sp, r0);
-        };
-        auto load_v = [&](int t, unsigned stage_at, int page) {
-            if (t >= in0 && t < in1) off_v.load(lds_v + stage_at, place.in(a.pv, a.pv.v, page, place.at(a.pv, page, t * KT + g * 16)));
-            else TL::template load<true, 8>(lds_v + stage_at, a.pv.v, a.pv, page, it.kvh, t * KT + g * 16, sp, r0);
-        };
         const float unit = R::unit_of(a);
-        // Tile t lies in stage (t - t0) % RG of either ring.  In order: K0 V0 K1 V1 K2 (two stages: K0 V0 K1), then one V and one K a step.
-#pragma unroll
-        for (int i = 0; i < RG; i++)
-            if (t0 + i < t1) {
-                const int page = page_of(t0 + i);
-                load_k(t0 + i, i * BYTES, page);
-                if (i < RG - 1) load_v(t0 + i, i * BYTES, page);
-            }
         int page_v = page_of(t0 + RG - 1), page_k = page_of(t0 + RG);          // (clamped to pages that there are)
         if (t0 + RG - 1 < t1) vm_wait<(RG - 1) * LOADS>();
         else vm_wait<0>();
@@ -551,50 +553,46 @@ __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_prom
         for (int i = 0; i < 16; i++) x[i] = R::shaped(x[i], a, y, t0 * KT, i);
         if (masked(t0)) R::hide(x, y, t0 * KT);
         float top = R::largest(x, unit);
-        unsigned stage = 0;                                          // where tile t's lies, in bytes
         int t = t0;
-        size_t at_v = 0;                                             // of the 16 keys whose V comes next
+        size_t at_v = place.at(a.pv, page_v, (t0 + RG - 1) * KT + g * 16);          // of the 16 keys whose V comes next
         typename R::frag p[2];
-        // plain: everything is there to load, whole, and all see all of tile t + 1
-        auto step = [&](auto plain) {
-            constexpr bool PLAIN = decltype(plain)::value;
-            const unsigned after = stage == (RG - 1) * BYTES ? 0 : stage + BYTES, before = stage == 0 ? (RG - 1) * BYTES : stage - BYTES;
+        // plain steps, from `from` to before `upto`: everything is there to load, whole, and all see all of tile t + 1
+        const int from = max(in0, seen0), upto = min(min(in1, t1) - RG - 1, seen1 - 1);
+        // The step of tile t, in the stage of that number (a constant: what lies where is known when this is compiled)
+        auto step = [&](int stage, f32x16_t &x, f32x16_t &next) __attribute__((always_inline)) {
+            const unsigned now = stage * BYTES, after = stage == RG - 1 ? 0 : now + BYTES, before = stage == 0 ? (RG - 1) * BYTES : now - BYTES;
+            const bool plain = t >= from && t < upto;
             // K of t + 1 and V of t have landed, and everyone is through with K of t and V of t - 1, whose places are loaded again
-            if (RG == 3 && (PLAIN || t + RG - 1 < t1)) vm_wait<LOADS>();
+            if (t + RG - 1 < t1) vm_wait<(RG - 2) * LOADS>();
             else vm_wait<0>();
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if constexpr (PLAIN) {
+            if (plain) {
                 off_v.load(lds_v + before, place.in(a.pv, a.pv.v, page_v, at_v));
                 at_v = place.at(a.pv, page_k, (t + RG) * KT + g * 16);
-                off_k.load(lds_k + stage, place.in(a.pv, a.pv.k, page_k, at_v));
+                off_k.load(lds_k + now, place.in(a.pv, a.pv.k, page_k, at_v));
                 page_v = page_k;
                 page_k = paged_int(table, ((t + 1 + RG) * KT + g * 16) >> a.pv.page_log);
             } else {
                 if (t + RG - 1 < t1) load_v(t + RG - 1, before, page_v);
-                if (t + RG < t1) load_k(t + RG, stage, page_k);
+                if (t + RG < t1) load_k(t + RG, now, page_k);
+                at_v = place.at(a.pv, page_k, (t + RG) * KT + g * 16);
                 page_v = page_k;
                 page_k = page_of(t + 1 + RG);
             }
             rows.move_to(top);
             rows.scores_and_weights(next, lds + after, p, x, unit);
-            top = rows.values_and_largest(p, lds + RG * BYTES + stage, next, a, y, (t + 1) * KT);
-            if (!PLAIN && masked(t + 1)) {                           // (behind the last tile `next` is of no use to anyone)
+            top = rows.values_and_largest(p, lds + RG * BYTES + now, next, a, y, (t + 1) * KT);
+            if (!plain && masked(t + 1)) {                           // (behind the last tile `next` is of no use to anyone)
                 R::hide(next, y, (t + 1) * KT);
                 top = R::largest(next, unit);
             }
-            x = next;
-            stage = after;
-            t++;
+            return ++t < t1;
         };
-        // plain steps: from `from` to before `upto`
-        const int from = max(max(in0, seen0), t0), upto = min(min(in1, t1) - RG - 1, seen1 - 1);
-        while (t < from && t < t1) step(std::integral_constant<bool, false>());
-        if (t < upto) {
-            at_v = place.at(a.pv, page_v, (t + RG - 1) * KT + g * 16);
-            do step(std::integral_constant<bool, true>());
-            while (t < upto);
+        for (;;) {
+            if (!step(0, x, next) || !step(1, next, x)) break;
+            if constexpr (RG == 4)
+                if (!step(2, x, next) || !step(3, next, x)) break;
         }
-        while (t < t1) step(std::integral_constant<bool, false>());
     }
     rows.finish(a, y, part);
 }
@@ -857,7 +855,8 @@ struct Plan {
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 // Tiles of 128 packed rows, their keys in parts by an estimate in cycles: rounds of workgroups, each a fixed time (its dependent loads, the first
-// tile, the writing out: 8 us) and its keys at the matrix and vector work of a tile; and the parts' sums, written and read again.
+// tile, the writing out: 8 us) and its keys at the matrix and vector work of a tile; and the parts' sums, written and read again, and the launch
+// that joins them (with a shared prefix there is one anyway).
 Prompt plan_prompt(const AttnArgs &a, bool f32, bool whole) {
     Prompt p{};
     const int row = padded_dim(a.pv.d) * (f32 ? 4 : 2);
@@ -877,7 +876,7 @@ Prompt plan_prompt(const AttnArgs &a, bool f32, bool whole) {
         const long chunk = keys > 0 ? (((keys + parts - 1) / parts) + 63) / 64 * 64 : 64, n = keys > 0 ? (keys + chunk - 1) / chunk : 1;
         if (n < parts) continue;
         const double rounds = (double)((p.items * n + 256 * per_cu - 1) / (256 * per_cu));
-        const double cost = rounds * (20e3 + chunk * 50.0 * per_cu * row / 256) + (n > 1 ? n * pairs * a.pv.d * 8.0 / 2000.0 : 0.0);
+        const double cost = rounds * (20e3 + chunk * 33.0 * per_cu * row / 256) + (n > 1 ? n * pairs * a.pv.d * 8.0 / 2000.0 + (whole ? 0.0 : 12e3) : 0.0);
         if (best == 0.0 || cost < best) { best = cost; p.chunk = (int)chunk; p.parts = (int)n; }
     }
     return p;
@@ -933,8 +932,8 @@ size_t lay_out(AttnArgs *a, const Plan &p, char *base) {
 
 template <typename T, int DP, int MODE>
 int launch_prompt(AttnArgs a, const Prompt &p, bool whole, int part0, hipStream_t st) {
-    constexpr size_t bytes = 2 * RING<T, DP> * 32 * Tile<T, DP>::ROW > 8192 ? 2 * RING<T, DP> * 32 * Tile<T, DP>::ROW : 8192;
-    if (int rc = vla_allow_lds((const void *)paged_prompt_kernel<T, DP, MODE>, bytes)) return rc;
+    const size_t bytes = 2 * RING<T, DP> * 32 * Tile<T, DP>::ROW + (whole && a.pv.n_seq <= LDS_STARTS ? a.pv.n_seq * sizeof(int32_t) : 0);
+    if (int rc = vla_allow_lds((const void *)paged_prompt_kernel<T, DP, MODE>, 2 * RING<T, DP> * 32 * Tile<T, DP>::ROW + LDS_STARTS * sizeof(int32_t))) return rc;
     a.whole = whole; a.row_tiles = p.row_tiles; a.chunk = p.chunk; a.part0 = part0;
     paged_prompt_kernel<T, DP, MODE><<<dim3((unsigned)p.items, p.parts), 256, bytes, st>>>(a);
     return vla_check_launch("paged_attention");

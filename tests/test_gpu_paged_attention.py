@@ -70,7 +70,7 @@ def run(b, dtype, heads, kv, d, cap=0.0, bias=False, prefix=None, window=0, shar
     assert (np.abs(got - o) <= tol).all(), (np.abs(got - o) - tol).max()
     blind = np.isinf(l)
     assert (got_l[blind] == -np.inf).all() and (got[blind] == 0).all()
-    assert (np.abs(got_l - l)[~blind] <= (ds + bound * 2.0 ** -24 + np.abs(l) * 2.0 ** -22)[~blind]).all()
+    assert (np.abs(got_l[~blind] - l[~blind]) <= (ds + bound * 2.0 ** -24 + np.abs(l) * 2.0 ** -22)[~blind]).all()
 
 
 BOTH = pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -123,6 +123,14 @@ def test_long_context_is_split(dtype, rows):
 @BOTH
 def test_chunk_behind_a_long_context(dtype):
     run(Batch([(70, 2500), (9, 40)], 64), dtype, 4, 2, 64)
+
+
+@BOTH
+@pytest.mark.parametrize("heads,kv,d", [(8, 8, 64), (4, 4, 128), (2, 2, 256)])
+def test_many_whole_tiles(dtype, heads, kv, d):
+    spec = [(130, 1030), (1, 1500), (129, 1129), (140, 1400)]                      # key ranges of dozens of tiles that every row sees
+    run(Batch(spec, 16), dtype, heads, kv, d)
+    run(Batch(spec, 64), dtype, heads, kv, d, window=900)
 
 
 @BOTH
