@@ -348,7 +348,7 @@ int vla_policy_objective_noalloc(const float *logp_new, const float *logp_old, c
  * vla_sample_logits: one token per row of logits (DEVICE dtype [n, vocab], row stride in elements), vocab at most 262,144.
  *   With T = temperature[i] and w_k = exp((z_k - max z) / T):  of the tokens the top_k[i] largest are kept (ties: lowest id first;
  *   <= 0: all), of these the shortest leading run, largest first, that holds top_p[i] of their mass (>= 1: all), of these those
- *   with w_k >= min_p[i].  token[i] = the lowest id at which the kept tokens' running mass, in id order, exceeds u[i] times its
+ *   with w_k >= min_p[i] (above 1: 1).  token[i] = the lowest id at which the kept tokens' running mass, in id order, exceeds u[i] times its
  *   total; u in [0, 1).  T <= 0, or u NULL: the largest (lowest id).  The largest is always kept; NaN and -inf never are; where +inf occurs only
  *   those are, at equal weights.  A row without any gets token -1, n_kept 0 and log-probabilities -inf.
  *   temperature, top_p, min_p, u: DEVICE fp32 [n]; top_k DEVICE int32 [n]; each may be NULL (1, all, all, greedy, all).

@@ -5,16 +5,20 @@
 // number.  Masses are w = exp((z - max) / T) in fp64, rounded to multiples of 2^-44 and summed as whole numbers: the sums are exact,
 // in any order, and the border cases of top-p and of u fall alike every time (2^18 tokens of mass 1 stay below 2^63).
 //
-// One workgroup a row.  Up to LIST tokens (the whole row, or what a count over bins of the value leaves for top-k) are sorted in
-// LDS; the cuts are then places in a running sum.  Longer rows with top-p alone: masses over bins of 1/32 in log2 units find the
-// bin in which the cut falls, and the tokens of that bin are sorted.  The row is read again from the caches for each step:
-// its maximum; the bins; the tokens of the border bin and the kept mass of every 2048 ids; and the 2048 ids in which u falls.
+// One workgroup a row.  A row of up to SHORT tokens is sorted whole in LDS; the cuts are then places in a running sum.  Longer rows: with
+// top-k, a count over bins of 1/32 in log2 units finds the bin of the k-th token, and the list is all tokens down to that bin.  With top-p
+// alone, masses over the same bins find the bin in which the cut falls, and the list is that bin's tokens.  The row is read again from the
+// caches for each step: its maximum; the bins; the list and the kept mass of every segment of ids; and the segment in which u falls.
+//
+// 256 rows of 128,000 fp32 logits, every setting in turn: 112 us (read once at the rate of a large copy: 27).  Of a row with top-p alone 18 us
+// are the maximum, at the rate of the memory; 31 the bins and 40 the list and segments, both bound by the issue of the vector ALU, where fp64
+// instructions of the masses are most; 14 the sort and the choice.  Small rows are bound by the steps behind each other: 256 of 256 bins 9.5 us.
 #include "vla_internal.h"
 
 namespace {
 
 constexpr double UNIT = 17592186044416.0;      // 2^44
-constexpr int LIST = 4096, BINS = 2048, SEGMENT = 2048, MAX_VOCAB = 262144;
+constexpr int LIST = 4096, SHORT = 512, BINS = 2048, SEGMENTS = 512;
 typedef unsigned long long u64;
 
 struct SampleArgs {
@@ -40,22 +44,26 @@ __device__ __forceinline__ u64 rank_key(unsigned order, int id) { return (u64)or
 __device__ __forceinline__ int id_of(u64 key) { return (int)~(unsigned)key; }
 __device__ __forceinline__ float value_at(u64 key) { return value_of((unsigned)(key >> 32)); }
 
-__device__ __forceinline__ u64 wave_sum(u64 v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+// Over the 64 lanes by lane moves of the vector ALU (through LDS a step of a 64-bit value takes some 150 cycles): running sums of rows of 16
+// lanes, then of 32 and 64.
+template <int CTRL, int ROWS> __device__ __forceinline__ u64 moved(u64 v) {
+    const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)v, CTRL, ROWS, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(v >> 32), CTRL, ROWS, 0xf, false);
+    return (u64)hi << 32 | lo;
 }
-__device__ __forceinline__ u64 wave_max(u64 v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) { const u64 w = __shfl_xor(v, o, 64); v = w > v ? w : v; }
-    return v;
+template <typename F> __device__ __forceinline__ u64 wave_run(u64 v, F f) {
+    v = f(v, moved<0x111, 0xf>(v));          // row_shr 1, 2, 4, 8
+    v = f(v, moved<0x112, 0xf>(v));
+    v = f(v, moved<0x114, 0xf>(v));
+    v = f(v, moved<0x118, 0xf>(v));
+    v = f(v, moved<0x142, 0xa>(v));          // row_bcast 15, 31
+    return f(v, moved<0x143, 0xc>(v));
 }
-__device__ __forceinline__ u64 wave_scan(u64 v) {            // inclusive
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const u64 w = __shfl_up(v, o, 64); if (lane >= o) v += w; }
-    return v;
+__device__ __forceinline__ u64 last_lane(u64 v) {
+    return (u64)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(v >> 32), 63) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)v, 63);
 }
+__device__ __forceinline__ u64 wave_scan(u64 v) { return wave_run(v, [](u64 a, u64 b) { return a + b; }); }
+__device__ __forceinline__ u64 wave_sum(u64 v) { return last_lane(wave_scan(v)); }
+__device__ __forceinline__ u64 wave_max(u64 v) { return last_lane(wave_run(v, [](u64 a, u64 b) { return a > b ? a : b; })); }
 
 // 2^y for y <= 0, relative error below 1e-14: 2^f by its series in f ln 2 (|f ln 2| <= 0.347), the last term left out 6e-15.
 __device__ __forceinline__ double exp2_neg(double y) {
@@ -77,27 +85,38 @@ __device__ __forceinline__ double exp2_neg(double y) {
 // w in [0, 1] to multiples of 2^-44: added to 2^52 its rounded multiple stands in the low bits.
 __device__ __forceinline__ u64 units_of(double w) { return __builtin_bit_cast(u64, __builtin_fma(w, UNIT, 4503599627370496.0)) & 0xfffffffffffffull; }
 
-// A row's masses: w = 2^y, y = (z - max) rate.  2^y = 2^e table[j] 2^r with y = e + j / 256 + r, |r| <= 1/512: table[j] = 2^(j/256), and four
-// terms of the series of 2^r, the next of which is below 1.4e-13.  (Without a table eleven terms: 75 of 180 us were fp64 instructions.)
-constexpr int TABLE = 256;
+// A row's masses: w = 2^y, y = (z - max) rate.  2^y = 2^e table[j] 2^r with y = e + j / 32 + r, |r| <= 1/64: table[j] = 2^(j/32), and five
+// terms of the series of 2^r, the next of which is below 1.3e-12.  Without a table eleven terms (256 rows of 128,000 logits: 75 of 180 us were
+// fp64 instructions); 32 entries are one for each pair of LDS banks, so that no lookup waits for another (256 entries and a term less were 121 us with top-p, 107 so).
+constexpr int TABLE = 32;
 struct Scale {
-    double zmax, rate;
+    double zmax, rate;       // (of table steps: 32 log2 e / T)
     const double *table;
-    __device__ __forceinline__ double power(float z) const { return ((double)z - zmax) * rate; }
-    __device__ __forceinline__ double weight_of(double y) const {
-        const double v = fmax(y, -4096.0) * (double)TABLE, n = __builtin_rint(v), x = (v - n) * (0.69314718055994530942 / TABLE);
-        const int k = (int)n;
-        const double p = __builtin_fma(__builtin_fma(__builtin_fma(x, 1.0 / 6.0, 0.5), x, 1.0), x, 1.0);
-        return __builtin_ldexp(p * table[k & (TABLE - 1)], k >> 8);
+    // Steps below the largest, and the whole number of them.  Added to 1.5 2^52 a number is rounded to a whole one, which stands in the low bits
+    // (fp64 conversions and ldexp run at a quarter of the rate).
+    struct Steps { double v, n; int k; };
+    __device__ __forceinline__ Steps steps(float z) const {
+        constexpr double MAGIC = 6755399441055744.0;
+        Steps s;
+        s.v = fmax(((double)z - zmax) * rate, -32000.0);          // (NaN and -inf too: a weight of 2^-1000)
+        const double m = s.v + MAGIC;
+        s.k = (int)(unsigned)__builtin_bit_cast(u64, m);
+        s.n = m - MAGIC;
+        return s;
     }
-    __device__ __forceinline__ double weight(float z) const { return weight_of(power(z)); }
+    __device__ __forceinline__ double weight_of(const Steps &s) const {
+        constexpr double C = 0.69314718055994530942 / TABLE, C2 = C * C / 2.0, C3 = C2 * C / 3.0, C4 = C3 * C / 4.0;
+        const double r = s.v - s.n;
+        const u64 p = __builtin_bit_cast(u64, __builtin_fma(__builtin_fma(__builtin_fma(__builtin_fma(r, C4, C3), r, C2), r, C), r, 1.0) * table[s.k & (TABLE - 1)]);
+        return __builtin_bit_cast(double, (u64)((unsigned)(p >> 32) + ((unsigned)(s.k >> 5) << 20)) << 32 | (unsigned)p);      // times 2^(k / 32)
+    }
+    __device__ __forceinline__ double weight(float z) const { return weight_of(steps(z)); }
     __device__ __forceinline__ u64 units(float z) const { return units_of(weight(z)); }
-    // bins of 1/32 in log2 units, never descending in -z; below 2^-63 all one
-    __device__ __forceinline__ int bin_of(double y) const { return (int)fmin(y * -32.0, (double)(BINS - 1)); }
+    // one bin per step, never descending in -z; below 2^-63 all one
+    __device__ __forceinline__ int bin_of(const Steps &s) const { return min(-s.k, BINS - 1); }
     // w to within 1e-7, where only the logarithm of many of them is wanted
-    __device__ __forceinline__ float rough(double y) const {
-        const double v = fmax(y, -200.0), n = __builtin_rint(v);
-        return __builtin_ldexpf(__builtin_amdgcn_exp2f((float)(v - n)), (int)n);
+    __device__ __forceinline__ float rough(const Steps &s) const {
+        return __builtin_ldexpf(__builtin_amdgcn_exp2f((float)(s.v - s.n) * (1.f / TABLE) + (float)(s.k & (TABLE - 1)) * (1.f / TABLE)), max(s.k >> 5, -200));
     }
 };
 __device__ __forceinline__ void fill_table(double *table) {
@@ -137,7 +156,7 @@ template <int THREADS> struct Block {
 template <int THREADS> struct Room {
     u64 keys[LIST];              // the list, sorted: largest key first; zeros behind it
     union { u64 mass[BINS]; unsigned count[BINS]; u64 bucket[BINS]; };
-    u64 segment[MAX_VOCAB / SEGMENT];
+    u64 segment[SEGMENTS];
     double table[TABLE];
     Block<THREADS> block;
     int n;                       // tokens that asked for a place in the list
@@ -147,8 +166,32 @@ template <int THREADS> struct Room {
 
 // keys[0 .. P), P a power of two, from the largest to the smallest.  Pairs of a distance up to 64 lie in the 128 keys of one wave's
 // threads, whose LDS accesses take place in order: only longer distances need the workgroup's barrier.
+// Up to 256 keys: each thread counts how many are larger than its own (a microsecond; in steps three).
 template <int THREADS> __device__ void sort_keys(u64 *keys, int P) {
+    const int t = threadIdx.x;
     __syncthreads();
+    if (P <= 256) {
+        typedef u64 u64x2 __attribute__((ext_vector_type(2)));
+        u64 mine = 0;
+        int place = 0;
+        if (t < P) {
+            mine = keys[t];
+            if (!mine) keys[t] = P - t;                      // (below every key, and no two alike)
+        }
+        __syncthreads();
+        if (t < P) {
+            const u64 key = keys[t];
+#pragma unroll 8
+            for (int i = 0; i < P; i += 2) {
+                const u64x2 k = *(const u64x2 *)(keys + i);
+                place += (k[0] > key) + (k[1] > key);
+            }
+        }
+        __syncthreads();
+        if (t < P) keys[place] = mine;
+        __syncthreads();
+        return;
+    }
     for (int k = 2; k <= P; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
             if (j >= 128 && j == k >> 1) __syncthreads();
@@ -163,29 +206,54 @@ template <int THREADS> __device__ void sort_keys(u64 *keys, int P) {
     __syncthreads();
 }
 
-// Tokens of ids [segment * SEGMENT, ...) to f, by one wave: 16 bytes a load, all of the segment's asked for before the first is used.
-template <typename T, typename F> __device__ __forceinline__ void each_of_segment(const T *z, int V, int segment, F f) {
-    constexpr int W = 16 / (int)sizeof(T), STEPS = SEGMENT / (64 * W);
+// A segment's tokens, SEGMENT ids, in the registers of a wave: 16 bytes a load.
+template <int SEGMENT, typename T> struct Segment {
+    static constexpr int W = SEGMENT / 64 < 16 / (int)sizeof(T) ? SEGMENT / 64 : 16 / (int)sizeof(T), STEPS = SEGMENT / (64 * W);
     typedef T tw __attribute__((ext_vector_type(W), aligned(sizeof(T))));
-    const int i0 = segment * SEGMENT + (threadIdx.x & 63) * W;
-    if (segment * SEGMENT + SEGMENT <= V) {
-        tw v[STEPS];
+    typedef const __attribute__((address_space(1))) tw *global;          // (not a flat load, which waits with LDS)
+    typedef const __attribute__((address_space(1))) T *global_one;
+    tw v[STEPS];
+    __device__ __forceinline__ void load(const T *z, int V, int segment) {
+        const int i0 = segment * SEGMENT + (threadIdx.x & 63) * W;
+        if (segment * SEGMENT + SEGMENT <= V) {
 #pragma unroll
-        for (int s = 0; s < STEPS; s++) v[s] = *(const tw *)(z + i0 + s * 64 * W);
+            for (int s = 0; s < STEPS; s++) v[s] = *(global)(z + i0 + s * 64 * W);
+        } else
+#pragma unroll
+            for (int s = 0; s < STEPS; s++)
+#pragma unroll
+                for (int e = 0; e < W; e++) v[s][e] = i0 + s * 64 * W + e < V ? ((global_one)z)[i0 + s * 64 * W + e] : (T)-INFINITY;
+    }
+    // f(value, number) of the lane's tokens; id_at: a number's id
+    template <typename F> __device__ __forceinline__ void each(F f) const {
 #pragma unroll
         for (int s = 0; s < STEPS; s++)
 #pragma unroll
-            for (int e = 0; e < W; e++) f((float)v[s][e], i0 + s * 64 * W + e);
-    } else
-        for (int s = 0; s < STEPS; s++)
-#pragma unroll
-            for (int e = 0; e < W; e++) {
-                const int i = i0 + s * 64 * W + e;
-                if (i < V) f((float)z[i], i);
-            }
+            for (int e = 0; e < W; e++) f((float)v[s][e], s * W + e);
+    }
+    __device__ static int id_at(int segment, int n) { return segment * SEGMENT + (threadIdx.x & 63) * W + n / W * 64 * W + n % W; }
+};
+// All tokens of the row (and -inf for ids behind it) to f(value, number, segment), a wave's segment after segment, the next one on its way meanwhile; end(segment) behind each.
+template <int THREADS, int SEGMENT, typename T, typename F, typename E> __device__ __forceinline__ void each_token(const T *z, int V, F f, E end) {
+    constexpr int WAVES = THREADS / 64;
+    const int n = (V + SEGMENT - 1) / SEGMENT;
+    int s = threadIdx.x >> 6;
+    if (s >= n) return;
+    Segment<SEGMENT, T> a, b;
+    a.load(z, V, s);
+    for (;;) {
+        if (s + WAVES < n) b.load(z, V, s + WAVES);
+        a.each([&](float v, int n) { f(v, n, s); });
+        end(s);
+        if ((s += WAVES) >= n) return;
+        if (s + WAVES < n) a.load(z, V, s + WAVES);
+        b.each([&](float v, int n) { f(v, n, s); });
+        end(s);
+        if ((s += WAVES) >= n) return;
+    }
 }
-template <int THREADS, typename T, typename F> __device__ __forceinline__ void each_token(const T *z, int V, F f) {
-    for (int s = threadIdx.x >> 6; s * SEGMENT < V; s += THREADS / 64) each_of_segment(z, V, s, f);
+template <int THREADS, int SEGMENT, typename T, typename F> __device__ __forceinline__ void each_token(const T *z, int V, F f) {
+    each_token<THREADS, SEGMENT>(z, V, f, [](int) {});
 }
 
 // Whether a token of mass w, with `run` before it in id order, is the one: the first whose sum exceeds `want`; the last with mass
@@ -205,7 +273,7 @@ template <int THREADS, typename T> __device__ void sample_by_bisection(const Sam
     const float T0 = a.temperature ? a.temperature[row] : 1.f;
     const bool infinite = zmax == INFINITY;
     const bool greedy = !(T0 > 0.f) || !a.u;
-    const Scale sc{infinite ? 0.0 : (double)zmax, 1.4426950408889634074 / (T0 > 0.f ? (double)T0 : 1.0), room.table};
+    const Scale sc{infinite ? 0.0 : (double)zmax, 1.4426950408889634074 * TABLE / (T0 > 0.f ? (double)T0 : 1.0), room.table};
     auto weight = [&](float v) { return infinite ? (v == INFINITY ? 1.0 : 0.0) : sc.weight(v); };
     auto units = [&](float v) { return units_of(weight(v)); };
     // count and mass of what lies at or above a threshold
@@ -242,12 +310,12 @@ template <int THREADS, typename T> __device__ void sample_by_bisection(const Sam
         const u64 c = bisect([&](Both b) { return (double)b.mass >= want; });
         cut = c > cut ? c : cut;
     }
-    const float least = a.min_p ? a.min_p[row] : 0.f;
+    const float least = fminf(a.min_p ? a.min_p[row] : 0.f, 1.f);
     auto kept = [&](float v, int i) {
         const unsigned o = order_of(v);
         if (!o) return false;
         const u64 key = rank_key(o, i);
-        return key == first || (key >= cut && weight(v) >= (double)least);
+        return key >= cut && weight(v) >= (double)least;
     };
     // ids in runs of consecutive ones per thread: running masses in id order
     const int per = (V + THREADS - 1) / THREADS, i0 = t * per, i1 = min(V, i0 + per);
@@ -281,7 +349,7 @@ template <int THREADS, typename T> __device__ void sample_by_bisection(const Sam
     }
     if (t == 0) {
         const float v = (float)z[token];
-        const double y = infinite ? 0.0 : ((double)v - sc.zmax) * sc.rate * 0.69314718055994530942;
+        const double y = infinite ? 0.0 : ((double)v - sc.zmax) * sc.rate * (0.69314718055994530942 / TABLE);
         a.token[row] = token;
         if (a.logp) a.logp[row] = (float)(y - log((double)all.mass / UNIT));
         if (a.logp_kept) a.logp_kept[row] = (float)(y - log((double)total.mass / UNIT));
@@ -290,17 +358,21 @@ template <int THREADS, typename T> __device__ void sample_by_bisection(const Sam
 }
 
 
-template <int THREADS, typename T> __global__ void __launch_bounds__(THREADS) sample_rows_kernel(SampleArgs a) {
+template <int THREADS, int SEGMENT, typename T> __global__ void __launch_bounds__(THREADS) sample_rows_kernel(SampleArgs a) {
     __shared__ Room<THREADS> room;
     Block<THREADS> &block = room.block;
     const int row = blockIdx.x, t = threadIdx.x, V = a.vocab;
     const T *z = (const T *)a.logits + row * a.stride;
-    const bool whole = THREADS < 1024 || V <= LIST;          // the row itself is the list
+    typedef Segment<SEGMENT, T> Seg;
+    constexpr bool whole = THREADS < 1024;          // the row itself is the list
+    // (asked for together with the row: each alone is a memory latency)
+    const float T0 = a.temperature ? a.temperature[row] : 1.f, p = a.top_p ? a.top_p[row] : 1.f, least = fminf(a.min_p ? a.min_p[row] : 0.f, 1.f), u = a.u ? a.u[row] : 0.f;
+    int k = a.top_k ? a.top_k[row] : 0;
     fill_table(room.table);                // (there for all once the largest is known)
     // ---- the largest, and how many there are
     Both top{0, 0};
     int P = 2;                             // places of the list, a power of two
-    if (whole) {
+    if constexpr (whole) {
         while (P < V) P <<= 1;
         for (int i = t; i < P; i += THREADS) {
             const unsigned o = i < V ? order_of((float)z[i]) : 0u;
@@ -311,13 +383,14 @@ template <int THREADS, typename T> __global__ void __launch_bounds__(THREADS) sa
         }
     } else {
         float best = -INFINITY;
-        int at = 0;
-        each_token<THREADS>(z, V, [&](float v, int i) {
-            if (v > best) { best = v; at = i; }              // (a lane's ids ascend: the lowest of equals stays)
-            top.mass += v > -INFINITY;
+        int at = 0, in = 0, is = 0;
+        each_token<THREADS, SEGMENT>(z, V, [&](float v, int n, int s) {
+            if (v > best) { best = v; at = n; in = s; }      // (a lane's ids ascend: the lowest of equals stays)
+            is += v > -INFINITY;
         });
         const unsigned o = order_of(best);
-        top.count = o ? rank_key(o, at) : 0;
+        top.count = o ? rank_key(o, Seg::id_at(in, at)) : 0;
+        top.mass = is;
     }
     top = block.both(top, true);
     const u64 first = top.count;
@@ -331,13 +404,11 @@ template <int THREADS, typename T> __global__ void __launch_bounds__(THREADS) sa
         }
         return;
     }
-    const float zmax = value_at(first), T0 = a.temperature ? a.temperature[row] : 1.f;
+    const float zmax = value_at(first);
     if (zmax == INFINITY) { sample_by_bisection<THREADS>(a, z, row, first, room); return; }
     const bool greedy = !(T0 > 0.f) || !a.u;
-    const Scale sc{(double)zmax, 1.4426950408889634074 / (T0 > 0.f ? (double)T0 : 1.0), room.table};
-    int k = a.top_k ? a.top_k[row] : 0;
+    const Scale sc{(double)zmax, 1.4426950408889634074 * TABLE / (T0 > 0.f ? (double)T0 : 1.0), room.table};
     if (k <= 0 || k >= valid) k = valid;
-    const float p = a.top_p ? a.top_p[row] : 1.f, least = a.min_p ? a.min_p[row] : 0.f;
     const bool cut_k = k < valid, cut_p = p < 1.f;
     const double share = p > 0.f ? (double)p : 0.0;
     const bool ranked = whole || cut_k;    // the list holds all leading tokens (else: those of the bin in which the cut of top-p falls)
@@ -345,7 +416,7 @@ template <int THREADS, typename T> __global__ void __launch_bounds__(THREADS) sa
     u64 all_mass = 0, kept_mass = 0, above = 0;      // of the row; of the kept tokens; of the bins before the border
     int n_kept = 0, border = BINS;
     double limit = 0.0;                              // mass before a token at which top-p ends
-    if (!whole) {
+    if constexpr (!whole) {
         // ---- bins: where the cut falls
         if (cut_k || cut_p) {
             for (int i = t; i < BINS; i += THREADS) room.mass[i] = 0;
@@ -353,17 +424,15 @@ template <int THREADS, typename T> __global__ void __launch_bounds__(THREADS) sa
             if (cut_k) {
                 // (of the row's mass only logp wants the logarithm: in fp64 sums of fp32 exponentials, in one order)
                 double all = 0.0;
-                each_token<THREADS>(z, V, [&](float v, int) {
-                    if (!(v > -INFINITY)) return;
-                    const double y = sc.power(v);
+                each_token<THREADS, SEGMENT>(z, V, [&](float v, int, int) {
+                    const auto y = sc.steps(v);
                     all += (double)sc.rough(y);
-                    atomicAdd(&room.count[sc.bin_of(y)], 1u);
+                    atomicAdd(&room.count[sc.bin_of(y)], v > -INFINITY ? 1u : 0u);
                 });
                 all_mass = block.both(Both{0, (u64)(all * UNIT)}).mass;
             } else
-                each_token<THREADS>(z, V, [&](float v, int) {
-                    if (!(v > -INFINITY)) return;
-                    const double y = sc.power(v);
+                each_token<THREADS, SEGMENT>(z, V, [&](float v, int, int) {
+                    const auto y = sc.steps(v);
                     atomicAdd(&room.mass[sc.bin_of(y)], units_of(sc.weight_of(y)));
                 });
             __syncthreads();
@@ -389,34 +458,38 @@ template <int THREADS, typename T> __global__ void __launch_bounds__(THREADS) sa
         // ---- the list; without top-k also the mass of the other kept tokens, by segment
         if (t == 0) room.n = 0;
         __syncthreads();
-        auto enlist = [&](float v, int i) {
-            const int at = atomicAdd(&room.n, 1);
-            if (at < LIST) room.keys[at] = rank_key(order_of(v), i);
+        auto enlist = [&](int segment, unsigned &listed) {
+            for (; listed; listed &= listed - 1) {
+                const int i = Seg::id_at(segment, __builtin_ctz(listed)), at = atomicAdd(&room.n, 1);
+                if (at < LIST) room.keys[at] = rank_key(order_of((float)z[i]), i);
+            }
         };
         if (cut_k) {
-            each_token<THREADS>(z, V, [&](float v, int i) {
-                if (v > -INFINITY && sc.bin_of(sc.power(v)) <= border) enlist(v, i);
-            });
+            unsigned listed = 0;                     // of a segment's numbers
+            each_token<THREADS, SEGMENT>(z, V, [&](float v, int n, int) {
+                listed |= (unsigned)(v > -INFINITY && sc.bin_of(sc.steps(v)) <= border) << n;
+            }, [&](int s) { enlist(s, listed); });
         } else {
-            u64 rest = 0;                            // not kept for min-p alone
-            for (int s = t >> 6; s * SEGMENT < V; s += THREADS / 64) {
-                u64 m = 0;
-                each_of_segment(z, V, s, [&](float v, int i) {
-                    if (!(v > -INFINITY)) return;
-                    const double y = sc.power(v);
-                    if (cut_p) {
-                        const int b = sc.bin_of(y);
-                        if (b == border) enlist(v, i);
-                        if (b >= border) return;
-                    }
-                    const double w = sc.weight_of(y);
-                    if (w >= (double)least || (v == zmax && i == id_of(first))) { m += units_of(w); n_kept++; }
-                    else rest += units_of(w);
-                });
+            u64 m = 0, all = 0;
+            unsigned listed = 0;
+            each_token<THREADS, SEGMENT>(z, V, [&](float v, int n, int) {
+                const auto y = sc.steps(v);
+                const int b = sc.bin_of(y);
+                const bool is = v > -INFINITY;
+                listed |= (unsigned)(b == border && is) << n;          // (border: BINS without a cut)
+                const double w = sc.weight_of(y);
+                const u64 x = units_of(w);
+                const bool in = b < border && is && w >= (double)least;
+                m += in ? x : 0;
+                n_kept += in;
+                all += x;
+            }, [&](int s) {
+                enlist(s, listed);
                 m = wave_sum(m);
                 if ((t & 63) == 0) room.segment[s] = m;
-            }
-            if (!cut_p) all_mass = block.both(Both{0, rest}).mass;          // (the kept ones' join below)
+                m = 0;
+            });
+            if (!cut_p) all_mass = block.both(Both{0, all}).mass;
         }
         __syncthreads();
         const int m = room.n;
@@ -459,38 +532,39 @@ template <int THREADS, typename T> __global__ void __launch_bounds__(THREADS) sa
         if (!greedy) {
             int shift = 0;
             while (((V - 1) >> shift) >= BINS) shift++;
-            for (int i = t; i < BINS; i += THREADS) room.bucket[i] = 0;
+            const int buckets = ((V - 1) >> shift) + 1, per = (buckets + THREADS - 1) / THREADS, b0 = t * per;
+            for (int i = t; i < buckets; i += THREADS) room.bucket[i] = 0;
             if (t == 0) room.n = 0;
             __syncthreads();
             for (int i = t; i < kept; i += THREADS) atomicAdd(&room.bucket[id_of(room.keys[i]) >> shift], sc.units(value_at(room.keys[i])));
             __syncthreads();
-            const double want = (double)a.u[row] * (double)kept_mass;
-            constexpr int RUN = BINS / THREADS;
-            u64 mine[RUN], sum = 0;
-#pragma unroll
-            for (int e = 0; e < RUN; e++) { mine[e] = room.bucket[t * RUN + e]; sum += mine[e]; }
+            const double want = (double)u * (double)kept_mass;
+            u64 sum = 0;
+            for (int e = b0; e < min(b0 + per, buckets); e++) sum += room.bucket[e];
             u64 run = block.before(sum);
-#pragma unroll
-            for (int e = 0; e < RUN; e++) {
-                if (falls_in(run, mine[e], want, kept_mass)) { room.found = t * RUN + e; room.found_before = run; }
-                run += mine[e];
+            for (int e = b0; e < min(b0 + per, buckets); e++) {
+                if (falls_in(run, room.bucket[e], want, kept_mass)) { room.found = e; room.found_before = run; }
+                run += room.bucket[e];
             }
             __syncthreads();
-            const int bucket = room.found;
-            // its tokens, at most 2^shift <= 128, take the buckets' place
-            for (int i = t; i < kept; i += THREADS)
-                if (id_of(room.keys[i]) >> shift == bucket) room.bucket[atomicAdd(&room.n, 1)] = room.keys[i];
-            __syncthreads();
-            const int m = room.n;
-            Both pick{0, 0};
-            if (t < m) {
-                const u64 key = room.bucket[t];
-                u64 r = room.found_before;
-                for (int j = 0; j < m; j++)
-                    if (id_of(room.bucket[j]) < id_of(key)) r += sc.units(value_at(room.bucket[j]));
-                if (falls_in(r, sc.units(value_at(key)), want, kept_mass)) pick.count = (u64)id_of(key) + 1;
+            token = room.found;                      // (shift 0: a bucket is an id)
+            if (shift) {
+                const int bucket = token;
+                // its tokens, at most 2^shift <= 128, take the buckets' place
+                for (int i = t; i < kept; i += THREADS)
+                    if (id_of(room.keys[i]) >> shift == bucket) room.bucket[atomicAdd(&room.n, 1)] = room.keys[i];
+                __syncthreads();
+                const int m = room.n;
+                Both pick{0, 0};
+                if (t < m) {
+                    const u64 key = room.bucket[t];
+                    u64 r = room.found_before;
+                    for (int j = 0; j < m; j++)
+                        if (id_of(room.bucket[j]) < id_of(key)) r += sc.units(value_at(room.bucket[j]));
+                    if (falls_in(r, sc.units(value_at(key)), want, kept_mass)) pick.count = (u64)id_of(key) + 1;
+                }
+                token = (int)block.both(pick, true).count - 1;
             }
-            token = (int)block.both(pick, true).count - 1;
         }
     } else {
         // ---- the list's kept tokens join their segments; the segment in which u falls is read once more
@@ -502,24 +576,24 @@ template <int THREADS, typename T> __global__ void __launch_bounds__(THREADS) sa
         const Both sums = block.both(Both{(u64)n_kept, mine});
         n_kept = (int)sums.count + kept;
         kept_mass = sums.mass;
-        if (!cut_p) all_mass += kept_mass;
         if (!greedy) {
-            const double want = (double)a.u[row] * (double)kept_mass;
+            const double want = (double)u * (double)kept_mass;
             if (falls_in(run, mine, want, kept_mass)) { room.found = t; room.found_before = run; }
             __syncthreads();
             const int i0 = room.found * SEGMENT;
-            constexpr int RUN = SEGMENT / THREADS;
+            constexpr int RUN = (SEGMENT + THREADS - 1) / THREADS;
             u64 w[RUN], sum = 0;
 #pragma unroll
             for (int e = 0; e < RUN; e++) {
                 const int i = i0 + t * RUN + e;
-                const float v = i < V ? (float)z[i] : -INFINITY;
+                const float v = i < min(V, i0 + SEGMENT) ? (float)z[i] : -INFINITY;
                 w[e] = 0;
                 if (v > -INFINITY) {
                     const u64 key = rank_key(order_of(v), i);
-                    const double y = sc.power(v), x = sc.weight_of(y);
+                    const auto y = sc.steps(v);
+                    const double x = sc.weight_of(y);
                     const int b = cut_p ? sc.bin_of(y) : 0;
-                    if ((b < border || (b == border && key >= last)) && (x >= (double)least || key == first)) w[e] = units_of(x);
+                    if ((b < border || (b == border && key >= last)) && x >= (double)least) w[e] = units_of(x);
                 }
                 sum += w[e];
             }
@@ -534,7 +608,7 @@ template <int THREADS, typename T> __global__ void __launch_bounds__(THREADS) sa
         }
     }
     if (t == 0) {
-        const double y = ((double)(float)z[token] - sc.zmax) * sc.rate * 0.69314718055994530942;
+        const double y = ((double)(float)z[token] - sc.zmax) * sc.rate * (0.69314718055994530942 / TABLE);
         a.token[row] = token;
         if (a.logp) a.logp[row] = (float)(y - log((double)all_mass / UNIT));
         if (a.logp_kept) a.logp_kept[row] = (float)(y - log((double)kept_mass / UNIT));
@@ -564,15 +638,17 @@ int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, 
     const SampleArgs a{(const char *)logits, (long)row_stride, n, vocab, temperature, top_k, top_p, min_p, u, token, logp, logp_kept, n_kept};
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps("sample_logits", (double)n * vocab * (dtype == VLA_DTYPE_F32 ? 4.0 : 2.0), st);
-    const bool f32 = dtype == VLA_DTYPE_F32;
-    // (a row of up to 1024 tokens sorts in few steps of few waves: smaller workgroups, three a CU)
-    if (vocab <= 1024) {
-        if (f32) sample_rows_kernel<256, float><<<n, 256, 0, st>>>(a);
-        else sample_rows_kernel<256, bf16_t><<<n, 256, 0, st>>>(a);
-    } else {
-        if (f32) sample_rows_kernel<1024, float><<<n, 1024, 0, st>>>(a);
-        else sample_rows_kernel<1024, bf16_t><<<n, 1024, 0, st>>>(a);
-    }
+    // A row of up to SHORT tokens is sorted whole, by few waves; longer ones go by bins (256 rows of 1024 tokens, 4096: sorted whole 28 and 63 us,
+    // by bins 23 and 25).  Segments of 512 ids have two loads of 16 bytes a lane on their way, and 512 of them are the longest row; shorter rows
+    // take 256, so that each of the 16 waves has some.  (1024 ids do not fit the registers: 128,000 logits 160 us for 112.)
+    auto go = [&](auto type) {
+        typedef decltype(type) T;
+        if (vocab <= SHORT) sample_rows_kernel<256, 256, T><<<n, 256, 0, st>>>(a);
+        else if (vocab <= 32768) sample_rows_kernel<1024, 256, T><<<n, 1024, 0, st>>>(a);
+        else sample_rows_kernel<1024, 512, T><<<n, 1024, 0, st>>>(a);
+    };
+    if (dtype == VLA_DTYPE_F32) go(0.f);
+    else go((bf16_t)0.f);
     return vla_check_launch("sample_logits");
 }
 
