@@ -105,7 +105,8 @@ class Rollout:
 
 class PagedRollout:
     """Rollouts of environments whose prefixes have any lengths, on a paged cache of ``n_pages`` pages a layer: one ragged prefill, then
-    action tokens sampled with top-k, top-p and min-p.  Pages are taken from the free ones as sequences grow."""
+    action tokens sampled with top-k, top-p and min-p.  Pages are taken from the free ones as sequences grow; a prefill frees all.  Work goes to
+    ``stream``, or to the current one; one that is not the last call's, or the one the arguments were made on, has to wait for it first."""
 
     def __init__(self, run: Rollout, n_pages: int, page_size: int = 16):
         s = run.shape
@@ -113,15 +114,26 @@ class PagedRollout:
         self.pools = [torch.zeros(s.n_layers, n_pages, s.n_heads, page_size, s.head_dim, dtype=s.torch_dtype, device=run.device) for _ in range(2)]
         self.cache = vb.make_paged_cache(self.pools[0][0], self.pools[1][0])
         self.layer_stride = self.pools[0][0].numel()
-        self.free = list(range(n_pages - 1, -1, -1))
-        self.pages, self.length, self.shared_len = [], [], 0
+        self.n_pages = n_pages
+        self._start(0)
+
+    def _start(self, n_seq):
+        self.free = list(range(self.n_pages - 1, -1, -1))
+        self.pages, self.length, self.shared_len = [[] for _ in range(n_seq)], [0] * n_seq, 0
 
     def _int(self, values):
         return torch.tensor(values, dtype=torch.int32, device=self.run.device)
 
     def forward(self, seqs, ids, rows, patch=None, prefix_len=None, shared_len=0, want_value=False, stream=None):
         """New rows for the sequences ``seqs``: rows[i] of them for seqs[i], ids of all together.  Returns (h_last, logits, value)."""
+        with torch.cuda.stream(stream):
+            return self._forward(seqs, ids, rows, patch, prefix_len, shared_len, want_value)
+
+    def _forward(self, seqs, ids, rows, patch=None, prefix_len=None, shared_len=0, want_value=False):
         run, dev = self.run, self.run.device
+        wanted = sum(max(0, (self.length[s] + n + self.page_size - 1) // self.page_size - len(self.pages[s])) for s, n in zip(seqs, rows))
+        if wanted > len(self.free):
+            raise ValueError(f"{wanted} pages wanted, {len(self.free)} of {self.n_pages} free")
         for s, n in zip(seqs, rows):
             self.length[s] += n
             while len(self.pages[s]) * self.page_size < self.length[s]:
@@ -137,42 +149,53 @@ class PagedRollout:
         h = torch.empty(len(seqs), run.shape.hidden, dtype=torch.float32, device=dev)
         logits = torch.empty(len(seqs), vb.VLA_N_BINS, dtype=torch.float32, device=dev)
         value = run._value_out(len(seqs)) if want_value else None
-        vb.vla_forward_paged(run.model.handle, self.cache, self.layer_stride, batch, ids, ws, h, patch, prefix_len, shared_len, logits, value, stream)
+        vb.vla_forward_paged(run.model.handle, self.cache, self.layer_stride, batch, ids, ws, h, patch, prefix_len, shared_len, logits, value)
         return h, logits, value
 
     def prefill(self, patches, ids, see_patches=False, stream=None):
         """patches[i] [P_i, hidden] (or None) and ids[i] [T_i] of environment i.  see_patches: an environment's patches see each other
         both ways, its instruction sees what is before it.  Returns (h_last, logits, value)."""
+        with torch.cuda.stream(stream):
+            return self._prefill(patches, ids, see_patches)
+
+    def _prefill(self, patches, ids, see_patches=False):
         dev = self.run.device
         n_patch = [0 if p is None else p.shape[0] for p in patches]
-        self.pages, self.length, self.shared_len = [[] for _ in ids], [0] * len(ids), 0
+        self._start(len(ids))
         parts, seen = [], 0
         for n, t in zip(n_patch, ids):
             parts += [-1 - torch.arange(seen, seen + n, dtype=torch.int32, device=dev), t.to(torch.int32)]
             seen += n
         held = [p for p in patches if p is not None and p.shape[0]]
-        return self.forward(list(range(len(ids))), torch.cat(parts), [n + t.numel() for n, t in zip(n_patch, ids)], torch.cat(held) if held else None,
-                            self._int(n_patch) if see_patches else None, 0, self.run.model._keep[4] is not None, stream)
+        return self._forward(list(range(len(ids))), torch.cat(parts), [n + t.numel() for n, t in zip(n_patch, ids)], torch.cat(held) if held else None,
+                             self._int(n_patch) if see_patches else None, 0, self.run.model._keep[4] is not None)
 
     def prefill_group(self, patch, ids, group: int, stream=None):
         """One observation for ``group`` rollouts: its whole pages are computed and kept once, what is behind them once per rollout."""
+        with torch.cuda.stream(stream):
+            return self._prefill_group(patch, ids, group)
+
+    def _prefill_group(self, patch, ids, group):
         n = patch.shape[0] + ids.numel()
         shared = (n - 1) // self.page_size * self.page_size
-        out = self.prefill([patch], [ids], stream=stream)
+        out = self._prefill([patch], [ids])
         if group == 1:
             return out
         self.pages += [self.pages[0][:shared // self.page_size] for _ in range(group - 1)]
         self.length += [shared] * (group - 1)
         dev = self.run.device
         tail = torch.cat([-1 - torch.arange(patch.shape[0], dtype=torch.int32, device=dev), ids.to(torch.int32)])[shared:]
-        others = self.forward(list(range(1, group)), tail.repeat(group - 1), [n - shared] * (group - 1), patch, None, shared,
-                              self.run.model._keep[4] is not None, stream)
+        others = self._forward(list(range(1, group)), tail.repeat(group - 1), [n - shared] * (group - 1), patch, None, shared, self.run.model._keep[4] is not None)
         self.shared_len = shared
         return tuple(None if a is None else torch.cat([a, b]) for a, b in zip(out, others))
 
     def decode(self, logits, n_tokens: int, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, u=None, stream=None):
         """n_tokens action tokens of every sequence from the first one's logits; u [n_tokens, n_seq] in [0, 1), or None: the largest.
         Returns bins, logp (under softmax(z / temperature)), logp_kept (among the kept bins), logits, each [n_seq, n_tokens, ...]."""
+        with torch.cuda.stream(stream):
+            return self._decode(logits, n_tokens, temperature, top_k, top_p, min_p, u)
+
+    def _decode(self, logits, n_tokens, temperature, top_k, top_p, min_p, u):
         run, n, dev = self.run, logits.shape[0], self.run.device
         every = lambda v, dtype: torch.full((n,), v, dtype=dtype, device=dev)
         t, k, p, least = every(temperature, torch.float32), every(top_k, torch.int32), every(top_p, torch.float32), every(min_p, torch.float32)
@@ -180,11 +203,11 @@ class PagedRollout:
         out = [[], [], [], []]
         for j in range(n_tokens):
             bins, logp, kept = (torch.empty(n, dtype=d, device=dev) for d in (torch.int32, torch.float32, torch.float32))
-            vb.vla_sample_logits(logits, bins, t, k, p, least, None if u is None else u[j].contiguous(), logp, kept, None, ws, stream)
+            vb.vla_sample_logits(logits, bins, t, k, p, least, None if u is None else u[j].contiguous(), logp, kept, None, ws)
             for o, x in zip(out, (bins, logp, kept, logits)):
                 o.append(x)
             if j + 1 < n_tokens:
-                _, logits, _ = self.forward(list(range(n)), bins + (run.shape.vocab - vb.VLA_N_BINS), [1] * n, shared_len=self.shared_len, stream=stream)
+                _, logits, _ = self._forward(list(range(n)), bins + (run.shape.vocab - vb.VLA_N_BINS), [1] * n, shared_len=self.shared_len)
         return tuple(torch.stack(o, 1) for o in out)
 
 

@@ -138,3 +138,29 @@ def test_captured_step_follows_its_arrays(dtype):
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (q, out, token, *pools)))
+
+
+def test_pages_come_back_and_run_out():
+    run, obs, _, _ = setup("f32", [(40, 9), (3, 2)])
+    paged = PagedRollout(run, 6)
+    args = [p for p, _ in obs], [t for _, t in obs]
+    first = paged.prefill(*args)[1]
+    for _ in range(3):                                       # 5 of 6 pages each time
+        assert torch.equal(paged.prefill(*args)[1], first)
+    held = [list(p) for p in paged.pages], list(paged.length), list(paged.free)
+    with pytest.raises(ValueError, match="2 pages wanted, 1 of 6 free"):
+        paged.forward([0, 1], torch.zeros(35, dtype=torch.int32, device=DEV), [16, 19])
+    assert held == (paged.pages, paged.length, paged.free)
+
+
+def test_another_stream():
+    run, obs, _, _ = setup("bf16", [(48, 21), (5, 3)])
+    u = torch.rand(4, 2, generator=torch.Generator().manual_seed(1)).to(DEV)
+    paged, stream = PagedRollout(run, 32), torch.cuda.Stream()
+    results = []
+    for s in (None, stream):
+        torch.cuda.synchronize()
+        logits = paged.prefill([p for p, _ in obs], [t for _, t in obs], stream=s)[1]
+        results.append(paged.decode(logits, 4, top_k=40, u=u, stream=s))
+        torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*results))
