@@ -342,7 +342,8 @@ int vla_policy_objective_noalloc(const float *logp_new, const float *logp_old, c
  *   (HOST): a multiple of page_size; the first shared_len positions of all sequences lie in the same pages, which are read once
  *   for the whole batch, through sequence 0's table (sequence 0 and every sequence with rows hold shared_len positions
  *   or more); not together with a window.
- *   ws: DEVICE, 16-byte aligned, of vla_paged_attention_workspace_bytes (from HOST numbers alone) bytes: partial sums of split key ranges; no state.
+ *   out does not overlap q.  ws: DEVICE, 16-byte aligned, of vla_paged_attention_workspace_bytes (from HOST numbers alone) bytes: partial sums of
+ *   split key ranges; no state, but calls that overlap in time need one each.
  *   Sums are added in a fixed order: the same call gives the same bits; the split depends on the HOST numbers.
  *
  * vla_sample_logits: one token per row of logits (DEVICE dtype [n, vocab], row stride in elements), vocab at most 262,144.
@@ -354,7 +355,7 @@ int vla_policy_objective_noalloc(const float *logp_new, const float *logp_old, c
  *   temperature, top_p, min_p, u: DEVICE fp32 [n]; top_k DEVICE int32 [n]; each may be NULL (1, all, all, greedy, all).
  *   logp (or NULL): log-probability under softmax(z / T), as the recompute gives it; logp_kept (or NULL): among the kept tokens;
  *   n_kept (or NULL).  With T <= 0 or u NULL the cuts still apply to n_kept and logp_kept; T <= 0 counts as 1 in all of them.  Masses are summed as 64-bit fixed point numbers,
- *   in any order the same, so equal inputs give equal tokens. */
+ *   in any order the same, so equal inputs give equal tokens.  ws: DEVICE, of vla_sample_logits_workspace_bytes bytes. */
 /* vla_forward_paged: the decoder over a ragged batch's new rows: a prefill of prefixes of any lengths, a decode step, or both at once.
  *   Row r is the embedding of token ids[r], or, where ids[r] < 0, row -1 - ids[r] of patch (DEVICE dtype [n_patch, hidden]; ids and rows out of
  *   range are clamped).  Every layer appends its K and V to its cache, layer l at cache->k, v + l * layer_stride elements, and attends:

@@ -342,14 +342,44 @@ def _want(t, kind: str, name: str, shape=None):
     return t.data_ptr()
 
 
+def _device_of(*tensors):
+    """The GPU that tensors are on; None if there are none, -1 for host memory or several."""
+    found = None
+    for t in tensors:
+        if t is not None:
+            d = t.get_device()
+            found = d if found is None or found == d else -1
+    return found
+
+
+def _on_current_device(what, structures, tensors):
+    """The library launches on the current GPU: arrays of another one, or of the host, would be read from there."""
+    here = tensors[0].get_device()
+    for s in structures:
+        if s.device is not None and s.device != here:
+            here = -1
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            here = -1
+    if here < 0 or here != _current_device():
+        raise VlaError(VLA_EINVAL, f"{what}: the arrays are not all on the current GPU")
+
+
+def _current_device() -> int:
+    import torch
+    device = getattr(torch._C, "_cuda_getDevice", None)          # (no public interface; 0.4 us less)
+    return device() if device and torch.cuda.is_initialized() else torch.cuda.current_device()
+
+
 def _rows_of_heads(t, heads, dim, rows, name):
     """Address and row stride of a [rows, heads, dim] view whose heads are packed within a row."""
-    if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
-        raise VlaError(VLA_ESHAPE, f"{name} is {list(t.shape)}, wanted [{rows}, {'heads' if heads is None else heads}, {dim}]")
-    if t.numel() and ((dim > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != dim)):
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != rows or shape[2] != dim or (heads is not None and shape[1] != heads):
+        raise VlaError(VLA_ESHAPE, f"{name} is {list(shape)}, wanted [{rows}, {'heads' if heads is None else heads}, {dim}]")
+    row, head, one = t.stride()
+    if (one != 1 or (head != dim and shape[1] > 1)) and dim > 1 and t.numel():
         raise VlaError(VLA_EINVAL, f"{name}: the heads of a row are not packed (strides {t.stride()})")
-    width = t.shape[1] * dim
-    return t.data_ptr(), (t.stride(0) if rows > 1 else width)
+    return t.data_ptr(), row if rows > 1 else shape[1] * dim
 
 
 def make_paged_cache(k, v) -> vla_paged_cache:
@@ -358,7 +388,7 @@ def make_paged_cache(k, v) -> vla_paged_cache:
         raise VlaError(VLA_ESHAPE, "k and v are contiguous [n_pages, n_kv_heads, page_size, head_dim] tensors of one type")
     n_pages, n_kv_heads, page_size, head_dim = k.shape
     c = vla_paged_cache(k.data_ptr(), v.data_ptr(), _dtype(k), n_pages, page_size, n_kv_heads, head_dim)
-    c.keep = (k, v)
+    c.keep, c.device = (k, v), _device_of(k, v)
     return c
 
 
@@ -369,7 +399,7 @@ def make_paged_batch(row_start, kv_len, page_table, n_rows: int, max_rows: int, 
         raise VlaError(VLA_ESHAPE, f"page_table is {list(page_table.shape)}, wanted [n_seq, entries]")
     b = vla_paged_batch(n_seq, n_rows, max_rows, max_len, page_table.shape[1], _want(row_start, "int32", "row_start", (n_seq + 1,)),
                         _want(kv_len, "int32", "kv_len", (n_seq,)), _want(page_table, "int32", "page_table", (n_seq, page_table.shape[1])))
-    b.keep = (row_start, kv_len, page_table)
+    b.keep, b.device = (row_start, kv_len, page_table), _device_of(row_start, kv_len, page_table)
     return b
 
 
@@ -377,13 +407,13 @@ def make_rotary(inv_freq=None, interleaved=False, scale=1.0, q_gain=None, k_gain
     """``inv_freq``: fp64 device tensor [rot_dim / 2], or None for no rotation."""
     r = vla_rotary(_want(inv_freq, "float64", "inv_freq"), 0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(interleaved)), scale, eps,
                    _want(q_gain, "float32", "q_gain"), _want(k_gain, "float32", "k_gain"))
-    r.keep = (inv_freq, q_gain, k_gain)
+    r.keep, r.device = (inv_freq, q_gain, k_gain), _device_of(inv_freq, q_gain, k_gain)
     return r
 
 
 def make_paged_mask(scale: float, softcap=0.0, slopes=None, prefix_len=None, window=0, shared_len=0) -> vla_paged_mask:
     m = vla_paged_mask(scale, softcap, _want(slopes, "float32", "slopes"), _want(prefix_len, "int32", "prefix_len"), window, shared_len)
-    m.keep = (slopes, prefix_len)
+    m.keep, m.device = (slopes, prefix_len), _device_of(slopes, prefix_len)
     return m
 
 
@@ -392,20 +422,22 @@ def vla_paged_append(cache, batch, rotary, q, k, v, q_out=None, stream=None) -> 
     d, rows = cache.head_dim, batch.n_rows
     if (q is None) != (q_out is None):
         raise VlaError(VLA_EINVAL, "paged_append: q and q_out come together")
-    for g, name in ((rotary.keep[1], "q_gain"), (rotary.keep[2], "k_gain")):
-        _want(g, "float32", name, (d,))
+    _, q_gain, k_gain = rotary.keep
+    if q_gain is not None or k_gain is not None:
+        _want(q_gain, "float32", "q_gain", (d,)), _want(k_gain, "float32", "k_gain", (d,))
     kp, ks = _rows_of_heads(k, cache.n_kv_heads, d, rows, "k")
     vp_, vs = _rows_of_heads(v, cache.n_kv_heads, d, rows, "v")
     qp = qs = op = os_ = 0
     heads = cache.n_kv_heads
     if q is not None:
-        heads = q.shape[1]
         qp, qs = _rows_of_heads(q, None, d, rows, "q")
+        heads = q.shape[1]
         op, os_ = _rows_of_heads(q_out, heads, d, rows, "q_out")
         if _dtype(q_out) != cache.dtype:
             raise VlaError(VLA_EDTYPE, "paged_append: q_out has the cache's type")
     if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
         raise VlaError(VLA_EDTYPE, "paged_append: q, k and v have one type")
+    _on_current_device("paged_append", (cache, batch, rotary), (k, v, q, q_out))
     _check(lib().vla_paged_append(C.byref(cache), C.byref(batch), C.byref(rotary), qp or None, kp, vp_, _dtype(k), heads, qs, ks, vs,
                                   op or None, os_, _stream(stream)))
 
@@ -418,13 +450,15 @@ def vla_paged_attention_workspace_bytes(cache, batch, mask, n_heads: int) -> int
 
 
 def vla_paged_attention(cache, batch, mask, q, out, lse=None, ws=None, stream=None) -> None:
-    heads, rows = q.shape[1], batch.n_rows
+    rows = batch.n_rows
     qp, qs = _rows_of_heads(q, None, cache.head_dim, rows, "q")
+    heads = q.shape[1]
     op, os_ = _rows_of_heads(out, heads, cache.head_dim, rows, "out")
     if _dtype(q) != cache.dtype or _dtype(out) != cache.dtype:
         raise VlaError(VLA_EDTYPE, "paged_attention: q and out have the cache's type")
     _want(mask.keep[0], "float32", "slopes", (heads,))
     _want(mask.keep[1], "int32", "prefix_len", (batch.n_seq,))
+    _on_current_device("paged_attention", (cache, batch, mask), (q, out, lse, ws))
     _check(lib().vla_paged_attention(C.byref(cache), C.byref(batch), C.byref(mask), qp, heads, qs, op, os_,
                                      _want(lse, "float32", "lse", (rows, heads)), _ptr(ws),
                                      0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
@@ -439,12 +473,16 @@ def vla_forward_paged_workspace_bytes(cfg: vla_config, cache, batch, shared_len:
 
 def vla_forward_paged(model, cache, layer_stride: int, batch, ids, ws, h_last, patch=None, prefix_len=None, shared_len=0, logits=None, value=None, stream=None) -> None:
     """``ids`` int32 [n_rows]; ``patch`` [n_patch, hidden] in the model's type: the rows that negative ids name."""
-    if patch is not None and not patch.is_contiguous():
-        raise VlaError(VLA_EINVAL, "forward_paged: patch is not contiguous")
-    _check(lib().vla_forward_paged(model, C.byref(cache), layer_stride, C.byref(batch), _want(ids, "int32", "ids", (batch.n_rows,)), _ptr(patch),
-                                   0 if patch is None else patch.shape[0], _want(prefix_len, "int32", "prefix_len", (batch.n_seq,)), shared_len, _ptr(ws),
-                                   ws.numel() * ws.element_size(), _want(h_last, "float32", "h_last"), _want(logits, "float32", "logits", (batch.n_seq, VLA_N_BINS)),
-                                   _want(value, "float32", "value"), _stream(stream)))
+    n, hidden = batch.n_seq, cache.n_kv_heads * cache.head_dim
+    if patch is not None and (not patch.is_contiguous() or patch.dim() != 2 or patch.shape[1] != hidden or _dtype(patch) != cache.dtype):
+        raise VlaError(VLA_EINVAL, f"forward_paged: patch is not contiguous [n_patch, {hidden}] of the cache's type")
+    if value is not None and value.shape[:1] != (n,):
+        raise VlaError(VLA_EINVAL, f"forward_paged: value is {list(value.shape)}, wanted [{n}, value_dim]")
+    arrays = (_want(ids, "int32", "ids", (batch.n_rows,)), _want(prefix_len, "int32", "prefix_len", (n,)), _want(h_last, "float32", "h_last", (n, hidden)),
+              _want(logits, "float32", "logits", (n, VLA_N_BINS)), _want(value, "float32", "value"))
+    _on_current_device("forward_paged", (cache, batch), (ids, patch, prefix_len, ws, h_last, logits, value))
+    _check(lib().vla_forward_paged(model, C.byref(cache), layer_stride, C.byref(batch), arrays[0], _ptr(patch), 0 if patch is None else patch.shape[0],
+                                   arrays[1], shared_len, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), *arrays[2:], _stream(stream)))
 
 
 def vla_sample_logits_workspace_bytes(n: int, vocab: int) -> int:
@@ -462,10 +500,12 @@ def vla_sample_logits(logits, token, temperature=None, top_k=None, top_p=None, m
     n, vocab = logits.shape
     f = lambda t, name: _want(t, "float32", name, (n,))
     i = lambda t, name: _want(t, "int32", name, (n,))
-    _check(lib().vla_sample_logits(logits.data_ptr(), _dtype(logits), logits.stride(0) if n > 1 else vocab, n, vocab, f(temperature, "temperature"),
-                                   i(top_k, "top_k"), f(top_p, "top_p"), f(min_p, "min_p"), f(u, "u"), i(token, "token"), f(logp, "logp"),
-                                   f(logp_kept, "logp_kept"), i(n_kept, "n_kept"), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
-                                   _stream(stream)))
+    settings = f(temperature, "temperature"), i(top_k, "top_k"), f(top_p, "top_p"), f(min_p, "min_p"), f(u, "u")
+    outputs = i(token, "token"), f(logp, "logp"), f(logp_kept, "logp_kept"), i(n_kept, "n_kept")
+    code = _dtype(logits)
+    _on_current_device("sample_logits", (), (logits, temperature, top_k, top_p, min_p, u, token, logp, logp_kept, n_kept, ws))
+    _check(lib().vla_sample_logits(logits.data_ptr(), code, logits.stride(0) if n > 1 else vocab, n, vocab, *settings, *outputs, _ptr(ws),
+                                   0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def _doubles(values):

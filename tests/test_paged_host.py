@@ -127,3 +127,18 @@ def test_forward_paged_refuses():
     q = lambda **k: L.vla_forward_paged_workspace_bytes(C.byref(cfg), C.byref(cache(**dict(good, **k))), C.byref(batch()), 0)
     assert q() > 5 * 256 * 4 and q(head_dim=48) == 0
     vb.vla_destroy(h)
+
+
+def test_binding_refuses_arrays_of_the_host():
+    import torch
+    z, i32 = torch.zeros, torch.int32
+    c, b = vb.make_paged_cache(z(8, 2, 16, 64), z(8, 2, 16, 64)), vb.make_paged_batch(z(3, dtype=i32), z(2, dtype=i32), z(2, 3, dtype=i32), 5, 3, 40)
+    for call in (lambda: vb.vla_paged_append(c, b, vb.make_rotary(), z(5, 4, 64), z(5, 2, 64), z(5, 2, 64), z(5, 4, 64)),
+                 lambda: vb.vla_paged_attention(c, b, vb.make_paged_mask(1.0), z(5, 4, 64), z(5, 4, 64), ws=z(1 << 20)),
+                 lambda: vb.vla_forward_paged(None, c, 0, b, z(5, dtype=i32), z(1 << 20), z(2, 128)),
+                 lambda: vb.vla_sample_logits(z(4, 9), z(4, dtype=i32), ws=z(64))):
+        with pytest.raises(vb.VlaError, match="not all on the current GPU"):
+            call()
+    for k in (dict(h_last=z(2, 64)), dict(patch=z(4, 64)), dict(patch=z(4, 128).bfloat16()), dict(value=z(3)), dict(logits=z(2, 255)), dict(prefix_len=z(2))):
+        with pytest.raises(vb.VlaError, match="wanted|patch"):
+            vb.vla_forward_paged(None, c, 0, b, z(5, dtype=i32), z(1 << 20), **{"h_last": z(2, 128), **k})
