@@ -316,8 +316,8 @@ int vla_policy_objective_noalloc(const float *logp_new, const float *logp_old, c
  *   page_table[sequence][p / page_size], row p % page_size.
  * vla_paged_batch: rows of n_seq sequences, one after the other: sequence s has rows row_start[s] .. row_start[s + 1] - 1
  *   (row_start ascending from 0), the newest of its kv_len[s] positions: row i of its n_s rows is at position
- *   kv_len[s] - n_s + i.  A sequence may have no rows.  Rows from row_start[n_seq] to n_rows - 1 are padding: neither read nor
- *   written.  max_rows, max_len (HOST): bounds of n_s and kv_len that the launches are sized by; work beyond them is left out, and so are
+ *   kv_len[s] - n_s + i.  A sequence may have no rows.  Rows from row_start[n_seq] to n_rows - 1 are padding: whatever they
+ *   hold changes nothing, and nothing is written for them.  max_rows, max_len (HOST): bounds of n_s and kv_len that the launches are sized by; work beyond them is left out, and so are
  *   pages whose id is not in [0, n_pages): the rows are not written, and read as zeros.  The arrays are read on the device, so a captured call follows them as they change.
  *   table_stride: entries per sequence in page_table, at least max_len / page_size rounded up; entries of pages that hold no
  *   visible position are never read.
