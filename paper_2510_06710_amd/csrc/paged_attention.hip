@@ -41,7 +41,7 @@ struct AttnArgs {
     const float *slopes;
     const int32_t *prefix_len;
     int window, shared_len;
-    float offset;            // what scores lack, in log2 units (see Rows::tile): lse alone knows it
+    float offset;            // what scores lack, in log2 units (see Rows::shaped): lse alone knows it
     int aligned;             // rows of q and out start at multiples of 16 bytes
     // this launch
     int decode;              // the new rows' own keys in decode form
@@ -483,6 +483,10 @@ __device__ __forceinline__ bool sees_all(const Query &y, int k0, int k1) { retur
 // Four waves of 32 packed rows each, all walking the same keys, 32 at a time.  K and V move through rings of RING tiles, K one tile before V: while
 // tile t's weights are formed on the vector units its successor's scores are on the matrix pipe, instruction by instruction in turn,
 // and while its values are summed the successor's largest is found.
+// Bound by the matrix pipe and the vector work beside it: 8192 causal rows of 32 heads of 128, 8 key heads: 530 us, 1.04 PFLOP/s where a plain matrix
+// product reaches 1.39 on this card; heads of 64: 340 us, of 256: 1.35 ms; capped 640; fp32, 2048 rows, heads of 64: 320 us, 107 of 154 TFLOP/s.  (Scores and
+// weights one after the other: 637 us; in turn, but every step with its checks: 654.)  A ragged batch of 13 chunks of up to 613 rows: 32 us, a few rounds of
+// workgroups, each with its chain of dependent loads.
 constexpr int LDS_STARTS = 2048;
 template <typename T, int DP> constexpr int RING = 32 * Tile<T, DP>::ROW * 8 <= 64 * 1024 ? 4 : 2;
 template <typename T, int DP, int MODE>
@@ -640,7 +644,7 @@ struct Walk {
 // their lengths, and streams through it, the next tile on its way whether it is of the same sequence or not.  A sequence's tiles that
 // fall to several waves leave parts for the join (a wave has at most two: of the sequence it begins within, and of the one it ends within).
 // Neighbouring waves have the same run of different heads, whose rows lie side by side in the pages.
-// Memory bound: 32 sequences of 2048 keys, 32 heads, 192 us, 5.6 TB/s; 256 of 294 keys 252 us; one of 32768 keys, 8 key heads, 27 us and 6 for
+// Memory bound: 32 sequences of 2048 keys, 32 heads, 192 us, 5.6 TB/s; 256 of 294 keys 246 us, 5.0; one of 32768 keys, 8 key heads, 26 us and 6 for
 // the join of 128 parts; 48 ragged ones of up to 8192 keys with capped scores and a bias 79 us.  (One workgroup of 1, 2 or 4 waves per sequence,
 // key head and even part of max_len: 200, 259, 30 + 5 and 125 to 155 us.)
 template <typename T, int DP, int MODE>
@@ -710,10 +714,10 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(AttnArgs a) {
             off_v.load(at + BYTES, place.in(a.pv, a.pv.v, p0, x));
             off_v.load(at + BYTES + 16 * TL::ROW, place.in(a.pv, a.pv.v, p1, z));
         } else {
-        TL::template load<false, 16>(at, a.pv.k, a.pv, p0, ahead.it.kvh, t * KT, sp);
-        TL::template load<false, 16>(at + 16 * TL::ROW, a.pv.k, a.pv, p1, ahead.it.kvh, t * KT + 16, sp);
-        TL::template load<true, 16>(at + BYTES, a.pv.v, a.pv, p0, ahead.it.kvh, t * KT, sp);
-        TL::template load<true, 16>(at + BYTES + 16 * TL::ROW, a.pv.v, a.pv, p1, ahead.it.kvh, t * KT + 16, sp);
+            TL::template load<false, 16>(at, a.pv.k, a.pv, p0, ahead.it.kvh, t * KT, sp);
+            TL::template load<false, 16>(at + 16 * TL::ROW, a.pv.k, a.pv, p1, ahead.it.kvh, t * KT + 16, sp);
+            TL::template load<true, 16>(at + BYTES, a.pv.v, a.pv, p0, ahead.it.kvh, t * KT, sp);
+            TL::template load<true, 16>(at + BYTES + 16 * TL::ROW, a.pv.v, a.pv, p1, ahead.it.kvh, t * KT + 16, sp);
         }
         if (++t < ahead.t1) pages();
         else { more = lead.next(a, &ahead); settle(); }

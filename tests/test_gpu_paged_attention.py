@@ -170,3 +170,29 @@ def test_loose_host_bounds_and_bad_pages(dtype):
         vb.vla_paged_attention(cache, batch, mask, q.to(DEV), out, None, ws)
         outs.append(out)
     assert torch.equal(*outs)
+
+
+@BOTH
+@pytest.mark.parametrize("shared", [0, 16])
+def test_thousands_of_sequences(dtype, shared):
+    run(Batch([(1, 17 + s % 40) for s in range(2051)], 16, shared=shared, padding=3), dtype, 2, 1, 32, shared=shared)
+
+
+@pytest.mark.parametrize("heads,kv", [(4, 2), (64, 1)])
+@pytest.mark.parametrize("shared", [0, 32])
+def test_rows_beyond_the_host_bound_are_left(heads, kv, shared):
+    b = Batch([(5, 60), (1, 200), (3, 35)], 16, shared=shared)
+    q, pools = make(b, "f32", heads, kv, 64, 0, None, 0, shared)
+    dev, outs = [p.to(DEV) for p in pools], []
+    for b.max_rows in (5, 2):
+        out, lse = torch.full((b.n_rows, heads, 64), -77.0, device=DEV), torch.full((b.n_rows, heads), -77.0, device=DEV)
+        cache, batch, mask = vb.make_paged_cache(*dev), b.on_device(), vb.make_paged_mask(0.125, shared_len=shared)
+        ws = torch.full((vb.vla_paged_attention_workspace_bytes(cache, batch, mask, heads),), 255, dtype=torch.uint8, device=DEV)
+        vb.vla_paged_attention(cache, batch, mask, q.to(DEV), out, lse, ws)
+        outs.append((out.cpu(), lse.cpu()))
+    (full, full_l), (some, some_l) = outs
+    kept = torch.tensor([0, 1, 5, 6, 7])
+    # two evaluations, each off by 2 ds A + n 2^-24 A with ds < 64 2^-24 x 40 + 5 x 2^-21, A < 5, n = 200
+    assert (full[kept] - some[kept]).abs().max() <= 2 * (2 * (64 * 40 * 2.0 ** -24 + 5 * 2.0 ** -21) + 200 * 2.0 ** -24) * 5 and (full_l[kept] - some_l[kept]).abs().max() <= 1e-3
+    left = torch.tensor([2, 3, 4, 8])
+    assert (some[left] == -77).all() and (some_l[left] == -77).all() and (full != -77).all()
