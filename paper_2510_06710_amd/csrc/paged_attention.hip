@@ -644,7 +644,7 @@ struct Walk {
 // their lengths, and streams through it, the next tile on its way whether it is of the same sequence or not.  A sequence's tiles that
 // fall to several waves leave parts for the join (a wave has at most two: of the sequence it begins within, and of the one it ends within).
 // Neighbouring waves have the same run of different heads, whose rows lie side by side in the pages.
-// Memory bound: 32 sequences of 2048 keys, 32 heads, 192 us, 5.6 TB/s; 256 of 294 keys 246 us, 5.0; one of 32768 keys, 8 key heads, 26 us and 6 for
+// Memory bound: 32 sequences of 2048 keys, 32 heads, 192 us, 5.6 TB/s; 256 of 294 keys 226 us, 5.5; one of 32768 keys, 8 key heads, 26 us and 6 for
 // the join of 128 parts; 48 ragged ones of up to 8192 keys with capped scores and a bias 79 us.  (One workgroup of 1, 2 or 4 waves per sequence,
 // key head and even part of max_len: 200, 259, 30 + 5 and 125 to 155 us.)
 template <typename T, int DP, int MODE>
@@ -751,9 +751,11 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(AttnArgs a) {
     }
 }
 
-// The parts of one (row, head), joined by one workgroup: DP / 4 lanes a part, so 1024 / DP parts at a time, whose sums are added in one order.
-// First the parts of all rows' layout (ml, o_part), then those of the waves that shared the sequence.
-// (One wave a pair and part after part: 41 us for 64 parts of 32 pairs, a memory latency each.)
+// The parts of a row's heads.  FEW or less, as where a prompt's keys are in two parts or a decode wave's end falls into a sequence: DP / 4 lanes
+// a (row, head) read them at once (4000 rows of 16 heads in two parts: 11 us; a workgroup for each 90).  More: a workgroup for each (row, head),
+// DP / 4 lanes a part, so 1024 / DP parts at a time, whose sums are added in one order.  (One wave and part after part: 41 us for 64 parts of 32
+// pairs, a memory latency each.)  The parts of all rows' layout (ml, o_part) come first, then those of the waves that shared the sequence.
+constexpr int FEW = 4;
 constexpr int JOIN_PARTS = 2048 + 512;          // of waves, and of own and shared ranges, at most
 template <typename T, int DP>
 __global__ void __launch_bounds__(256) paged_join_kernel(AttnArgs a) {
@@ -778,12 +780,40 @@ __global__ void __launch_bounds__(256) paged_join_kernel(AttnArgs a) {
     }
     const int n = a.parts - first, total = n + shared, dim = (t % LANES) * 4;
     const size_t step = (size_t)pv.n_rows * a.n_heads;
+    // (the wave that begins a sequence holds it as its last, the others as their first)
+    auto wave_slot = [&](int h, int z) { return (((size_t)(w0 + z) * pv.n_kv + h / a.group) * 2 + (z == 0 ? 1 : 0)) * a.packed + i0 * a.group + h % a.group; };
+    auto ml_at = [&](int h, int z) { return z < n ? a.ml[(z + first) * step + (size_t)row * a.n_heads + h] : a.wave_ml[wave_slot(h, z - n)]; };
+    auto sums_at = [&](int h, int z) { return *(const f32x4_t *)((z < n ? a.o_part + ((z + first) * step + (size_t)row * a.n_heads + h) * d : a.wave_o + wave_slot(h, z - n) * d) + dim); };
+    if (total <= FEW) {                                      // every DP / 4 lanes a head of their own, whose parts they read themselves
+        for (int h = blockIdx.y * AT_ONCE + t / LANES; h < a.n_heads; h += gridDim.y * AT_ONCE) {
+            float2 ml[FEW];
+            f32x4_t v[FEW], o = {0.f, 0.f, 0.f, 0.f};
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int z = 0; z < FEW; z++) {
+                ml[z] = z < total ? ml_at(h, z) : make_float2(-INFINITY, 0.f);
+                if (z < total && dim < d) v[z] = sums_at(h, z);
+                top = fmaxf(top, ml[z].x);
+            }
+#pragma unroll
+            for (int z = 0; z < FEW; z++) {
+                const float f = ml[z].y > 0.f ? __builtin_amdgcn_exp2f(ml[z].x - top) : 0.f;
+                sum += f * ml[z].y;
+#pragma unroll
+                for (int e = 0; e < 4; e++) o[e] += f > 0.f ? f * v[z][e] : 0.f;
+            }
+            if (dim >= d) continue;
+            const float f = sum > 0.f ? 1.f / sum : 0.f;
+            T *dst = (T *)a.out + row * a.o_stride + (size_t)h * d + dim;
+#pragma unroll
+            for (int e = 0; e < 4; e++) dst[e] = (T)(o[e] * f);
+            if (a.lse && dim == 0) a.lse[(size_t)row * a.n_heads + h] = sum > 0.f ? (top + a.offset + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        }
+        return;
+    }
     for (int h = blockIdx.y; h < a.n_heads; h += gridDim.y) {
         const size_t at = (size_t)row * a.n_heads + h;
-        const int packed = i0 * a.group + h % a.group;
-        // (the wave that begins a sequence holds it as its last, the others as their first)
-        auto wave_slot = [&](int z) { return (((size_t)(w0 + z) * pv.n_kv + h / a.group) * 2 + (z == 0 ? 1 : 0)) * a.packed + packed; };
-        auto ml_of = [&](int z) { return z < n ? a.ml[(z + first) * step + at] : a.wave_ml[wave_slot(z - n)]; };
+        auto ml_of = [&](int z) { return ml_at(h, z); };
         float top = -INFINITY, sum = 0.f;
         for (int z = lane; z < total; z += 64) top = fmaxf(top, ml_of(z).x);
         top = vla_wave_fold(top, VlaMax());
@@ -801,7 +831,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(AttnArgs a) {
 #pragma unroll 8
             for (int z = t / LANES; z < total; z += AT_ONCE) {
                 const float f = weights[z];
-                const f32x4_t v = *(const f32x4_t *)((z < n ? a.o_part + ((z + first) * step + at) * d : a.wave_o + wave_slot(z - n) * d) + dim);
+                const f32x4_t v = sums_at(h, z);
 #pragma unroll
                 for (int e = 0; e < 4; e++) o[e] += f > 0.f ? f * v[e] : 0.f;          // (an empty part has no sums, whatever lies there)
             }
@@ -890,11 +920,15 @@ Plan plan(const AttnArgs &a, bool f32) {
     // Decode form: up to 32 packed rows a sequence (a matrix instruction's columns).  (Every wave looks at all sequences' lengths: not for many thousands.)
     p.decode = (long)a.pv.max_rows * a.group <= 32 && a.pv.n_seq <= 2048 && (long)a.pv.n_seq * (a.pv.max_len / 32 + 2) < 1L << 30;
     if (p.decode) {
-        // as many waves as their rings, 128 rows of K or V each, fit the CUs' LDS; a few tiles at most per sequence: not divided, which saves the join
-        // (handed out in units of 1280 bytes: four of 32 KB)
+        // as many waves as their rings, 128 rows of K or V each, fit the CUs' LDS (handed out in units of 1280 bytes: four of 32 KB)
         const int fit = 128 / ((128 * padded_dim(a.pv.d) * (f32 ? 4 : 2) + 1279) / 1280);
-        const int waves = 256 * (fit > 8 ? 8 : fit) / a.pv.n_kv;
-        p.waves = a.pv.max_len - a.shared_len > 128 ? (waves > 0 ? waves : 1) : 0;
+        const int all = 256 * (fit > 8 ? 8 : fit), waves = all / a.pv.n_kv;
+        // Not divided, a wave per sequence and key head, which saves the search for a share and most of the join: where these are enough to fill the chip and
+        // the longest is no long tail behind the others.  1024 waves, 32 key heads: 256 sequences of 294 keys 226 us (divided 248), of 1024 744 (801), ragged up to
+        // 1024 399 (430); 16 of up to 512 26 both ways; but 16 ragged ones of up to 1024 42 (36), 64 of up to 2048 235 (222).
+        const long pairs = (long)a.pv.n_seq * a.pv.n_kv, longest = a.pv.max_len - a.shared_len;
+        const bool divided = longest > (pairs >= 4 * all ? 1024 : 2 * pairs >= all ? 512 : 128);
+        p.waves = divided ? (waves > 0 ? waves : 1) : 0;
         p.parts = 1;
     } else {
         p.own = plan_prompt(a, f32, false);
