@@ -358,13 +358,13 @@ template <int THREADS, typename T> __device__ void sample_by_bisection(const Sam
 }
 
 
-template <int THREADS, int SEGMENT, typename T> __global__ void __launch_bounds__(THREADS) sample_rows_kernel(SampleArgs a) {
+// WHOLE: the row itself is the list.
+template <int THREADS, int SEGMENT, bool WHOLE, typename T> __global__ void __launch_bounds__(THREADS) sample_rows_kernel(SampleArgs a) {
     __shared__ Room<THREADS> room;
     Block<THREADS> &block = room.block;
     const int row = blockIdx.x, t = threadIdx.x, V = a.vocab;
     const T *z = (const T *)a.logits + row * a.stride;
     typedef Segment<SEGMENT, T> Seg;
-    constexpr bool whole = THREADS < 1024;          // the row itself is the list
     // (asked for together with the row: each alone is a memory latency)
     const float T0 = a.temperature ? a.temperature[row] : 1.f, p = a.top_p ? a.top_p[row] : 1.f, least = fminf(a.min_p ? a.min_p[row] : 0.f, 1.f), u = a.u ? a.u[row] : 0.f;
     int k = a.top_k ? a.top_k[row] : 0;
@@ -372,7 +372,7 @@ template <int THREADS, int SEGMENT, typename T> __global__ void __launch_bounds_
     // ---- the largest, and how many there are
     Both top{0, 0};
     int P = 2;                             // places of the list, a power of two
-    if constexpr (whole) {
+    if constexpr (WHOLE) {
         while (P < V) P <<= 1;
         for (int i = t; i < P; i += THREADS) {
             const unsigned o = i < V ? order_of((float)z[i]) : 0u;
@@ -411,12 +411,12 @@ template <int THREADS, int SEGMENT, typename T> __global__ void __launch_bounds_
     if (k <= 0 || k >= valid) k = valid;
     const bool cut_k = k < valid, cut_p = p < 1.f;
     const double share = p > 0.f ? (double)p : 0.0;
-    const bool ranked = whole || cut_k;    // the list holds all leading tokens (else: those of the bin in which the cut of top-p falls)
+    const bool ranked = WHOLE || cut_k;    // the list holds all leading tokens (else: those of the bin in which the cut of top-p falls)
 
     u64 all_mass = 0, kept_mass = 0, above = 0;      // of the row; of the kept tokens; of the bins before the border
     int n_kept = 0, border = BINS;
     double limit = 0.0;                              // mass before a token at which top-p ends
-    if constexpr (!whole) {
+    if constexpr (!WHOLE) {
         // ---- bins: where the cut falls
         if (cut_k || cut_p) {
             for (int i = t; i < BINS; i += THREADS) room.mass[i] = 0;
@@ -510,7 +510,7 @@ template <int THREADS, int SEGMENT, typename T> __global__ void __launch_bounds_
         }
         u64 run = above + block.before(sum);
         const Both sums = block.both(Both{all, sum});
-        if (whole) all_mass = sums.count;
+        if (WHOLE) all_mass = sums.count;
         if (ranked) limit = share * (double)sums.mass;
         Both c{0, 0};
         for (int i = i0; i < min(i1, leading); i++) {
@@ -639,13 +639,15 @@ int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, 
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps("sample_logits", (double)n * vocab * (dtype == VLA_DTYPE_F32 ? 4.0 : 2.0), st);
     // A row of up to SHORT tokens is sorted whole, by few waves; longer ones go by bins (256 rows of 1024 tokens, 4096: sorted whole 28 and 63 us,
-    // by bins 23 and 25).  Segments of 512 ids have two loads of 16 bytes a lane on their way, and 512 of them are the longest row; shorter rows
-    // take 256, so that each of the 16 waves has some.  (1024 ids do not fit the registers: 128,000 logits 160 us for 112.)
+    // by bins 20 and 24).  Up to 8192 by eight waves, whose barriers cost less than sixteen's (1000: 20 us for 23, 8000: 26 for 27; 16,000: 31 both ways, 32,000: 45
+    // for 40).  Segments of 512 ids have two loads of 16 bytes a lane on their way, and 512 of them are the longest row; shorter rows
+    // take 256, so that each of the waves has some.  (1024 ids do not fit the registers: 128,000 logits 160 us for 112.)
     auto go = [&](auto type) {
         typedef decltype(type) T;
-        if (vocab <= SHORT) sample_rows_kernel<256, 256, T><<<n, 256, 0, st>>>(a);
-        else if (vocab <= 32768) sample_rows_kernel<1024, 256, T><<<n, 1024, 0, st>>>(a);
-        else sample_rows_kernel<1024, 512, T><<<n, 1024, 0, st>>>(a);
+        if (vocab <= SHORT) sample_rows_kernel<256, 256, true, T><<<n, 256, 0, st>>>(a);
+        else if (vocab <= 8192) sample_rows_kernel<512, 256, false, T><<<n, 512, 0, st>>>(a);
+        else if (vocab <= 32768) sample_rows_kernel<1024, 256, false, T><<<n, 1024, 0, st>>>(a);
+        else sample_rows_kernel<1024, 512, false, T><<<n, 1024, 0, st>>>(a);
     };
     if (dtype == VLA_DTYPE_F32) go(0.f);
     else go((bf16_t)0.f);
