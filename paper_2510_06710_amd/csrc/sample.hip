@@ -263,9 +263,10 @@ __device__ __forceinline__ bool falls_in(u64 run, u64 w, double want, u64 total)
     return w && (over ? run == 0 || !((double)run > want) : run + w == total);
 }
 
-// What the other ways decline (infinite logits; more than LIST tokens in one bin of a cut): each cut by bisection of the order's 50 bits, a pass
-// over the row a bit.
-template <int THREADS, typename T> __device__ void sample_by_bisection(const SampleArgs &a, const T *z, int row, u64 first, Room<THREADS> &room) {
+// What the other ways decline (infinite logits; more than LIST tokens in one bin of a cut, as where logits are flat or few values): each cut by the 50 bits of
+// the order, ten a pass over the row: the counts or masses of the tokens that agree in the higher digits, by the next one.  (256 rows of 128,000 logits
+// N(0, 0.05) with top-p: 1.0 ms; a bit a pass was some fifty such passes a cut.)
+template <int THREADS, typename T> __device__ void sample_by_digits(const SampleArgs &a, const T *z, int row, u64 first, Room<THREADS> &room) {
     const int t = threadIdx.x, V = a.vocab;
     Block<THREADS> &block = room.block;
     u64 *scan = room.mass;
@@ -286,28 +287,51 @@ template <int THREADS, typename T> __device__ void sample_by_bisection(const Sam
         }
         return block.both(b);
     };
-    // the largest threshold that holds at least what `enough` asks for; below it nothing changes what was asked
-    auto bisect = [&](auto enough) {
-        u64 lo = 1ull, hi = first;                    // enough(lo) by assumption
-        while (lo < hi) {
-            const u64 mid = lo + (hi - lo + 1) / 2;
-            if (enough(above(mid))) lo = mid; else hi = mid - 1;
+    // The largest threshold at or above which there is enough (there is in all), at most the largest key: 32 bits of order, 18 of id.
+    auto threshold = [&](bool masses, auto enough) {
+        constexpr int DIGITS = 1024, RUN = DIGITS / THREADS;
+        u64 c = 0, over = 0;                          // the digits so far; what lies above all keys that have them
+        for (int shift = 40; shift >= 0; shift -= 10) {
+            __syncthreads();
+            for (int i = t; i < DIGITS; i += THREADS) room.mass[i] = 0;
+            __syncthreads();
+            for (int i = t; i < V; i += THREADS) {
+                const float v = (float)z[i];
+                const unsigned o = order_of(v);
+                const u64 key = (u64)o << 18 | (~i & 0x3ffff);
+                if (o && key >> (shift + 10) == c) atomicAdd(&room.mass[(key >> shift) & (DIGITS - 1)], masses ? units(v) : 1ull);
+            }
+            if (t == 0) { room.found = enough(over) ? DIGITS - 1 : 0; room.found_before = over; }
+            __syncthreads();
+            u64 mine[RUN], sum = 0;                   // from the highest digit down
+#pragma unroll
+            for (int e = 0; e < RUN; e++) sum += mine[e] = room.mass[DIGITS - 1 - (t * RUN + e)];
+            u64 run = over + block.before(sum);
+#pragma unroll
+            for (int e = 0; e < RUN; e++) {
+                if (enough(run + mine[e]) && !enough(run)) { room.found = DIGITS - 1 - (t * RUN + e); room.found_before = run; }
+                run += mine[e];
+            }
+            __syncthreads();
+            c = c << 10 | (unsigned)room.found;
+            over = room.found_before;
         }
-        return lo;
+        const u64 key = (c >> 18) << 32 | 0xfffc0000u | (c & 0x3ffff);
+        return key < first ? key : first;
     };
     const Both all = above(1);
     u64 cut = 1, leading = all.mass;
     if (infinite) cut = (u64)order_of(INFINITY) << 32;
     const int k = a.top_k ? a.top_k[row] : 0;
     if (k > 0 && (u64)k < all.count) {
-        const u64 c = bisect([&](Both b) { return b.count >= (u64)k; });
+        const u64 c = threshold(false, [&](u64 count) { return count >= (u64)k; });
         cut = c > cut ? c : cut;
         leading = above(cut).mass;
     }
     const float p = a.top_p ? a.top_p[row] : 1.f;
     if (p < 1.f) {
         const double want = (double)(p > 0.f ? p : 0.f) * (double)leading;
-        const u64 c = bisect([&](Both b) { return (double)b.mass >= want; });
+        const u64 c = threshold(true, [&](u64 mass) { return (double)mass >= want; });
         cut = c > cut ? c : cut;
     }
     const float least = fminf(a.min_p ? a.min_p[row] : 0.f, 1.f);
@@ -405,7 +429,7 @@ template <int THREADS, int SEGMENT, bool WHOLE, typename T> __global__ void __la
         return;
     }
     const float zmax = value_at(first);
-    if (zmax == INFINITY) { sample_by_bisection<THREADS>(a, z, row, first, room); return; }
+    if (zmax == INFINITY) { sample_by_digits<THREADS>(a, z, row, first, room); return; }
     const bool greedy = !(T0 > 0.f) || !a.u;
     const Scale sc{(double)zmax, 1.4426950408889634074 * TABLE / (T0 > 0.f ? (double)T0 : 1.0), room.table};
     if (k <= 0 || k >= valid) k = valid;
@@ -493,7 +517,7 @@ template <int THREADS, int SEGMENT, bool WHOLE, typename T> __global__ void __la
         }
         __syncthreads();
         const int m = room.n;
-        if (m > LIST) { sample_by_bisection<THREADS>(a, z, row, first, room); return; }
+        if (m > LIST) { sample_by_digits<THREADS>(a, z, row, first, room); return; }
         while (P < m) P <<= 1;
         for (int i = m + t; i < P; i += THREADS) room.keys[i] = 0;
     }

@@ -95,3 +95,12 @@ def test_wide_ranges():
     s = positive(mixed(n, 9))
     s["temperature"] = np.where(np.arange(n) % 2, 1e-3, 100.0)
     run(r.standard_normal((n, vocab)) * 3, s)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_flat_logits(dtype):
+    """More tokens in one step of the value than are sorted."""
+    n, vocab = 12, 100003
+    s = positive(mixed(n, 11))
+    s["top_k"] = np.where(np.arange(n) % 2, 20000, 0)
+    run(np.random.default_rng(12).standard_normal((n, vocab)) * 0.05, s, dtype)
