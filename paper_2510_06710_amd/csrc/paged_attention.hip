@@ -14,8 +14,9 @@
 // part of its own, whose packed rows are those of the whole batch.
 //
 // Weights are exp2 of scores in units of log2 e; the reference of a row moves only when its maximum has grown by more than 2^8, so
-// sums stay below 2^8 times the count and most tiles rescale nothing.  P is rounded to bf16 once (relative 2^-8 of each weight, as the
-// tolerances count it; the sum that divides is that of the unrounded weights).
+// sums stay below 2^8 times the count and most tiles rescale nothing.  A weight enters the product with a bf16 V as a bf16 head and a bf16 tail (2^-16
+// of it is lost, as in attn_mfma.hip), the sum that divides is that of the fp32 weights.  With the head alone outputs were off by 1.4 times what their own rounding
+// costs (rms 0.0023 of them for 0.0017); the tail's product takes a prompt from 550 to 745 us and a decode step, which waits for memory, 1 % longer.
 #include "paged.h"
 
 #include <type_traits>
@@ -187,7 +188,15 @@ __device__ __forceinline__ Query make_query(const AttnArgs &a, int kvh, int s, i
 template <typename T, int DP, int MODE> struct Rows {
     typedef typename FragOf<T>::type frag;
     typedef Tile<T, DP> TL;
-    static constexpr int KS = DP / 16, DB = DP / 32;
+    static constexpr int KS = DP / 16, DB = DP / 32, HALVES = sizeof(T) == 2 ? 2 : 1;
+    // A lane's weights of a tile as matrix operands: bf16 head and bf16 tail, or the fp32 weights.
+    struct Weights {
+        frag p[HALVES][2];
+        __device__ __forceinline__ void put(int i, float w) {
+            p[0][i / 8][i % 8] = (T)w;
+            if constexpr (HALVES == 2) p[1][i / 8][i % 8] = (T)(w - (float)p[0][i / 8][i % 8]);
+        }
+    };
     frag q[KS];
     f32x16_t o[DB];
     float m, l;
@@ -243,7 +252,7 @@ template <typename T, int DP, int MODE> struct Rows {
     }
     // scores(next, kt) and weights(p, x) in turn: a matrix instruction, then the vector work it covers (left to itself the compiler
     // puts all of the one before all of the other).  The operands come out of LDS three instructions ahead.
-    __device__ __forceinline__ void scores_and_weights(f32x16_t &next, const char *kt, frag (&p)[2], const f32x16_t &x, float unit) {
+    __device__ __forceinline__ void scores_and_weights(f32x16_t &next, const char *kt, Weights &p, const f32x16_t &x, float unit) {
         constexpr int EACH = 16 / KS, AHEAD = KS < 3 ? KS : 3;
         const float ref = m == -INFINITY ? 0.f : m;
         frag k[AHEAD];
@@ -260,25 +269,26 @@ template <typename T, int DP, int MODE> struct Rows {
             for (int i = kk * EACH; i < (kk + 1) * EACH; i++) {
                 const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, -ref));
                 l += w;
-                p[i / 8][i % 8] = (T)w;
+                p.put(i, w);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
     }
-    // values(p, vt), and in its cover shape and the largest of `next`.
-    __device__ __forceinline__ float values_and_largest(const frag (&p)[2], const char *vt, f32x16_t &next, const AttnArgs &a, const Query &y, int key0) {
-        constexpr int N = 2 * DB, EACH = (16 + N - 1) / N, AHEAD = 3;
+    // values(p, vt), and in its cover shape and the largest of `next`.  Two products by heads, then the same two by tails: none waits for the one before it.
+    __device__ __forceinline__ float values_and_largest(const Weights &p, const char *vt, f32x16_t &next, const AttnArgs &a, const Query &y, int key0) {
+        constexpr int N = 2 * DB, EACH = (16 + N * HALVES - 1) / (N * HALVES), AHEAD = 4;
         frag v[AHEAD];
         float top = -INFINITY;
 #pragma unroll
         for (int s = 0; s < AHEAD; s++) v[s] = value(vt, s / DB, s % DB);
 #pragma unroll
-        for (int s = 0; s < N; s++) {
+        for (int n = 0; n < N * HALVES; n++) {
+            const int half = n / 2 % HALVES, s = n / (2 * HALVES) * 2 + n % 2;
             __builtin_amdgcn_sched_barrier(0);
-            o[s % DB] = mma(v[s % AHEAD], p[s / DB], o[s % DB]);
-            if (s + AHEAD < N) v[s % AHEAD] = value(vt, (s + AHEAD) / DB, (s + AHEAD) % DB);
+            o[s % DB] = mma(v[s % AHEAD], p.p[half][s / DB], o[s % DB]);
+            if (half == HALVES - 1 && s + AHEAD < N) v[s % AHEAD] = value(vt, (s + AHEAD) / DB, (s + AHEAD) % DB);
 #pragma unroll
-            for (int i = s * EACH; i < (s + 1) * EACH && i < 16; i++) {
+            for (int i = n * EACH; i < (n + 1) * EACH && i < 16; i++) {
                 next[i] = shaped(next[i], a, y, key0, i);
                 top = fmaxf(top, next[i]);
             }
@@ -336,13 +346,13 @@ template <typename T, int DP, int MODE> struct Rows {
             m = to;
         }
     }
-    __device__ __forceinline__ void weights(frag (&p)[2], const f32x16_t &x, float unit) {
+    __device__ __forceinline__ void weights(Weights &p, const f32x16_t &x, float unit) {
         const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int i = 0; i < 16; i++) {
             const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], unit, -ref));
             l += w;
-            p[i / 8][i % 8] = (T)w;
+            p.put(i, w);
         }
     }
     __device__ __forceinline__ static frag value(const char *vt, int u, int b) {
@@ -361,16 +371,20 @@ template <typename T, int DP, int MODE> struct Rows {
         }
         return v;
     }
-    __device__ __forceinline__ void values(const frag (&p)[2], const char *vt) {
+    __device__ __forceinline__ void values(const Weights &p, const char *vt) {
 #pragma unroll
         for (int u = 0; u < 2; u++)
 #pragma unroll
-            for (int b = 0; b < DB; b++) o[b] = mma(value(vt, u, b), p[u], o[b]);
+            for (int b = 0; b < DB; b++) {
+                const frag v = value(vt, u, b);
+#pragma unroll
+                for (int half = 0; half < HALVES; half++) o[b] = mma(v, p.p[half][u], o[b]);
+            }
     }
     // masked: some query may not see some key.
     __device__ __forceinline__ void tile(const AttnArgs &a, const Query &y, const char *kt, const char *vt, int key0, bool masked) {
         f32x16_t x;
-        frag p[2];
+        Weights p;
         scores(x, kt);
 #pragma unroll
         for (int i = 0; i < 16; i++) x[i] = shaped(x[i], a, y, key0, i);
@@ -483,9 +497,9 @@ __device__ __forceinline__ bool sees_all(const Query &y, int k0, int k1) { retur
 // Four waves of 32 packed rows each, all walking the same keys, 32 at a time.  K and V move through rings of RING tiles, K one tile before V: while
 // tile t's weights are formed on the vector units its successor's scores are on the matrix pipe, instruction by instruction in turn,
 // and while its values are summed the successor's largest is found.
-// Bound by the matrix pipe and the vector work beside it: 8192 causal rows of 32 heads of 128, 8 key heads: 530 us, 1.04 PFLOP/s where a plain matrix
-// product reaches 1.39 on this card; heads of 64: 340 us, of 256: 1.35 ms; capped 640; fp32, 2048 rows, heads of 64: 320 us, 107 of 154 TFLOP/s.  (Scores and
-// weights one after the other: 637 us; in turn, but every step with its checks: 654.)  A ragged batch of 13 chunks of up to 613 rows: 32 us, a few rounds of
+// Bound by the matrix pipe and the vector work beside it: 8192 causal rows of 32 heads of 128, 8 key heads: 745 us, 1.11 PFLOP/s of matrix instructions (three
+// products, of which the tail's is one) where a plain matrix product reaches 1.39 on this card; heads of 64: 457 us, of 256: 1.71 ms; capped 820; fp32, 2048 rows, heads of 64: 320 us, 107 of 154 TFLOP/s.  (Before the tail 530, with scores and
+// weights one after the other 637, in turn but every step with its checks 654.)  A ragged batch of 13 chunks of up to 613 rows: 39 us, a few rounds of
 // workgroups, each with its chain of dependent loads.
 constexpr int LDS_STARTS = 2048;
 template <typename T, int DP> constexpr int RING = 32 * Tile<T, DP>::ROW * 8 <= 64 * 1024 ? 4 : 2;
@@ -559,7 +573,7 @@ __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_prom
         float top = R::largest(x, unit);
         int t = t0;
         size_t at_v = place.at(a.pv, page_v, (t0 + RG - 1) * KT + g * 16);          // of the 16 keys whose V comes next
-        typename R::frag p[2];
+        typename R::Weights p;
         // plain steps, from `from` to before `upto`: everything is there to load, whole, and all see all of tile t + 1
         const int from = max(in0, seen0), upto = min(min(in1, t1) - RG - 1, seen1 - 1);
         // The step of tile t, in the stage of that number (a constant: what lies where is known when this is compiled)
@@ -644,7 +658,7 @@ struct Walk {
 // their lengths, and streams through it, the next tile on its way whether it is of the same sequence or not.  A sequence's tiles that
 // fall to several waves leave parts for the join (a wave has at most two: of the sequence it begins within, and of the one it ends within).
 // Neighbouring waves have the same run of different heads, whose rows lie side by side in the pages.
-// Memory bound: 32 sequences of 2048 keys, 32 heads, 192 us, 5.6 TB/s; 256 of 294 keys 226 us, 5.5; one of 32768 keys, 8 key heads, 26 us and 6 for
+// Memory bound: 32 sequences of 2048 keys, 32 heads, 192 us, 5.6 TB/s; 256 of 294 keys 229 us, 5.4; one of 32768 keys, 8 key heads, 26 us and 6 for
 // the join of 128 parts; 48 ragged ones of up to 8192 keys with capped scores and a bias 79 us.  (One workgroup of 1, 2 or 4 waves per sequence,
 // key head and even part of max_len: 200, 259, 30 + 5 and 125 to 155 us.)
 template <typename T, int DP, int MODE>
