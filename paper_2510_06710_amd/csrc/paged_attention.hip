@@ -185,6 +185,9 @@ __device__ __forceinline__ Query make_query(const AttnArgs &a, int kvh, int s, i
     return q;
 }
 
+// ln of a row's sum of exponentials; -inf where it sees no key.
+__device__ __forceinline__ float lse_of(const AttnArgs &a, float m, float sum) { return sum == 0.f ? -INFINITY : (m + a.offset + log2f(sum)) * 0.6931471805599453f; }
+
 template <typename T, int DP, int MODE> struct Rows {
     typedef typename FragOf<T>::type frag;
     typedef Tile<T, DP> TL;
@@ -394,10 +397,10 @@ template <typename T, int DP, int MODE> struct Rows {
         values(p, vt);
     }
 
-    // A part's sums.
+    // A part's sums.  (It is empty where its sum is zero: a sum that is no number belongs to the output.)
     __device__ __forceinline__ void keep(const AttnArgs &a, float2 *ml, float *dst, float sum, int hh) {
         if (hh == 0) *ml = make_float2(m, sum);
-        if (!(sum > 0.f)) return;                            // (the join reads nothing of an empty part)
+        if (sum == 0.f) return;                              // (the join reads nothing of an empty part)
 #pragma unroll
         for (int b = 0; b < DB; b++)
 #pragma unroll
@@ -416,8 +419,8 @@ template <typename T, int DP, int MODE> struct Rows {
             keep(a, a.ml + slot, a.o_part + slot * d, sum, hh);
             return;
         }
-        const float f = sum > 0.f ? 1.f / sum : 0.f;
-        if (a.lse && hh == 0) a.lse[at] = sum > 0.f ? (m + a.offset + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        const float f = sum == 0.f ? 0.f : 1.f / sum;
+        if (a.lse && hh == 0) a.lse[at] = lse_of(a, m, sum);
         T *dst = (T *)a.out + y.row * a.o_stride + (size_t)y.head * d;
 #pragma unroll
         for (int b = 0; b < DB; b++)
@@ -770,6 +773,7 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(AttnArgs a) {
 // DP / 4 lanes a part, so 1024 / DP parts at a time, whose sums are added in one order.  (One wave and part after part: 41 us for 64 parts of 32
 // pairs, a memory latency each.)  The parts of all rows' layout (ml, o_part) come first, then those of the waves that shared the sequence.
 constexpr int FEW = 4;
+constexpr float EMPTY = -1.f;                    // of a part without a visible key, where weights stand
 constexpr int JOIN_PARTS = 2048 + 512;          // of waves, and of own and shared ranges, at most
 template <typename T, int DP>
 __global__ void __launch_bounds__(256) paged_join_kernel(AttnArgs a) {
@@ -811,17 +815,17 @@ __global__ void __launch_bounds__(256) paged_join_kernel(AttnArgs a) {
             }
 #pragma unroll
             for (int z = 0; z < FEW; z++) {
-                const float f = ml[z].y > 0.f ? __builtin_amdgcn_exp2f(ml[z].x - top) : 0.f;
+                const float f = ml[z].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[z].x - top);
                 sum += f * ml[z].y;
 #pragma unroll
-                for (int e = 0; e < 4; e++) o[e] += f > 0.f ? f * v[z][e] : 0.f;
+                for (int e = 0; e < 4; e++) o[e] += ml[z].y == 0.f ? 0.f : f * v[z][e];          // (an empty part has no sums, whatever lies there)
             }
             if (dim >= d) continue;
-            const float f = sum > 0.f ? 1.f / sum : 0.f;
+            const float f = sum == 0.f ? 0.f : 1.f / sum;
             T *dst = (T *)a.out + row * a.o_stride + (size_t)h * d + dim;
 #pragma unroll
             for (int e = 0; e < 4; e++) dst[e] = (T)(o[e] * f);
-            if (a.lse && dim == 0) a.lse[(size_t)row * a.n_heads + h] = sum > 0.f ? (top + a.offset + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+            if (a.lse && dim == 0) a.lse[(size_t)row * a.n_heads + h] = lse_of(a, top, sum);
         }
         return;
     }
@@ -834,9 +838,9 @@ __global__ void __launch_bounds__(256) paged_join_kernel(AttnArgs a) {
         __syncthreads();
         for (int z = lane; z < total; z += 64) {
             const float2 v = ml_of(z);
-            const float f = v.y > 0.f ? __builtin_amdgcn_exp2f(v.x - top) : 0.f;
+            const float f = v.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(v.x - top);
             sum += f * v.y;
-            if (t < 64) weights[z] = f;
+            if (t < 64) weights[z] = v.y == 0.f ? EMPTY : f;
         }
         sum = vla_wave_sum(sum);
         __syncthreads();
@@ -847,7 +851,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(AttnArgs a) {
                 const float f = weights[z];
                 const f32x4_t v = sums_at(h, z);
 #pragma unroll
-                for (int e = 0; e < 4; e++) o[e] += f > 0.f ? f * v[e] : 0.f;          // (an empty part has no sums, whatever lies there)
+                for (int e = 0; e < 4; e++) o[e] += f == EMPTY ? 0.f : f * v[e];
             }
         sums[t] = o;
         __syncthreads();
@@ -857,11 +861,11 @@ __global__ void __launch_bounds__(256) paged_join_kernel(AttnArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; e++) o[e] += v[e];
             }
-            const float f = sum > 0.f ? 1.f / sum : 0.f;
+            const float f = sum == 0.f ? 0.f : 1.f / sum;
             T *dst = (T *)a.out + row * a.o_stride + (size_t)h * d + dim;
 #pragma unroll
             for (int e = 0; e < 4; e++) dst[e] = (T)(o[e] * f);
-            if (a.lse && t == 0) a.lse[at] = sum > 0.f ? (top + a.offset + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+            if (a.lse && t == 0) a.lse[at] = lse_of(a, top, sum);
         }
     }
 }
