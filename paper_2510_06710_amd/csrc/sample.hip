@@ -114,10 +114,6 @@ struct Scale {
     __device__ __forceinline__ u64 units(float z) const { return units_of(weight(z)); }
     // one bin per step, never descending in -z; below 2^-63 all one
     __device__ __forceinline__ int bin_of(const Steps &s) const { return min(-s.k, BINS - 1); }
-    // w to within 1e-7, where only the logarithm of many of them is wanted
-    __device__ __forceinline__ float rough(const Steps &s) const {
-        return __builtin_ldexpf(__builtin_amdgcn_exp2f((float)(s.v - s.n) * (1.f / TABLE) + (float)(s.k & (TABLE - 1)) * (1.f / TABLE)), max(s.k >> 5, -200));
-    }
 };
 __device__ __forceinline__ void fill_table(double *table) {
     for (int j = threadIdx.x; j < TABLE; j += blockDim.x) table[j] = j == 0 ? 1.0 : 2.0 * exp2_neg((double)j / TABLE - 1.0);
@@ -446,14 +442,13 @@ template <int THREADS, int SEGMENT, bool WHOLE, typename T> __global__ void __la
             for (int i = t; i < BINS; i += THREADS) room.mass[i] = 0;
             __syncthreads();
             if (cut_k) {
-                // (of the row's mass only logp wants the logarithm: in fp64 sums of fp32 exponentials, in one order)
-                double all = 0.0;
+                u64 all = 0;                         // (of the row, for logp: the same whole numbers whatever the cuts are)
                 each_token<THREADS, SEGMENT>(z, V, [&](float v, int, int) {
                     const auto y = sc.steps(v);
-                    all += (double)sc.rough(y);
+                    all += units_of(sc.weight_of(y));
                     atomicAdd(&room.count[sc.bin_of(y)], v > -INFINITY ? 1u : 0u);
                 });
-                all_mass = block.both(Both{0, (u64)(all * UNIT)}).mass;
+                all_mass = block.both(Both{0, all}).mass;
             } else
                 each_token<THREADS, SEGMENT>(z, V, [&](float v, int, int) {
                     const auto y = sc.steps(v);
