@@ -106,11 +106,15 @@ class Rollout:
 class PagedRollout:
     """Rollouts of environments whose prefixes have any lengths, on a paged cache of ``n_pages`` pages a layer: one ragged prefill, then
     action tokens sampled with top-k, top-p and min-p.  Pages are taken from the free ones as sequences grow; a prefill frees all.  Work goes to
-    ``stream``, or to the current one; one that is not the last call's, or the one the arguments were made on, has to wait for it first."""
+    ``stream``, or to the current one; one that is not the last call's, or the one the arguments were made on, has to wait for it first.
+    Several on one ``run`` share its weights alone: their calls may overlap on different streams."""
+
+    _buf = Rollout._buf
 
     def __init__(self, run: Rollout, n_pages: int, page_size: int = 16):
         s = run.shape
         self.run, self.page_size = run, page_size
+        self.device, self._bufs = run.device, {}
         self.pools = [torch.zeros(s.n_layers, n_pages, s.n_heads, page_size, s.head_dim, dtype=s.torch_dtype, device=run.device) for _ in range(2)]
         self.cache = vb.make_paged_cache(self.pools[0][0], self.pools[1][0])
         self.layer_stride = self.pools[0][0].numel()
@@ -145,7 +149,7 @@ class PagedRollout:
             starts.append(starts[-1] + n)
         batch = vb.make_paged_batch(self._int(starts), self._int([self.length[s] for s in seqs]), table, starts[-1], max(rows),
                                     max(self.length[s] for s in seqs))
-        ws = run._buf("ws_paged", vb.vla_forward_paged_workspace_bytes(run.cfg, self.cache, batch, shared_len))
+        ws = self._buf("ws_paged", vb.vla_forward_paged_workspace_bytes(run.cfg, self.cache, batch, shared_len))
         h = torch.empty(len(seqs), run.shape.hidden, dtype=torch.float32, device=dev)
         logits = torch.empty(len(seqs), vb.VLA_N_BINS, dtype=torch.float32, device=dev)
         value = run._value_out(len(seqs)) if want_value else None
@@ -199,7 +203,7 @@ class PagedRollout:
         run, n, dev = self.run, logits.shape[0], self.run.device
         every = lambda v, dtype: torch.full((n,), v, dtype=dtype, device=dev)
         t, k, p, least = every(temperature, torch.float32), every(top_k, torch.int32), every(top_p, torch.float32), every(min_p, torch.float32)
-        ws = run._buf("ws_sample", vb.vla_sample_logits_workspace_bytes(n, vb.VLA_N_BINS))
+        ws = self._buf("ws_sample", vb.vla_sample_logits_workspace_bytes(n, vb.VLA_N_BINS))
         out = [[], [], [], []]
         for j in range(n_tokens):
             bins, logp, kept = (torch.empty(n, dtype=d, device=dev) for d in (torch.int32, torch.float32, torch.float32))
