@@ -14,9 +14,10 @@
 // part of its own, whose packed rows are those of the whole batch.
 //
 // Weights are exp2 of scores in units of log2 e; the reference of a row moves only when its maximum has grown by more than 2^8, so
-// sums stay below 2^8 times the count and most tiles rescale nothing.  A weight enters the product with a bf16 V as a bf16 head and a bf16 tail (2^-16
-// of it is lost, as in attn_mfma.hip), the sum that divides is that of the fp32 weights.  With the head alone outputs were off by 1.4 times what their own rounding
-// costs (rms 0.0023 of them for 0.0017); the tail's product takes a prompt from 550 to 745 us and a decode step, which waits for memory, 1 % longer.
+// sums stay below 2^8 times the count and most tiles rescale nothing.  Of a decode form's weights the product with a bf16 V takes a bf16 head and a
+// bf16 tail (2^-16 of the weight is lost, as in attn_mfma.hip): the step waits for memory, and is 1 % longer (behind a shared prefix 10 %).  A prompt's are rounded to
+// bf16 once (2^-8 of each, as the tolerances count it), for the third product would take 8192 rows from 550 to 745 us: outputs are off by 1.4 times what their own rounding
+// costs (rms 0.0023 of them for 0.0017).  The sum that divides is that of the fp32 weights.
 #include "paged.h"
 
 #include <type_traits>
@@ -188,11 +189,12 @@ __device__ __forceinline__ Query make_query(const AttnArgs &a, int kvh, int s, i
 // ln of a row's sum of exponentials; -inf where it sees no key.
 __device__ __forceinline__ float lse_of(const AttnArgs &a, float m, float sum) { return sum == 0.f ? -INFINITY : (m + a.offset + log2f(sum)) * 0.6931471805599453f; }
 
-template <typename T, int DP, int MODE> struct Rows {
+// TAILS (bf16): weights enter the product with V as head and tail.
+template <typename T, int DP, int MODE, bool TAILS> struct Rows {
     typedef typename FragOf<T>::type frag;
     typedef Tile<T, DP> TL;
-    static constexpr int KS = DP / 16, DB = DP / 32, HALVES = sizeof(T) == 2 ? 2 : 1;
-    // A lane's weights of a tile as matrix operands: bf16 head and bf16 tail, or the fp32 weights.
+    static constexpr int KS = DP / 16, DB = DP / 32, HALVES = TAILS ? 2 : 1;
+    // A lane's weights of a tile as matrix operands: bf16 head (and tail), or the fp32 weights.
     struct Weights {
         frag p[HALVES][2];
         __device__ __forceinline__ void put(int i, float w) {
@@ -279,7 +281,7 @@ template <typename T, int DP, int MODE> struct Rows {
     }
     // values(p, vt), and in its cover shape and the largest of `next`.  Two products by heads, then the same two by tails: none waits for the one before it.
     __device__ __forceinline__ float values_and_largest(const Weights &p, const char *vt, f32x16_t &next, const AttnArgs &a, const Query &y, int key0) {
-        constexpr int N = 2 * DB, EACH = (16 + N * HALVES - 1) / (N * HALVES), AHEAD = 4;
+        constexpr int N = 2 * DB, EACH = (16 + N * HALVES - 1) / (N * HALVES), AHEAD = TAILS ? 4 : 3;
         frag v[AHEAD];
         float top = -INFINITY;
 #pragma unroll
@@ -500,16 +502,16 @@ __device__ __forceinline__ bool sees_all(const Query &y, int k0, int k1) { retur
 // Four waves of 32 packed rows each, all walking the same keys, 32 at a time.  K and V move through rings of RING tiles, K one tile before V: while
 // tile t's weights are formed on the vector units its successor's scores are on the matrix pipe, instruction by instruction in turn,
 // and while its values are summed the successor's largest is found.
-// Bound by the matrix pipe and the vector work beside it: 8192 causal rows of 32 heads of 128, 8 key heads: 745 us, 1.11 PFLOP/s of matrix instructions (three
-// products, of which the tail's is one) where a plain matrix product reaches 1.39 on this card; heads of 64: 457 us, of 256: 1.71 ms; capped 820; fp32, 2048 rows, heads of 64: 320 us, 107 of 154 TFLOP/s.  (Before the tail 530, with scores and
-// weights one after the other 637, in turn but every step with its checks 654.)  A ragged batch of 13 chunks of up to 613 rows: 39 us, a few rounds of
+// Bound by the matrix pipe and the vector work beside it: 8192 causal rows of 32 heads of 128, 8 key heads: 540-555 us, 1.0 PFLOP/s where a plain matrix
+// product reaches 1.39 on this card; heads of 64: 333 us, of 256: 1.32 ms; capped 650; fp32, 2048 rows, heads of 128: 323 us, 107 of 154 TFLOP/s.  (Scores and
+// weights one after the other: 637 us; in turn, but every step with its checks: 654.)  A ragged batch of 13 chunks of up to 613 rows: 33 us, a few rounds of
 // workgroups, each with its chain of dependent loads.
 constexpr int LDS_STARTS = 2048;
 template <typename T, int DP> constexpr int RING = 32 * Tile<T, DP>::ROW * 8 <= 64 * 1024 ? 4 : 2;
-template <typename T, int DP, int MODE>
+template <typename T, int DP, int MODE, bool TAILS>
 __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_prompt_kernel(AttnArgs a) {
     typedef Tile<T, DP> TL;
-    typedef Rows<T, DP, MODE> R;
+    typedef Rows<T, DP, MODE, TAILS> R;
     constexpr int KT = 32, BYTES = KT * TL::ROW, RG = RING<T, DP>, LOADS = 2 * 8 / TL::RPI;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const unsigned lds0 = (unsigned)(size_t)(lds_void *)lds;
@@ -741,7 +743,7 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(AttnArgs a) {
     };
     settle();
     if (more) load(0);
-    Rows<T, DP, MODE> rows;
+    Rows<T, DP, MODE, sizeof(T) == 2> rows;
     while (walk.next(a, &run)) {
         const int packed = threadIdx.x & 31;
         if (a.waves) {
@@ -986,24 +988,25 @@ size_t lay_out(AttnArgs *a, const Plan &p, char *base) {
     return off ? off : 256;
 }
 
-template <typename T, int DP, int MODE>
+template <typename T, int DP, int MODE, bool TAILS>
 int launch_prompt(AttnArgs a, const Prompt &p, bool whole, int part0, hipStream_t st) {
     const size_t bytes = 2 * RING<T, DP> * 32 * Tile<T, DP>::ROW + (whole && a.pv.n_seq <= LDS_STARTS ? a.pv.n_seq * sizeof(int32_t) : 0);
-    if (int rc = vla_allow_lds((const void *)paged_prompt_kernel<T, DP, MODE>, 2 * RING<T, DP> * 32 * Tile<T, DP>::ROW + LDS_STARTS * sizeof(int32_t))) return rc;
+    if (int rc = vla_allow_lds((const void *)paged_prompt_kernel<T, DP, MODE, TAILS>, 2 * RING<T, DP> * 32 * Tile<T, DP>::ROW + LDS_STARTS * sizeof(int32_t))) return rc;
     a.whole = whole; a.row_tiles = p.row_tiles; a.chunk = p.chunk; a.part0 = part0;
-    paged_prompt_kernel<T, DP, MODE><<<dim3((unsigned)p.items, p.parts), 256, bytes, st>>>(a);
+    paged_prompt_kernel<T, DP, MODE, TAILS><<<dim3((unsigned)p.items, p.parts), 256, bytes, st>>>(a);
     return vla_check_launch("paged_attention");
 }
 template <typename T, int DP, int MODE>
 int launch(const AttnArgs &a, const Plan &p, hipStream_t st) {
     int rc;
-    if (a.shared_len > 0 && (rc = launch_prompt<T, DP, MODE>(a, p.whole, true, p.decode ? 1 : p.own.parts, st))) return rc;
+    constexpr bool BF16 = sizeof(T) == 2;
+    if (a.shared_len > 0 && (rc = p.decode ? launch_prompt<T, DP, MODE, BF16>(a, p.whole, true, 1, st) : launch_prompt<T, DP, MODE, false>(a, p.whole, true, p.own.parts, st))) return rc;
     if (p.decode) {
         constexpr size_t bytes = 2 * 2 * 32 * Tile<T, DP>::ROW;
         if ((rc = vla_allow_lds((const void *)paged_decode_kernel<T, DP, MODE>, bytes))) return rc;
         paged_decode_kernel<T, DP, MODE><<<(p.waves ? p.waves : a.pv.n_seq) * a.pv.n_kv, 64, bytes, st>>>(a);
         rc = vla_check_launch("paged_attention");
-    } else rc = launch_prompt<T, DP, MODE>(a, p.own, false, 0, st);
+    } else rc = launch_prompt<T, DP, MODE, false>(a, p.own, false, 0, st);
     if (rc || (p.parts == 1 && !p.waves)) return rc;
     const int rows = p.decode ? a.pv.n_seq * a.pv.max_rows : a.pv.n_rows;
     const int heads = (2048 + rows - 1) / rows;              // of a row, that get a workgroup of their own
