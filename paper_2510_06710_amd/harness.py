@@ -109,7 +109,11 @@ class PagedRollout:
     ``stream``, or to the current one; one that is not the last call's, or the one the arguments were made on, has to wait for it first.
     Several on one ``run`` share its weights alone: their calls may overlap on different streams."""
 
-    _buf = Rollout._buf
+    def _buf(self, name, nbytes):
+        t = Rollout._buf(self, name, nbytes)
+        if t.is_cuda:                                        # (of the stream it was made on: not given out there before this one is through with it)
+            t.record_stream(torch.cuda.current_stream(self.device))
+        return t
 
     def __init__(self, run: Rollout, n_pages: int, page_size: int = 16):
         s = run.shape

@@ -25,3 +25,18 @@ def test_two_rollouts_of_one_model_at_once():
         together = [go(i, streams[i]) for i in range(2)]
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for i in range(2) for a, b in zip(alone[i], together[i]))
+
+
+def test_a_workspace_in_use_elsewhere_is_not_given_out():
+    run, obs, _, _ = setup("bf16", [(48, 21), (5, 3)])
+    paged, stream = PagedRollout(run, 32), torch.cuda.Stream()
+    logits = paged.prefill([p for p, _ in obs], [t for _, t in obs])[1]          # the workspace comes from the current stream's memory
+    torch.cuda.synchronize()
+    paged.decode(logits, 2, stream=stream)
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(100_000_000)                       # the stream is not through with it ...
+    size, place = paged._bufs["ws_paged"].numel(), paged._bufs["ws_paged"].data_ptr()
+    paged._bufs.clear()                                      # ... when a larger one takes its place
+    fresh = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    assert all(t.data_ptr() != place for t in fresh)
+    torch.cuda.synchronize()
