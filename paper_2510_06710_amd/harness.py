@@ -105,7 +105,8 @@ class Rollout:
 
 class PagedRollout:
     """Rollouts of environments whose prefixes have any lengths, on a paged cache of ``n_pages`` pages a layer: one ragged prefill, then
-    action tokens sampled with top-k, top-p and min-p.  Pages are taken from the free ones as sequences grow; a prefill frees all.  Work goes to
+    action tokens sampled with top-k, top-p and min-p.  Pages are taken from the free ones as sequences grow; a prefill frees all.  A call that is refused
+    changes nothing: the sequences that are there go on.  Work goes to
     ``stream``, or to the current one; one that is not the last call's, or the one the arguments were made on, has to wait for it first.
     Several on one ``run`` share its weights alone: their calls may overlap on different streams."""
 
@@ -123,11 +124,27 @@ class PagedRollout:
         self.cache = vb.make_paged_cache(self.pools[0][0], self.pools[1][0])
         self.layer_stride = self.pools[0][0].numel()
         self.n_pages = n_pages
-        self._start(0)
+        self.shared_len = 0
+        self._hold(self._fresh(0))
 
-    def _start(self, n_seq):
-        self.free = list(range(self.n_pages - 1, -1, -1))
-        self.pages, self.length, self.shared_len = [[] for _ in range(n_seq)], [0] * n_seq, 0
+    def _fresh(self, n_seq):
+        """Of n_seq sequences without a position: their pages, their lengths, the free pages."""
+        return [[] for _ in range(n_seq)], [0] * n_seq, list(range(self.n_pages - 1, -1, -1))
+
+    def _hold(self, held):
+        self.pages, self.length, self.free = held
+
+    def _grown(self, held, seqs, rows):
+        """`held` with rows[i] more positions for seqs[i]; what is given stays as it is."""
+        pages, length, free = (list(x) for x in held)
+        wanted = [max(0, -(-(length[s] + n) // self.page_size) - len(pages[s])) for s, n in zip(seqs, rows)]
+        if sum(wanted) > len(free):
+            raise ValueError(f"{sum(wanted)} pages wanted, {len(free)} of {self.n_pages} free")
+        for s, n, more in zip(seqs, rows, wanted):
+            length[s] += n
+            if more:
+                pages[s] = pages[s] + [free.pop() for _ in range(more)]
+        return pages, length, free
 
     def _int(self, values):
         return torch.tensor(values, dtype=torch.int32, device=self.run.device)
@@ -137,28 +154,31 @@ class PagedRollout:
         with torch.cuda.stream(stream):
             return self._forward(seqs, ids, rows, patch, prefix_len, shared_len, want_value)
 
-    def _forward(self, seqs, ids, rows, patch=None, prefix_len=None, shared_len=0, want_value=False):
-        run, dev = self.run, self.run.device
-        wanted = sum(max(0, (self.length[s] + n + self.page_size - 1) // self.page_size - len(self.pages[s])) for s, n in zip(seqs, rows))
-        if wanted > len(self.free):
-            raise ValueError(f"{wanted} pages wanted, {len(self.free)} of {self.n_pages} free")
-        for s, n in zip(seqs, rows):
-            self.length[s] += n
-            while len(self.pages[s]) * self.page_size < self.length[s]:
-                self.pages[s].append(self.free.pop())
-        entries = max(len(self.pages[s]) for s in seqs)
-        table = self._int([self.pages[s] + [-1] * (entries - len(self.pages[s])) for s in seqs])
+    def _plan(self, held, seqs, rows, shared_len):
+        """The batch of new rows for seqs as `held` has them, and the workspace it takes: all that can be refused of it for its sizes."""
+        pages, length, _ = held
+        entries = max(len(pages[s]) for s in seqs)
+        table = self._int([pages[s] + [-1] * (entries - len(pages[s])) for s in seqs])
         starts = [0]
         for n in rows:
             starts.append(starts[-1] + n)
-        batch = vb.make_paged_batch(self._int(starts), self._int([self.length[s] for s in seqs]), table, starts[-1], max(rows),
-                                    max(self.length[s] for s in seqs))
-        ws = self._buf("ws_paged", vb.vla_forward_paged_workspace_bytes(run.cfg, self.cache, batch, shared_len))
-        h = torch.empty(len(seqs), run.shape.hidden, dtype=torch.float32, device=dev)
-        logits = torch.empty(len(seqs), vb.VLA_N_BINS, dtype=torch.float32, device=dev)
-        value = run._value_out(len(seqs)) if want_value else None
-        vb.vla_forward_paged(run.model.handle, self.cache, self.layer_stride, batch, ids, ws, h, patch, prefix_len, shared_len, logits, value)
+        batch = vb.make_paged_batch(self._int(starts), self._int([length[s] for s in seqs]), table, starts[-1], max(rows), max(length[s] for s in seqs))
+        return batch, vb.vla_forward_paged_workspace_bytes(self.run.cfg, self.cache, batch, shared_len)
+
+    def _run(self, plan, ids, patch, prefix_len, shared_len, want_value):
+        run, dev = self.run, self.run.device
+        batch, ws_bytes = plan
+        h = torch.empty(batch.n_seq, run.shape.hidden, dtype=torch.float32, device=dev)
+        logits = torch.empty(batch.n_seq, vb.VLA_N_BINS, dtype=torch.float32, device=dev)
+        value = run._value_out(batch.n_seq) if want_value else None
+        vb.vla_forward_paged(run.model.handle, self.cache, self.layer_stride, batch, ids, self._buf("ws_paged", ws_bytes), h, patch, prefix_len, shared_len, logits, value)
         return h, logits, value
+
+    def _forward(self, seqs, ids, rows, patch=None, prefix_len=None, shared_len=0, want_value=False, held=None):
+        held = self._grown(held or (self.pages, self.length, self.free), seqs, rows)
+        out = self._run(self._plan(held, seqs, rows, shared_len), ids, patch, prefix_len, shared_len, want_value)
+        self._hold(held)                                     # (nothing has changed where any of this was refused)
+        return out
 
     def prefill(self, patches, ids, see_patches=False, stream=None):
         """patches[i] [P_i, hidden] (or None) and ids[i] [T_i] of environment i.  see_patches: an environment's patches see each other
@@ -169,14 +189,15 @@ class PagedRollout:
     def _prefill(self, patches, ids, see_patches=False):
         dev = self.run.device
         n_patch = [0 if p is None else p.shape[0] for p in patches]
-        self._start(len(ids))
         parts, seen = [], 0
         for n, t in zip(n_patch, ids):
             parts += [-1 - torch.arange(seen, seen + n, dtype=torch.int32, device=dev), t.to(torch.int32)]
             seen += n
-        held = [p for p in patches if p is not None and p.shape[0]]
-        return self._forward(list(range(len(ids))), torch.cat(parts), [n + t.numel() for n, t in zip(n_patch, ids)], torch.cat(held) if held else None,
-                             self._int(n_patch) if see_patches else None, 0, self.run.model._keep[4] is not None)
+        patch = [p for p in patches if p is not None and p.shape[0]]
+        out = self._forward(list(range(len(ids))), torch.cat(parts), [n + t.numel() for n, t in zip(n_patch, ids)], torch.cat(patch) if patch else None,
+                            self._int(n_patch) if see_patches else None, 0, self.run.model._keep[4] is not None, self._fresh(len(ids)))
+        self.shared_len = 0
+        return out
 
     def prefill_group(self, patch, ids, group: int, stream=None):
         """One observation for ``group`` rollouts: its whole pages are computed and kept once, what is behind them once per rollout."""
@@ -186,16 +207,23 @@ class PagedRollout:
     def _prefill_group(self, patch, ids, group):
         n = patch.shape[0] + ids.numel()
         shared = (n - 1) // self.page_size * self.page_size
-        out = self._prefill([patch], [ids])
-        if group == 1:
-            return out
-        self.pages += [self.pages[0][:shared // self.page_size] for _ in range(group - 1)]
-        self.length += [shared] * (group - 1)
-        dev = self.run.device
-        tail = torch.cat([-1 - torch.arange(patch.shape[0], dtype=torch.int32, device=dev), ids.to(torch.int32)])[shared:]
-        others = self._forward(list(range(1, group)), tail.repeat(group - 1), [n - shared] * (group - 1), patch, None, shared, self.run.model._keep[4] is not None)
-        self.shared_len = shared
-        return tuple(None if a is None else torch.cat([a, b]) for a, b in zip(out, others))
+        rows, others = [n - shared] * (group - 1), list(range(1, group))
+        first = self._grown(self._fresh(1), [0], [n])
+        held = first
+        if others:                                           # both halves are laid out before either runs
+            pages, length, free = first
+            held = self._grown((pages + [pages[0][:shared // self.page_size] for _ in others], length + [shared] * len(others), free), others, rows)
+            rest = self._plan(held, others, rows, shared)
+            self._buf("ws_paged", rest[1])
+        value = self.run.model._keep[4] is not None
+        every = torch.cat([-1 - torch.arange(patch.shape[0], dtype=torch.int32, device=self.run.device), ids.to(torch.int32)])
+        out = self._run(self._plan(first, [0], [n], 0), every, patch, None, 0, value)
+        if others:
+            more = self._run(rest, every[shared:].repeat(group - 1), patch, None, shared, value)
+            out = tuple(None if a is None else torch.cat([a, b]) for a, b in zip(out, more))
+        self._hold(held)
+        self.shared_len = shared if others else 0
+        return out
 
     def decode(self, logits, n_tokens: int, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, u=None, stream=None):
         """n_tokens action tokens of every sequence from the first one's logits; u [n_tokens, n_seq] in [0, 1), or None: the largest.
@@ -205,6 +233,7 @@ class PagedRollout:
 
     def _decode(self, logits, n_tokens, temperature, top_k, top_p, min_p, u):
         run, n, dev = self.run, logits.shape[0], self.run.device
+        self._grown((self.pages, self.length, self.free), list(range(n)), [n_tokens - 1] * n)          # (the pages of all steps, before the first)
         every = lambda v, dtype: torch.full((n,), v, dtype=dtype, device=dev)
         t, k, p, least = every(temperature, torch.float32), every(top_k, torch.int32), every(top_p, torch.float32), every(min_p, torch.float32)
         ws = self._buf("ws_sample", vb.vla_sample_logits_workspace_bytes(n, vb.VLA_N_BINS))
