@@ -175,7 +175,12 @@ class PagedRollout:
         return h, logits, value
 
     def _forward(self, seqs, ids, rows, patch=None, prefix_len=None, shared_len=0, want_value=False, held=None):
-        held = self._grown(held or (self.pages, self.length, self.free), seqs, rows)
+        held = held or (self.pages, self.length, self.free)
+        if not len(seqs) or len(set(seqs)) != len(seqs) or min(seqs) < 0 or max(seqs) >= len(held[0]):
+            raise ValueError(f"sequences {list(seqs)}: wanted some of the {len(held[0])}, each once")
+        if len(rows) != len(seqs) or min(rows) < 0 or sum(rows) != ids.numel():
+            raise ValueError(f"{ids.numel()} ids in rows {list(rows)} for {len(seqs)} sequences")
+        held = self._grown(held, seqs, rows)
         out = self._run(self._plan(held, seqs, rows, shared_len), ids, patch, prefix_len, shared_len, want_value)
         self._hold(held)                                     # (nothing has changed where any of this was refused)
         return out
@@ -188,6 +193,8 @@ class PagedRollout:
 
     def _prefill(self, patches, ids, see_patches=False):
         dev = self.run.device
+        if not len(ids) or len(patches) != len(ids):
+            raise ValueError(f"patches of {len(patches)} and ids of {len(ids)} sequences")
         n_patch = [0 if p is None else p.shape[0] for p in patches]
         parts, seen = [], 0
         for n, t in zip(n_patch, ids):
@@ -205,6 +212,8 @@ class PagedRollout:
             return self._prefill_group(patch, ids, group)
 
     def _prefill_group(self, patch, ids, group):
+        if group < 1:
+            raise ValueError(f"a group of {group} rollouts")
         n = patch.shape[0] + ids.numel()
         shared = (n - 1) // self.page_size * self.page_size
         rows, others = [n - shared] * (group - 1), list(range(1, group))
@@ -233,6 +242,10 @@ class PagedRollout:
 
     def _decode(self, logits, n_tokens, temperature, top_k, top_p, min_p, u):
         run, n, dev = self.run, logits.shape[0], self.run.device
+        if n != len(self.pages) or n_tokens < 1:
+            raise ValueError(f"{n_tokens} tokens from logits of {n} sequences: there are {len(self.pages)}")
+        if u is not None and (u.dim() != 2 or u.shape[0] < n_tokens or u.shape[1] != n):
+            raise ValueError(f"u is {list(u.shape)}, wanted [{n_tokens}, {n}]")
         self._grown((self.pages, self.length, self.free), list(range(n)), [n_tokens - 1] * n)          # (the pages of all steps, before the first)
         every = lambda v, dtype: torch.full((n,), v, dtype=dtype, device=dev)
         t, k, p, least = every(temperature, torch.float32), every(top_k, torch.int32), every(top_p, torch.float32), every(min_p, torch.float32)

@@ -80,3 +80,18 @@ def test_group_lays_its_pages_out_once(monkeypatch):
     first, rest = calls
     assert (first.lens, first.ids, first.shared_len) == ([33], [-1 - i for i in range(30)] + [7, 8, 9], 0)
     assert (rest.lens, rest.ids, rest.starts, rest.shared_len) == ([33, 33], [9, 9], [0, 1, 2], 32)
+
+
+def test_calls_that_make_no_sense(monkeypatch):
+    calls, p, before = started(monkeypatch)
+    z, group = torch.zeros(2, 256), torch.zeros(3, 256)
+    for call in (lambda: p.forward([0, 0], ids(1, 2), [1, 1]),                     # one sequence twice
+                 lambda: p.forward([0, 2], ids(1, 2), [1, 1]), lambda: p.forward([-1], ids(1), [1]), lambda: p.forward([], ids(), []),
+                 lambda: p.forward([0, 1], ids(1, 2), [2]), lambda: p.forward([0, 1], ids(1), [2, -1]), lambda: p.forward([0, 1], ids(1, 2, 3), [1, 1]),
+                 lambda: p.prefill([None], [ids(1), ids(2)]), lambda: p.prefill([], []), lambda: p.prefill_group(group, ids(1), 0), lambda: p.prefill_group(group, ids(1), -3),
+                 lambda: p.decode(torch.zeros(1, 256), 2), lambda: p.decode(torch.zeros(3, 256), 2), lambda: p.decode(z, 0),
+                 lambda: p.decode(z, 3, u=torch.zeros(2, 2)), lambda: p.decode(z, 3, u=torch.zeros(3, 1)), lambda: p.decode(z, 3, u=torch.zeros(3))):
+        refused(p, before, calls, ValueError, call, "sequences|rows|ids|rollouts|tokens|u is")
+    p.decode(z, 2, u=torch.zeros(3, 2))                      # numbers for more tokens than are wanted
+    p.forward([1, 0], ids(1, 2, 3), [3, 0])                  # another order, and one without new rows
+    assert p.length == [41, 9] and calls[-1].lens == [9, 41] and calls[-1].starts == [0, 3, 3]
