@@ -207,14 +207,15 @@ class PagedRollout:
         return out
 
     def prefill_group(self, patch, ids, group: int, stream=None):
-        """One observation for ``group`` rollouts: its whole pages are computed and kept once, what is behind them once per rollout."""
+        """One observation (patch or None, ids) for ``group`` rollouts: its whole pages are computed and kept once, what is behind them once per rollout."""
         with torch.cuda.stream(stream):
             return self._prefill_group(patch, ids, group)
 
     def _prefill_group(self, patch, ids, group):
         if group < 1:
             raise ValueError(f"a group of {group} rollouts")
-        n = patch.shape[0] + ids.numel()
+        n_patch = 0 if patch is None else patch.shape[0]
+        n = n_patch + ids.numel()
         shared = (n - 1) // self.page_size * self.page_size
         rows, others = [n - shared] * (group - 1), list(range(1, group))
         first = self._grown(self._fresh(1), [0], [n])
@@ -225,7 +226,7 @@ class PagedRollout:
             rest = self._plan(held, others, rows, shared)
             self._buf("ws_paged", rest[1])
         value = self.run.model._keep[4] is not None
-        every = torch.cat([-1 - torch.arange(patch.shape[0], dtype=torch.int32, device=self.run.device), ids.to(torch.int32)])
+        every = torch.cat([-1 - torch.arange(n_patch, dtype=torch.int32, device=self.run.device), ids.to(torch.int32)])
         out = self._run(self._plan(first, [0], [n], 0), every, patch, None, 0, value)
         if others:
             more = self._run(rest, every[shared:].repeat(group - 1), patch, None, shared, value)

@@ -95,3 +95,11 @@ def test_calls_that_make_no_sense(monkeypatch):
     p.decode(z, 2, u=torch.zeros(3, 2))                      # numbers for more tokens than are wanted
     p.forward([1, 0], ids(1, 2, 3), [3, 0])                  # another order, and one without new rows
     assert p.length == [41, 9] and calls[-1].lens == [9, 41] and calls[-1].starts == [0, 3, 3]
+
+
+def test_group_without_patches(monkeypatch):
+    calls = record(monkeypatch)
+    p = PagedRollout(Run(), 8)
+    p.prefill_group(None, torch.arange(20, dtype=torch.int32), 2)
+    first, rest = calls
+    assert first.ids == list(range(20)) and rest.ids == [16, 17, 18, 19] and first.patch is rest.patch is None
