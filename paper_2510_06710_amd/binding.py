@@ -61,21 +61,25 @@ class vla_placement(C.Structure):
 
 
 class vla_paged_cache(C.Structure):
+    keep, device = (), None          # (make_* puts the tensors and their GPU here: of plain addresses nothing is known)
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32),
                 ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
 
 
 class vla_paged_batch(C.Structure):
+    keep, device = (), None
     _fields_ = [("n_seq", C.c_int32), ("n_rows", C.c_int32), ("max_rows", C.c_int32), ("max_len", C.c_int32), ("table_stride", C.c_int32),
                 ("row_start", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p)]
 
 
 class vla_rotary(C.Structure):
+    keep, device = (None, None, None), None
     _fields_ = [("inv_freq", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_float), ("eps", C.c_float),
                 ("q_gain", C.c_void_p), ("k_gain", C.c_void_p)]
 
 
 class vla_paged_mask(C.Structure):
+    keep, device = (None, None), None
     _fields_ = [("scale", C.c_float), ("softcap", C.c_float), ("slopes", C.c_void_p), ("prefix_len", C.c_void_p), ("window", C.c_int32),
                 ("shared_len", C.c_int32)]
 
