@@ -358,6 +358,7 @@ def _device_of(*tensors):
 
 def _on_current_device(what, structures, tensors):
     """The library launches on the current GPU: arrays of another one, or of the host, would be read from there."""
+    import torch
     here = tensors[0].get_device()
     for s in structures:
         if s.device is not None and s.device != here:
@@ -365,14 +366,8 @@ def _on_current_device(what, structures, tensors):
     for t in tensors:
         if t is not None and t.get_device() != here:
             here = -1
-    if here < 0 or here != _current_device():
+    if here < 0 or here != torch.cuda.current_device():
         raise VlaError(VLA_EINVAL, f"{what}: the arrays are not all on the current GPU")
-
-
-def _current_device() -> int:
-    import torch
-    device = getattr(torch._C, "_cuda_getDevice", None)          # (no public interface; 0.4 us less)
-    return device() if device and torch.cuda.is_initialized() else torch.cuda.current_device()
 
 
 def _rows_of_heads(t, heads, dim, rows, name):
