@@ -156,7 +156,7 @@ template <int THREADS> struct Room {
     double table[TABLE];
     Block<THREADS> block;
     int n;                       // tokens that asked for a place in the list
-    int found, which;
+    int found;
     u64 found_before;
 };
 
