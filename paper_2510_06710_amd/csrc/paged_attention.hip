@@ -663,8 +663,8 @@ struct Walk {
 // their lengths, and streams through it, the next tile on its way whether it is of the same sequence or not.  A sequence's tiles that
 // fall to several waves leave parts for the join (a wave has at most two: of the sequence it begins within, and of the one it ends within).
 // Neighbouring waves have the same run of different heads, whose rows lie side by side in the pages.
-// Memory bound: 32 sequences of 2048 keys, 32 heads, 192 us, 5.6 TB/s; 256 of 294 keys 229 us, 5.4; one of 32768 keys, 8 key heads, 26 us and 6 for
-// the join of 128 parts; 48 ragged ones of up to 8192 keys with capped scores and a bias 79 us.  (One workgroup of 1, 2 or 4 waves per sequence,
+// Memory bound: 32 sequences of 2048 keys, 32 heads, 192 us, 5.6 TB/s; 256 of 294 keys 229 us, 5.4; one of 32768 keys, 8 key heads, 27 us and 6 for
+// the join of 128 parts; 48 ragged ones of up to 8192 keys with capped scores and a bias 80 us.  (One workgroup of 1, 2 or 4 waves per sequence,
 // key head and even part of max_len: 200, 259, 30 + 5 and 125 to 155 us.)
 template <typename T, int DP, int MODE>
 __global__ void __launch_bounds__(64) paged_decode_kernel(AttnArgs a) {
@@ -1063,7 +1063,7 @@ int vla_paged_attention(const vla_paged_cache *cache, const vla_paged_batch *bat
     a.aligned = ((uintptr_t)q | (uintptr_t)out | (size_t)q_stride * es | (size_t)out_stride * es) % 16 == 0;
     a.offset = !f32 ? a.cap * 1.4426950408889634f : 0.f;
     hipStream_t st = (hipStream_t)stream;
-    ProfScope ps("paged_attention", 0.0, st);
+    ProfScope ps("paged_attention", 0.0, st);               // (how much there is to do stands in arrays of the device)
     return f32 ? launch_typed<float>(a, p, st) : launch_typed<bf16_t>(a, p, st);
 }
 
