@@ -338,7 +338,8 @@ int vla_policy_objective_noalloc(const float *logp_new, const float *logp_old, c
  *   NULL);  visible are j < kv_len with  (j <= p and (window == 0 or j > p - window))  or  j < prefix_len[sequence];
  *   out = sum softmax(s) v, fp32 sums; weights enter the products with v with 16 bits at least, but on a bf16 cache as bf16 where
  *   n_heads / n_kv_heads times max_rows is above 32 (prompts).  lse (fp32 [n_rows, n_heads] or NULL) = ln sum exp(s).  A row that sees no
- *   key gets zeros and -inf; a head of a row with a visible score that is NaN or +inf gets NaN in both, however the keys are split.  K and V of visible positions are taken to be finite where any row of the call masks them.
+ *   key gets zeros and -inf; a head of a row with a visible score that is NaN or +inf gets NaN in both, however the keys are split (so
+ *   may one with an infinite k whose score is -inf).  K and V of visible positions are taken to be finite where any row of the call masks them.
  *   vla_paged_mask: scale > 0; softcap, window >= 0; slopes DEVICE fp32 [n_heads]; prefix_len DEVICE int32 [n_seq]; shared_len
  *   (HOST): a multiple of page_size; the first shared_len positions of all sequences lie in the same pages, which are read once
  *   for the whole batch, through sequence 0's table (sequence 0 and every sequence with rows hold shared_len positions

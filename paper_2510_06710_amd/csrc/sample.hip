@@ -641,7 +641,7 @@ extern "C" {
 
 size_t vla_sample_logits_workspace_bytes(int n, int vocab) {
     if (n <= 0 || vocab <= 0 || vocab > 262144) { vla_set_error("sample_logits: n must be positive, vocab 1 .. 262,144"); return 0; }
-    return 256;
+    return 256;          // (room that the call's form leaves: nothing is kept there)
 }
 
 int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, int vocab, const float *temperature, const int32_t *top_k,

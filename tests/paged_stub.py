@@ -22,7 +22,7 @@ class Run:
 
 
 def record(monkeypatch):
-    """Calls of the library from here on: (name, arguments by position, arguments by name).  `fail` of the list, an exception, is what the next forward raises."""
+    """The library's calls from here on, in their order, with what the device arrays held.  `fail` of the list, an exception, is what the next forward raises."""
     class Calls(list):
         fail = None
 
