@@ -214,6 +214,7 @@ class PagedRollout:
     def _prefill_group(self, patch, ids, group):
         if group < 1:
             raise ValueError(f"a group of {group} rollouts")
+        patch = None if patch is None else patch.contiguous()
         n_patch = 0 if patch is None else patch.shape[0]
         n = n_patch + ids.numel()
         shared = (n - 1) // self.page_size * self.page_size

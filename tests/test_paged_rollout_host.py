@@ -103,3 +103,11 @@ def test_group_without_patches(monkeypatch):
     p.prefill_group(None, torch.arange(20, dtype=torch.int32), 2)
     first, rest = calls
     assert first.ids == list(range(20)) and rest.ids == [16, 17, 18, 19] and first.patch is rest.patch is None
+
+
+@pytest.mark.parametrize("group", [1, 2])
+def test_group_of_a_patch_that_is_a_view(monkeypatch, group):
+    calls = record(monkeypatch)
+    wide = torch.arange(20 * 512, dtype=torch.float32).view(20, 512)
+    PagedRollout(Run(), 8).prefill_group(wide[:, ::2], ids(1, 2, 3), group)
+    assert len(calls) == group and all(c.patch.is_contiguous() and torch.equal(c.patch, wide[:, ::2]) for c in calls)
