@@ -15,7 +15,7 @@
 //
 // Weights are exp2 of scores in units of log2 e; the reference of a row moves only when its maximum has grown by more than 2^8, so
 // sums stay below 2^8 times the count and most tiles rescale nothing.  Of a decode form's weights the product with a bf16 V takes a bf16 head and a
-// bf16 tail (2^-16 of the weight is lost, as in attn_mfma.hip): the step waits for memory, and is 1 % longer (behind a shared prefix 10 %).  A prompt's are rounded to
+// bf16 tail (2^-16 of the weight is lost, as in attn_mfma.hip): the step waits for memory, and is 1 % longer (behind a shared prefix 8 %).  A prompt's are rounded to
 // bf16 once (2^-8 of each, as the tolerances count it), for the third product would take 8192 rows from 550 to 745 us: outputs are off by 1.4 times what their own rounding
 // costs (rms 0.0023 of them for 0.0017).  The sum that divides is that of the fp32 weights.
 #include "paged.h"

@@ -136,14 +136,17 @@ class PagedRollout:
 
     def _grown(self, held, seqs, rows):
         """`held` with rows[i] more positions for seqs[i]; what is given stays as it is."""
-        pages, length, free = (list(x) for x in held)
+        pages, length, free = held
         wanted = [max(0, -(-(length[s] + n) // self.page_size) - len(pages[s])) for s, n in zip(seqs, rows)]
         if sum(wanted) > len(free):
             raise ValueError(f"{sum(wanted)} pages wanted, {len(free)} of {self.n_pages} free")
-        for s, n, more in zip(seqs, rows, wanted):
+        length, left = list(length), len(free) - sum(wanted)
+        for s, n in zip(seqs, rows):
             length[s] += n
-            if more:
-                pages[s] = pages[s] + [free.pop() for _ in range(more)]
+        if left < len(free):
+            pages, more, free = list(pages), iter(free[left:][::-1]), free[:left]
+            for s, n in zip(seqs, wanted):
+                pages[s] = pages[s] + [next(more) for _ in range(n)]
         return pages, length, free
 
     def _int(self, values):
