@@ -387,6 +387,9 @@ typedef struct vla_paged_mask {
     const int32_t *prefix_len;
     int32_t window, shared_len;
 } vla_paged_mask;
+/* The largest tree of drafted rows of one sequence, and the most pages of a sequence that are chosen from. */
+#define VLA_TREE_ROWS 1024
+#define VLA_SELECT_PAGES 8192
 int vla_paged_append(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_rotary *rotary, const void *q,
                      const void *k, const void *v, int in_dtype, int n_heads, int64_t q_stride, int64_t k_stride,
                      int64_t v_stride, void *q_out, int64_t q_out_stride, void *stream);
@@ -404,6 +407,82 @@ int vla_forward_paged(vla_model *model, const vla_paged_cache *cache, size_t lay
 int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, int vocab, const float *temperature,
                       const int32_t *top_k, const float *top_p, const float *min_p, const float *u, int32_t *token,
                       float *logp, float *logp_kept, int32_t *n_kept, void *ws, size_t ws_bytes, void *stream);
+
+/* ---- reading less per token: drafted trees, sparse pages, eviction --------------------------------------------------------
+ * A decode step on the paged cache reads all K and V of a sequence for one token.  These take several drafted tokens through one such
+ * step, read only the pages that matter to a row, or cut the cache to the positions that mattered.  Cache, batch, mask, padding, page ids
+ * out of range, streams and workspaces are as above.
+ *
+ * vla_paged_append_at: vla_paged_append with the rotation's position of every row in `position` (DEVICE int32 [n_rows], not negative)
+ *   instead of its place in the cache: a drafted node's is its depth behind the cache, and behind a cache that was cut places have moved.
+ *
+ * Drafted trees.  The new rows of a sequence (n_s of them, at most VLA_TREE_ROWS) are the nodes of a tree: the first is the last committed
+ * token, the others drafts, each behind its parent.  parent: DEVICE int32 [n_rows], the parent's number among the sequence's rows, smaller
+ * than the node's own (of the first row, and wherever it is not in 0 .. i - 1: none, the node stands on the cache itself).
+ * vla_paged_tree: seen [n_rows][words] out, DEVICE int32: bit j % 32 of word j / 32 says that the row sees its sequence's new row j: its
+ *   ancestors and itself; position [n_rows] out or NULL: kv_len - n_s + depth.  words: at least max_rows / 32 rounded up, at most 32.
+ * vla_paged_tree_attention: as vla_paged_attention, but a row sees the positions below kv_len - n_s and of the new rows those whose
+ *   bits are set in its `seen` (any bits: not only a tree's).  mask: scale, softcap and shared_len (at most kv_len - n_s of every sequence with rows) alone;
+ *   slopes and prefix_len NULL, window 0.  On a bf16 cache weights enter the products with v with 16 bits whatever the number of rows.
+ *   ws: of vla_paged_attention_workspace_bytes bytes.
+ * vla_paged_accept: the drafts that the model agrees with.  ids: DEVICE int32 [n_rows], the rows' tokens; chosen: DEVICE int32
+ *   [n_rows], the model's own token behind each row (vla_sample_logits of its logits).  From the first row on, the path goes to the
+ *   lowest row whose parent is the path's last and whose id is what that chose (a negative choice: none), until there is none.  path
+ *   [n_seq, max_rows] out: the rows of the path, then -1; n_accepted [n_seq] out: how many; next [n_seq] out or NULL: what the last of
+ *   them chose (-1 without rows); new_len [n_seq] out or NULL: kv_len - n_s + n_accepted.  In each of n_layers layers, layer l at
+ *   cache->k, v + l * layer_stride elements, K and V of row path[i] move to position kv_len - n_s + i (n_layers may be 0: nothing moves).  The rows behind
+ *   new_len keep what they hold.  The pages of the new rows belong to their sequence alone.  Without rows, or where rows lie at negative positions, new_len is not below 0.
+ *
+ * Sparse attention over pages.
+ * vla_paged_bounds: bounds, DEVICE cache's dtype [n_pages][n_kv_heads][2][head_dim], 16-byte aligned: the least and the largest K of each dim over the
+ *   positions below kv_len of a page, for every page that holds one of the batch's rows (positions kv_len - n_s on; a batch whose rows
+ *   are all positions: every page).  K of these positions is finite; pages of other rows keep their bounds.
+ * vla_paged_select: for each row and key head, the pages to read.  score(page) = sum over the heads h of the group and the dims of
+ *   max(q_h lo, q_h hi), no less than the sum of the heads' q.k for any key of the page; fp64.  Of the pages 0 .. p / page_size of a row at
+ *   position p the first `first` and the last `recent` (at least 1) are taken, then those with the largest scores (ties: lowest page
+ *   first; a score that is NaN comes last), until there are n_select (at least first + recent).  selected [n_rows][n_kv_heads][n_select]
+ *   out, DEVICE int32: numbers of pages within the sequence, ascending, then -1.  Rows at negative positions get none.  max_len / page_size at most VLA_SELECT_PAGES.
+ * vla_paged_sparse_attention: as vla_paged_attention, but a row's heads see the positions j <= p, j < kv_len of the pages in their `selected` alone
+ *   (any ascending list; it ends at the first negative entry, and an entry not above the one before it is left out).  mask: scale and
+ *   softcap alone.  Each row reads its own pages: for few rows per sequence.
+ *
+ * Eviction by accumulated weight.
+ * vla_paged_weights: mass [n_seq][n_kv_heads][mass_stride], DEVICE fp32: to every position j < kv_len - n_s that a row sees is added, and every
+ *   new position gets, the sum over the call's rows and the heads of the group of exp(s - lse), with s and the visibility of
+ *   vla_paged_attention under the same mask (shared_len changes nothing) and lse its output [n_rows, n_heads].  A row whose lse is -inf adds nothing.
+ *   mass_stride: at least max_len.  Sums in fp32 in a fixed order.
+ * vla_paged_evict: each sequence and key head keeps `keep` positions: the first `first` and the last `recent`, then those of the largest
+ *   mass (ties: lowest position first; NaN comes last); all where there are no more.  kept [n_seq][n_kv_heads][keep] out: positions,
+ *   ascending, then -1.  K, V and mass of the i-th go to position i: K and V in page to_table[sequence][i / page_size] (to_stride entries per
+ *   sequence, at least keep / page_size rounded up), mass to mass_out [n_seq][n_kv_heads][mass_out_stride] (mass itself with its stride, or apart
+ *   from it; entries behind the last keep what they hold).  new_len [n_seq] out or NULL: min(kv_len, keep).  to_table's pages hold nothing that the call reads, but that a sequence
+ *   with no more than `keep` may name its own pages again (nothing moves).  One layer a call.  Of the batch it uses the sequences, not their rows. */
+int vla_paged_append_at(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_rotary *rotary, const int32_t *position,
+                        const void *q, const void *k, const void *v, int in_dtype, int n_heads, int64_t q_stride, int64_t k_stride,
+                        int64_t v_stride, void *q_out, int64_t q_out_stride, void *stream);
+int vla_paged_tree(const vla_paged_cache *cache, const vla_paged_batch *batch, const int32_t *parent, int32_t *seen, int words, int32_t *position,
+                   void *stream);
+int vla_paged_tree_attention(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, const int32_t *seen,
+                             int words, const void *q, int n_heads, int64_t q_stride, void *out, int64_t out_stride, float *lse, void *ws,
+                             size_t ws_bytes, void *stream);
+int vla_paged_accept(const vla_paged_cache *cache, int n_layers, size_t layer_stride, const vla_paged_batch *batch, const int32_t *parent,
+                     const int32_t *ids, const int32_t *chosen, int32_t *path, int32_t *n_accepted, int32_t *next, int32_t *new_len,
+                     void *stream);
+int vla_paged_bounds(const vla_paged_cache *cache, const vla_paged_batch *batch, void *bounds, void *stream);
+size_t vla_paged_select_workspace_bytes(const vla_paged_cache *cache, const vla_paged_batch *batch);
+int vla_paged_select(const vla_paged_cache *cache, const vla_paged_batch *batch, const void *bounds, const void *q, int n_heads,
+                     int64_t q_stride, int n_select, int first, int recent, int32_t *selected, void *ws, size_t ws_bytes, void *stream);
+size_t vla_paged_sparse_attention_workspace_bytes(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask,
+                                                  int n_heads, int n_select);
+int vla_paged_sparse_attention(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask,
+                               const int32_t *selected, int n_select, const void *q, int n_heads, int64_t q_stride, void *out,
+                               int64_t out_stride, float *lse, void *ws, size_t ws_bytes, void *stream);
+size_t vla_paged_weights_workspace_bytes(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, int n_heads);
+int vla_paged_weights(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, const void *q, int n_heads,
+                      int64_t q_stride, const float *lse, float *mass, int64_t mass_stride, void *ws, size_t ws_bytes, void *stream);
+int vla_paged_evict(const vla_paged_cache *cache, const vla_paged_batch *batch, const float *mass, int64_t mass_stride, int keep, int first,
+                    int recent, const int32_t *to_table, int to_stride, int32_t *kept, float *mass_out, int64_t mass_out_stride,
+                    int32_t *new_len, void *stream);
 
 /* ---------------------------------------------------------------- GPU allocation modes (section IV-A)
  * Host-only arithmetic (no device work, all pointers HOST): the rollout-time model behind the

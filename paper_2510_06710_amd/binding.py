@@ -149,6 +149,22 @@ def lib() -> C.CDLL:
         L.vla_sample_logits_workspace_bytes.argtypes = [i32, i32]
         L.vla_sample_logits_workspace_bytes.restype = sz
         L.vla_sample_logits.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        mask = C.POINTER(vla_paged_mask)
+        L.vla_paged_append_at.argtypes = [cache, batch, C.POINTER(vla_rotary), vp, vp, vp, vp, i32, i32, i64, i64, i64, vp, i64, vp]
+        L.vla_paged_tree.argtypes = [cache, batch, vp, vp, i32, vp, vp]
+        L.vla_paged_tree_attention.argtypes = [cache, batch, mask, vp, i32, vp, i32, i64, vp, i64, vp, vp, sz, vp]
+        L.vla_paged_accept.argtypes = [cache, i32, sz, batch, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.vla_paged_bounds.argtypes = [cache, batch, vp, vp]
+        L.vla_paged_select_workspace_bytes.argtypes = [cache, batch]
+        L.vla_paged_select_workspace_bytes.restype = sz
+        L.vla_paged_select.argtypes = [cache, batch, vp, vp, i32, i64, i32, i32, i32, vp, vp, sz, vp]
+        L.vla_paged_sparse_attention_workspace_bytes.argtypes = [cache, batch, mask, i32, i32]
+        L.vla_paged_sparse_attention_workspace_bytes.restype = sz
+        L.vla_paged_sparse_attention.argtypes = [cache, batch, mask, vp, i32, vp, i32, i64, vp, i64, vp, vp, sz, vp]
+        L.vla_paged_weights_workspace_bytes.argtypes = [cache, batch, mask, i32]
+        L.vla_paged_weights_workspace_bytes.restype = sz
+        L.vla_paged_weights.argtypes = [cache, batch, mask, vp, i32, i64, vp, vp, i64, vp, sz, vp]
+        L.vla_paged_evict.argtypes = [cache, batch, vp, i64, i32, i32, i32, vp, i32, vp, vp, i64, vp, vp]
         dp = C.POINTER(C.c_double)
         L.vla_pipeline_time.argtypes = [C.c_double, C.c_double, i32, i32, dp]
         L.vla_profile_lookup.argtypes = [dp, i32, C.c_double, dp]
@@ -416,8 +432,7 @@ def make_paged_mask(scale: float, softcap=0.0, slopes=None, prefix_len=None, win
     return m
 
 
-def vla_paged_append(cache, batch, rotary, q, k, v, q_out=None, stream=None) -> None:
-    """``q`` [n_rows, n_heads, head_dim] (or None with ``q_out``), ``k``, ``v`` [n_rows, n_kv_heads, head_dim]: views with packed heads."""
+def _append_arguments(cache, batch, rotary, q, k, v, q_out, position=None):
     d, rows = cache.head_dim, batch.n_rows
     if (q is None) != (q_out is None):
         raise VlaError(VLA_EINVAL, "paged_append: q and q_out come together")
@@ -436,9 +451,21 @@ def vla_paged_append(cache, batch, rotary, q, k, v, q_out=None, stream=None) -> 
             raise VlaError(VLA_EDTYPE, "paged_append: q_out has the cache's type")
     if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
         raise VlaError(VLA_EDTYPE, "paged_append: q, k and v have one type")
-    _on_current_device("paged_append", (cache, batch, rotary), (k, v, q, q_out))
-    _check(lib().vla_paged_append(C.byref(cache), C.byref(batch), C.byref(rotary), qp or None, kp, vp_, _dtype(k), heads, qs, ks, vs,
-                                  op or None, os_, _stream(stream)))
+    _on_current_device("paged_append", (cache, batch, rotary), (k, v, q, q_out, position))
+    return qp or None, kp, vp_, _dtype(k), heads, qs, ks, vs, op or None, os_
+
+
+def vla_paged_append(cache, batch, rotary, q, k, v, q_out=None, stream=None) -> None:
+    """``q`` [n_rows, n_heads, head_dim] (or None with ``q_out``), ``k``, ``v`` [n_rows, n_kv_heads, head_dim]: views with packed heads."""
+    arguments = _append_arguments(cache, batch, rotary, q, k, v, q_out)
+    _check(lib().vla_paged_append(C.byref(cache), C.byref(batch), C.byref(rotary), *arguments, _stream(stream)))
+
+
+def vla_paged_append_at(cache, batch, rotary, position, q, k, v, q_out=None, stream=None) -> None:
+    """``position`` int32 [n_rows]: of the rotation; the rest as in vla_paged_append."""
+    at = _want(position, "int32", "position", (batch.n_rows,))
+    arguments = _append_arguments(cache, batch, rotary, q, k, v, q_out, position)
+    _check(lib().vla_paged_append_at(C.byref(cache), C.byref(batch), C.byref(rotary), at, *arguments, _stream(stream)))
 
 
 def vla_paged_attention_workspace_bytes(cache, batch, mask, n_heads: int) -> int:
@@ -505,6 +532,142 @@ def vla_sample_logits(logits, token, temperature=None, top_k=None, top_p=None, m
     _on_current_device("sample_logits", (), (logits, temperature, top_k, top_p, min_p, u, token, logp, logp_kept, n_kept, ws))
     _check(lib().vla_sample_logits(logits.data_ptr(), code, logits.stride(0) if n > 1 else vocab, n, vocab, *settings, *outputs, _ptr(ws),
                                    0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def _ws(ws):
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+
+
+def _ints(t, name, *shape):
+    return _want(t, "int32", name, shape)
+
+
+def _positive(n: int) -> int:
+    if n == 0:
+        raise VlaError(VLA_EINVAL, vla_last_error())
+    return n
+
+
+def vla_paged_tree(cache, batch, parent, seen, position=None, stream=None) -> None:
+    """``parent`` int32 [n_rows]; ``seen`` int32 [n_rows, words] out; ``position`` int32 [n_rows] out."""
+    rows = batch.n_rows
+    if seen.dim() != 2:
+        raise VlaError(VLA_ESHAPE, f"seen is {list(seen.shape)}, wanted [{rows}, words]")
+    arrays = _ints(parent, "parent", rows), _ints(seen, "seen", rows, seen.shape[1]), seen.shape[1], _ints(position, "position", rows)
+    _on_current_device("paged_tree", (cache, batch), (parent, seen, position))
+    _check(lib().vla_paged_tree(C.byref(cache), C.byref(batch), *arrays, _stream(stream)))
+
+
+def _attended(what, cache, batch, mask, q, out):
+    """Address, heads and stride of q, address and stride of out."""
+    qp, qs = _rows_of_heads(q, None, cache.head_dim, batch.n_rows, "q")
+    heads = q.shape[1]
+    op, os_ = _rows_of_heads(out, heads, cache.head_dim, batch.n_rows, "out")
+    if _dtype(q) != cache.dtype or _dtype(out) != cache.dtype:
+        raise VlaError(VLA_EDTYPE, f"{what}: q and out have the cache's type")
+    return qp, heads, qs, op, os_
+
+
+def vla_paged_tree_attention(cache, batch, mask, seen, q, out, lse=None, ws=None, stream=None) -> None:
+    """``seen`` int32 [n_rows, words] as vla_paged_tree gives it; ``ws`` of vla_paged_attention_workspace_bytes bytes."""
+    rows = batch.n_rows
+    arguments = _attended("paged_tree_attention", cache, batch, mask, q, out)
+    if seen.dim() != 2:
+        raise VlaError(VLA_ESHAPE, f"seen is {list(seen.shape)}, wanted [{rows}, words]")
+    bits, sums = _ints(seen, "seen", rows, seen.shape[1]), _want(lse, "float32", "lse", (rows, arguments[1]))
+    _on_current_device("paged_tree_attention", (cache, batch, mask), (q, out, seen, lse, ws))
+    _check(lib().vla_paged_tree_attention(C.byref(cache), C.byref(batch), C.byref(mask), bits, seen.shape[1], *arguments, sums, *_ws(ws),
+                                          _stream(stream)))
+
+
+def vla_paged_accept(cache, n_layers: int, layer_stride: int, batch, parent, ids, chosen, path, n_accepted, next=None, new_len=None, stream=None) -> None:
+    """``parent``, ``ids``, ``chosen`` int32 [n_rows]; ``path`` int32 [n_seq, max_rows] out; ``n_accepted``, ``next``, ``new_len`` int32 [n_seq] out."""
+    rows, n = batch.n_rows, batch.n_seq
+    arrays = (_ints(parent, "parent", rows), _ints(ids, "ids", rows), _ints(chosen, "chosen", rows), _ints(path, "path", n, batch.max_rows),
+              _ints(n_accepted, "n_accepted", n), _ints(next, "next", n), _ints(new_len, "new_len", n))
+    _on_current_device("paged_accept", (cache, batch), (n_accepted, parent, ids, chosen, path, next, new_len))
+    _check(lib().vla_paged_accept(C.byref(cache), n_layers, layer_stride, C.byref(batch), *arrays, _stream(stream)))
+
+
+def _bounds(cache, bounds):
+    if _dtype(bounds) != cache.dtype or bounds.shape != (cache.n_pages, cache.n_kv_heads, 2, cache.head_dim) or not bounds.is_contiguous():
+        raise VlaError(VLA_EINVAL, f"bounds: contiguous [n_pages, n_kv_heads, 2, head_dim] of the cache's type wanted, {bounds.dtype} {list(bounds.shape)} given")
+    return bounds.data_ptr()
+
+
+def vla_paged_bounds(cache, batch, bounds, stream=None) -> None:
+    """``bounds`` [n_pages, n_kv_heads, 2, head_dim] in the cache's type: those of the pages that hold the batch's rows are written."""
+    at = _bounds(cache, bounds)
+    _on_current_device("paged_bounds", (cache, batch), (bounds,))
+    _check(lib().vla_paged_bounds(C.byref(cache), C.byref(batch), at, _stream(stream)))
+
+
+def vla_paged_select_workspace_bytes(cache, batch) -> int:
+    return _positive(lib().vla_paged_select_workspace_bytes(C.byref(cache), C.byref(batch)))
+
+
+def _selected(cache, batch, selected):
+    if selected.dim() != 3:
+        raise VlaError(VLA_ESHAPE, f"selected is {list(selected.shape)}, wanted [{batch.n_rows}, {cache.n_kv_heads}, n_select]")
+    return _ints(selected, "selected", batch.n_rows, cache.n_kv_heads, selected.shape[2])
+
+
+def vla_paged_select(cache, batch, bounds, q, selected, first=1, recent=1, ws=None, stream=None) -> None:
+    """``selected`` int32 [n_rows, n_kv_heads, n_select] out."""
+    qp, qs = _rows_of_heads(q, None, cache.head_dim, batch.n_rows, "q")
+    if _dtype(q) != cache.dtype:
+        raise VlaError(VLA_EDTYPE, "paged_select: q has the cache's type")
+    at, out = _bounds(cache, bounds), _selected(cache, batch, selected)
+    _on_current_device("paged_select", (cache, batch), (q, bounds, selected, ws))
+    _check(lib().vla_paged_select(C.byref(cache), C.byref(batch), at, qp, q.shape[1], qs, selected.shape[2], first, recent, out, *_ws(ws), _stream(stream)))
+
+
+def vla_paged_sparse_attention_workspace_bytes(cache, batch, mask, n_heads: int, n_select: int) -> int:
+    return _positive(lib().vla_paged_sparse_attention_workspace_bytes(C.byref(cache), C.byref(batch), C.byref(mask), n_heads, n_select))
+
+
+def vla_paged_sparse_attention(cache, batch, mask, selected, q, out, lse=None, ws=None, stream=None) -> None:
+    """``selected`` int32 [n_rows, n_kv_heads, n_select]: ascending numbers of pages within the row's sequence, then -1."""
+    arguments = _attended("paged_sparse_attention", cache, batch, mask, q, out)
+    pages, sums = _selected(cache, batch, selected), _want(lse, "float32", "lse", (batch.n_rows, arguments[1]))
+    _on_current_device("paged_sparse_attention", (cache, batch, mask), (q, out, selected, lse, ws))
+    _check(lib().vla_paged_sparse_attention(C.byref(cache), C.byref(batch), C.byref(mask), pages, selected.shape[2], *arguments, sums,
+                                            *_ws(ws), _stream(stream)))
+
+
+def vla_paged_weights_workspace_bytes(cache, batch, mask, n_heads: int) -> int:
+    return _positive(lib().vla_paged_weights_workspace_bytes(C.byref(cache), C.byref(batch), C.byref(mask), n_heads))
+
+
+def _mass(cache, batch, mass, name):
+    if mass.dim() != 3:
+        raise VlaError(VLA_ESHAPE, f"{name} is {list(mass.shape)}, wanted [{batch.n_seq}, {cache.n_kv_heads}, positions]")
+    return _want(mass, "float32", name, (batch.n_seq, cache.n_kv_heads, mass.shape[2])), mass.shape[2]
+
+
+def vla_paged_weights(cache, batch, mask, q, lse, mass, ws=None, stream=None) -> None:
+    """``lse`` [n_rows, n_heads] of the attention under the same mask; ``mass`` fp32 [n_seq, n_kv_heads, positions] in and out."""
+    qp, qs = _rows_of_heads(q, None, cache.head_dim, batch.n_rows, "q")
+    heads = q.shape[1]
+    if _dtype(q) != cache.dtype:
+        raise VlaError(VLA_EDTYPE, "paged_weights: q has the cache's type")
+    _want(mask.keep[0], "float32", "slopes", (heads,))
+    _want(mask.keep[1], "int32", "prefix_len", (batch.n_seq,))
+    arrays = _want(lse, "float32", "lse", (batch.n_rows, heads)), *_mass(cache, batch, mass, "mass")
+    _on_current_device("paged_weights", (cache, batch, mask), (q, lse, mass, ws))
+    _check(lib().vla_paged_weights(C.byref(cache), C.byref(batch), C.byref(mask), qp, heads, qs, *arrays, *_ws(ws), _stream(stream)))
+
+
+def vla_paged_evict(cache, batch, mass, first: int, recent: int, to_table, kept, mass_out, new_len=None, stream=None) -> None:
+    """``kept`` int32 [n_seq, n_kv_heads, keep] out; ``to_table`` int32 [n_seq, entries]; ``mass``, ``mass_out`` fp32 [n_seq, n_kv_heads, positions]."""
+    n = batch.n_seq
+    if kept.dim() != 3 or to_table.dim() != 2:
+        raise VlaError(VLA_ESHAPE, f"kept is {list(kept.shape)}, wanted [{n}, {cache.n_kv_heads}, keep]; to_table is {list(to_table.shape)}, wanted [{n}, entries]")
+    sums, out = _mass(cache, batch, mass, "mass"), _mass(cache, batch, mass_out, "mass_out")
+    keep, entries = kept.shape[2], to_table.shape[1]
+    pages, which, lens = _ints(to_table, "to_table", n, entries), _ints(kept, "kept", n, cache.n_kv_heads, keep), _ints(new_len, "new_len", n)
+    _on_current_device("paged_evict", (cache, batch), (mass, to_table, kept, mass_out, new_len))
+    _check(lib().vla_paged_evict(C.byref(cache), C.byref(batch), *sums, keep, first, recent, pages, entries, which, *out, lens, _stream(stream)))
 
 
 def _doubles(values):

@@ -23,6 +23,7 @@ struct AppendArgs {
     int half, interleaved;
     float scale, eps;
     const float *q_gain, *k_gain;
+    const int32_t *position; // of the rotation, per row; NULL: the row's place
     int lanes_log;           // log2 of the lanes per head (d / 8 rounded up to a power of two)
     int aligned;             // every row and head of the inputs and of q_out starts at a multiple of 16 bytes
 };
@@ -103,7 +104,7 @@ __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a) {
     const int page = paged_int(pv.table, (size_t)s * pv.table_stride + (pos >> pv.page_log));
     const bool kept = (unsigned)page < (unsigned)pv.n_pages;
     if ((int)threadIdx.x < a.half) {
-        double t = (double)pos * freq * 0.15915494309189533577, sn, cs;      // turns
+        double t = (double)(a.position ? max(paged_int(a.position, row), 0) : pos) * freq * 0.15915494309189533577, sn, cs;      // turns
         t -= rint(t);
         sincospi(2.0 * t, &sn, &cs);
         turn[threadIdx.x] = make_float2((float)cs * a.scale, (float)sn * a.scale);
@@ -234,10 +235,11 @@ int vla_check_paged(const char *what, const vla_paged_cache *c, const vla_paged_
     return VLA_OK;
 }
 
-extern "C" int vla_paged_append(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_rotary *rotary, const void *q,
-                                const void *k, const void *v, int in_dtype, int n_heads, int64_t q_stride, int64_t k_stride,
-                                int64_t v_stride, void *q_out, int64_t q_out_stride, void *stream) {
+static int append(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_rotary *rotary, const int32_t *position, const void *q,
+                  const void *k, const void *v, int in_dtype, int n_heads, int64_t q_stride, int64_t k_stride, int64_t v_stride, void *q_out,
+                  int64_t q_out_stride, void *stream) {
     AppendArgs a{};
+    a.position = position;
     if (int rc = vla_check_paged("paged_append", cache, batch, &a.pv)) return rc;
     if (in_dtype != VLA_DTYPE_F32 && in_dtype != VLA_DTYPE_BF16) { vla_set_error("paged_append: unknown dtype %d", in_dtype); return VLA_EDTYPE; }
     if (!rotary || (batch->n_rows > 0 && (!k || !v))) { vla_set_error("paged_append: rotary, k or v is NULL"); return VLA_EINVAL; }
@@ -281,4 +283,16 @@ extern "C" int vla_paged_append(const vla_paged_cache *cache, const vla_paged_ba
     else if (fo) paged_append_kernel<bf16_t, float><<<grid, 256, 0, st>>>(a);
     else paged_append_kernel<bf16_t, bf16_t><<<grid, 256, 0, st>>>(a);
     return vla_check_launch("paged_append");
+}
+
+extern "C" int vla_paged_append(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_rotary *rotary, const void *q,
+                                const void *k, const void *v, int in_dtype, int n_heads, int64_t q_stride, int64_t k_stride,
+                                int64_t v_stride, void *q_out, int64_t q_out_stride, void *stream) {
+    return append(cache, batch, rotary, nullptr, q, k, v, in_dtype, n_heads, q_stride, k_stride, v_stride, q_out, q_out_stride, stream);
+}
+extern "C" int vla_paged_append_at(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_rotary *rotary, const int32_t *position,
+                                   const void *q, const void *k, const void *v, int in_dtype, int n_heads, int64_t q_stride, int64_t k_stride,
+                                   int64_t v_stride, void *q_out, int64_t q_out_stride, void *stream) {
+    if (batch && batch->n_rows > 0 && !position) { vla_set_error("paged_append_at: position is NULL"); return VLA_EINVAL; }
+    return append(cache, batch, rotary, position, q, k, v, in_dtype, n_heads, q_stride, k_stride, v_stride, q_out, q_out_stride, stream);
 }

@@ -1,0 +1,463 @@
+// Sparse attention on a paged KV cache: bounds of each page's keys, the pages that a row's heads read, and the attention over them.
+//
+// For a key k of a page with lo <= k <= hi (dim by dim), q.k <= sum_d max(q_d lo_d, q_d hi_d).  Summed over the heads of a group that is
+// (sum_h max(q_h, 0)) . hi + (sum_h min(q_h, 0)) . lo: two products a dim whatever the group, in fp64, where the sums of bf16 products are exact
+// but for the last bits and the order of additions decides no border.
+#include "paged_rows.h"
+
+namespace {
+
+// ---- bounds ----------------------------------------------------------------------------------------------------------------
+// A workgroup for each (page, sequence): its lanes each hold eight dims of one key head (16 bytes of bf16, 32 of fp32).  Reads the keys
+// below kv_len of a page once and writes two rows a head.
+template <typename T>
+__global__ void __launch_bounds__(256) paged_bounds_kernel(PagedView pv, T *bounds) {
+    typedef T t8 __attribute__((ext_vector_type(8)));
+    const int s = blockIdx.x, page_size = 1 << pv.page_log, chunks = pv.d / 8;
+    const PagedSeq sq = paged_seq(pv, s);
+    if (sq.rows == 0) return;
+    const int number = (max(sq.len - sq.n, 0) >> pv.page_log) + blockIdx.y, key0 = number << pv.page_log;
+    if (key0 >= sq.keys) return;
+    const int page = paged_int(pv.table, (size_t)s * pv.table_stride + number), n = min(page_size, sq.keys - key0);
+    if ((unsigned)page >= (unsigned)pv.n_pages) return;
+    for (int x = threadIdx.x; x < pv.n_kv * chunks; x += 256) {
+        const int h = x / chunks, c = x - h * chunks;
+        const T *k = (const T *)pv.k + (((size_t)page * pv.n_kv + h) << pv.page_log) * pv.d + c * 8;
+        t8 v = *(const t8 *)k;
+        float lo[8], hi[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) lo[e] = hi[e] = (float)v[e];
+        for (int i = 1; i < n; i++) {
+            v = *(const t8 *)(k + (size_t)i * pv.d);
+#pragma unroll
+            for (int e = 0; e < 8; e++) { lo[e] = fminf(lo[e], (float)v[e]); hi[e] = fmaxf(hi[e], (float)v[e]); }
+        }
+        T *to = bounds + ((size_t)page * pv.n_kv + h) * 2 * pv.d + c * 8;
+        t8 a, b;
+#pragma unroll
+        for (int e = 0; e < 8; e++) { a[e] = (T)lo[e]; b[e] = (T)hi[e]; }
+        *(t8 *)to = a;
+        *(t8 *)(to + pv.d) = b;
+    }
+}
+
+// ---- selection -------------------------------------------------------------------------------------------------------------
+struct SelectArgs {
+    PagedView pv;
+    const void *bounds, *q;
+    long q_stride;
+    int group, n_select, first, recent;
+    int pages;               // of a sequence at most
+    unsigned long long *keys;  // [n_rows][n_kv][pages]: scores, in an order of whole numbers
+    int32_t *selected;
+};
+
+// Scores as numbers that ascend with them; 0 for NaN.
+__device__ __forceinline__ unsigned long long order_of(double x) {
+    if (x != x) return 0;
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, x + 0.0);          // (-0 is 0)
+    return u >> 63 ? ~u : u | 1ull << 63;
+}
+
+// A row's place: its sequence's table and the number of its page, -1 where it has none.
+__device__ __forceinline__ int page_of_row(const PagedView &pv, int row, int *s) {
+    *s = paged_seq_of_row(pv, row);
+    if (*s >= pv.n_seq) return -2;                            // padding
+    const PagedSeq sq = paged_seq(pv, *s);
+    const int i = row - sq.r0, p = min(sq.len - sq.n + i, sq.keys - 1);
+    if (i < 0 || i >= sq.rows) return -2;
+    return p < 0 ? -1 : p >> pv.page_log;
+}
+
+// One wave a page, its lanes each some dims of lo or hi; four pages of a (row, key head) a workgroup at a time.
+template <typename T>
+__global__ void __launch_bounds__(256) paged_score_kernel(SelectArgs a) {
+    __shared__ double part[2][256];                          // the group's positive and negative parts of q
+    const PagedView &pv = a.pv;
+    const int h = blockIdx.x % pv.n_kv, row = blockIdx.x / pv.n_kv, t = threadIdx.x, lane = t & 63;
+    int s;
+    const int last = page_of_row(pv, row, &s);
+    if (last < 0) return;
+    for (int e = t; e < pv.d; e += 256) {
+        const T *q = (const T *)a.q + row * a.q_stride + (size_t)h * a.group * pv.d + e;
+        double up = 0.0, down = 0.0;
+        for (int g = 0; g < a.group; g++) {
+            const double x = (double)(float)q[(size_t)g * pv.d];
+            up += x > 0.0 ? x : 0.0;
+            down += x > 0.0 ? 0.0 : x;
+        }
+        part[0][e] = down;
+        part[1][e] = up;
+    }
+    __syncthreads();
+    const int32_t *table = pv.table + (size_t)s * pv.table_stride;
+    for (int n = blockIdx.y * 4 + (t >> 6); n <= last; n += gridDim.y * 4) {
+        const int page = table[n];
+        double x = 0.0;
+        if ((unsigned)page < (unsigned)pv.n_pages) {
+            const T *b = (const T *)a.bounds + ((size_t)page * pv.n_kv + h) * 2 * pv.d;
+            for (int e = lane; e < 2 * pv.d; e += 64) x += (double)(float)b[e] * (e < pv.d ? part[0][e] : part[1][e - pv.d]);
+        }
+        for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+        if (lane == 0) a.keys[((size_t)row * pv.n_kv + h) * a.pages + n] = order_of(x);
+    }
+}
+
+// Exclusive sum over a workgroup's threads; *all: the total.  red: one int a wave.
+template <int THREADS> __device__ __forceinline__ int block_scan(int v, int *all, int *red) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int in = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int x = __shfl_up(in, o, 64); if (lane >= o) in += x; }
+    __syncthreads();
+    if (lane == 63) red[wave] = in;
+    __syncthreads();
+    int before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; w++) { if (w < wave) before += red[w]; total += red[w]; }
+    *all = total;
+    return before + in - v;
+}
+
+// A workgroup for each (row, key head): the keys to LDS, the smallest that is taken digit by digit (eight bits a time, counted in LDS), then the
+// numbers of what is above it and of the first that equal it, in order.
+__global__ void __launch_bounds__(256) paged_select_kernel(SelectArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ int bins[256], red[4], digit, rest;
+    unsigned long long *key = (unsigned long long *)lds;
+    const PagedView &pv = a.pv;
+    const int h = blockIdx.x % pv.n_kv, row = blockIdx.x / pv.n_kv, t = threadIdx.x;
+    int s;
+    const int last = page_of_row(pv, row, &s), n = last + 1;
+    if (last < -1) return;
+    int32_t *out = a.selected + ((size_t)row * pv.n_kv + h) * a.n_select;
+    if (n <= a.n_select) {
+        for (int i = t; i < a.n_select; i += 256) out[i] = i < n ? i : -1;
+        return;
+    }
+    // free to choose: [first, n - recent); of these `want` (more than there are pages by one at least are left out)
+    const int lo = min(a.first, n), hi = n - a.recent;
+    const unsigned long long *src = a.keys + ((size_t)row * pv.n_kv + h) * a.pages;
+    for (int i = lo + t; i < hi; i += 256) key[i] = src[i];
+    int want = a.n_select - a.first - a.recent;
+    unsigned long long prefix = 0, mask = 0;
+    for (int shift = 56; shift >= 0 && want > 0; shift -= 8) {
+        bins[t] = 0;
+        __syncthreads();
+        for (int i = lo + t; i < hi; i += 256)
+            if ((key[i] & mask) == prefix) atomicAdd(&bins[key[i] >> shift & 255], 1);
+        __syncthreads();
+        // the digit at which the count from above reaches `want`: thread t has digit 255 - t
+        int all;
+        const int c = bins[255 - t], above = block_scan<256>(c, &all, red);
+        if (above < want && above + c >= want) { digit = 255 - t; rest = want - above; }
+        __syncthreads();
+        want = rest;
+        prefix |= (unsigned long long)digit << shift;
+        mask |= 255ull << shift;
+        __syncthreads();
+    }
+    if (a.n_select == a.first + a.recent) prefix = ~0ull;    // (no key is that: none is taken)
+    int done = 0, equal = 0;
+    for (int i0 = 0; i0 < n; i0 += 256) {
+        const int i = i0 + t;
+        const bool open = i >= lo && i < hi, tie = open && key[i] == prefix;
+        int ties, taken;
+        const int e = block_scan<256>(tie, &ties, red);
+        const bool take = i < n && (!open || key[i] > prefix || (tie && equal + e < want));
+        const int at = block_scan<256>(take, &taken, red);
+        if (take) out[done + at] = i;
+        done += taken;
+        equal += ties;
+    }
+}
+
+// ---- attention over the selected pages ----------------------------------------------------------------------------------------
+struct SparseArgs {
+    AttnArgs a;
+    const int32_t *selected;
+    int n_select, heads_tiles;               // tiles of 32 heads of a group
+};
+
+// Keys are taken 16 at a time (a page's run of them), two such runs to a tile of 32, through the same ring and products as paged_decode_kernel.
+// A workgroup is one wave: of one row and key head, up to 32 heads of its group, and a part of its list.
+template <typename T, int DP, int MODE>
+__global__ void __launch_bounds__(64) paged_sparse_kernel(SparseArgs x) {
+    typedef Tile<T, DP> TL;
+    constexpr int BYTES = 32 * TL::ROW, STAGE = 2 * BYTES, LOADS = 4 * 16 / TL::RPI;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const unsigned ring0 = (unsigned)(size_t)(lds_void *)lds;
+    const AttnArgs &a = x.a;
+    const PagedView &pv = a.pv;
+    const int lane = threadIdx.x, part = blockIdx.y;
+    const unsigned id = blockIdx.x / (unsigned)pv.n_kv;
+    const int kvh = blockIdx.x % (unsigned)pv.n_kv, ht = id % (unsigned)x.heads_tiles, row = id / (unsigned)x.heads_tiles;
+    const int s = paged_seq_of_row(pv, row);
+    if (s >= pv.n_seq) return;
+    const PagedSeq sq = paged_seq(pv, s);
+    const int i = row - sq.r0;
+    if (i < 0 || i >= sq.rows) return;
+    const int p = min(sq.len - sq.n + i, sq.keys - 1);       // the last position it sees
+    const int32_t *list = x.selected + ((size_t)row * pv.n_kv + kvh) * x.n_select, *table = pv.table + (size_t)s * pv.table_stride;
+    int m = 0;                                               // entries before the first negative one
+    for (; m < x.n_select; m += 64) {
+        const int e = m + lane;
+        const unsigned long long ends = __ballot(e >= x.n_select || list[e] < 0);
+        if (ends) { m += __builtin_ctzll(ends); break; }
+    }
+    m = __builtin_amdgcn_readfirstlane(min(m, x.n_select));
+    const int per_log = pv.page_log - 4, runs = p < 0 ? 0 : m << per_log, tiles = (runs + 1) / 2;
+    const int share = __builtin_amdgcn_readfirstlane((unsigned)(tiles + a.parts - 1) / (unsigned)a.parts), t0 = min(part * share, tiles), t1 = min(t0 + share, tiles);
+    // run r: where its 16 keys begin, and their page; a run that nothing sees begins behind p
+    auto run_of = [&](int r, int *page) __attribute__((always_inline)) {
+        *page = -1;
+        if (r >= runs) return p + 1;
+        const int e = r >> per_log, number = paged_int(list, e), before = e ? paged_int(list, e - 1) : -1;
+        const long key = ((long)number << pv.page_log) + (r & ((1 << per_log) - 1)) * 16;
+        if (number <= before || key > p) return p + 1;
+        *page = paged_int(table, number);
+        return (int)key;
+    };
+    typename TL::template Offsets<false, 16> off_k;
+    typename TL::template Offsets<true, 16> off_v;
+    off_k.start(pv, 0);
+    off_v.start(pv, 0);
+    const Place place(pv, kvh, sizeof(T));
+    int begin[2][2];                                         // of the tiles in the ring's stages
+    auto load_run = [&](unsigned at, int key, int page) __attribute__((always_inline)) {
+        if (key + 15 <= p || key > p) {                      // (behind p: zeros)
+            const size_t from = place.at(pv, page, key);
+            off_k.load(at, place.in(pv, pv.k, key > p ? -1 : page, from));
+            off_v.load(at + BYTES, place.in(pv, pv.v, key > p ? -1 : page, from));
+        } else {
+            const Span sp{key, p + 1, 0, 0};
+            TL::template load<false, 16>(at, pv.k, pv, page, kvh, key, sp);
+            TL::template load<true, 16>(at + BYTES, pv.v, pv, page, kvh, key, sp);
+        }
+    };
+    auto load = [&](int t, int stage) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            int page;
+            const int key = run_of(2 * t + u, &page);
+            if (stage) begin[1][u] = key; else begin[0][u] = key;
+            load_run(ring0 + stage * STAGE + u * 16 * TL::ROW, key, page);
+        }
+    };
+    if (t0 < t1) load(t0, 0);
+    Query y{};
+    y.row = row;
+    y.valid = ht * 32 + (lane & 31) < a.group;
+    y.head = kvh * a.group + min(ht * 32 + (lane & 31), a.group - 1);
+    Rows<T, DP, MODE, sizeof(T) == 2> rows;
+    rows.start(a, y);
+    auto step = [&](int t, int stage) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (t + 1 < t1) { load(t + 1, stage ^ 1); vm_wait<LOADS>(); }
+        else vm_wait<0>();
+        const char *kt = lds + stage * STAGE;
+        f32x16_t z;
+        typename Rows<T, DP, MODE, sizeof(T) == 2>::Weights w;
+        rows.scores(z, kt);
+#pragma unroll
+        for (int k = 0; k < 16; k++) z[k] = rows.shaped(z[k], a, y, 0, k);
+        const int hh = (lane >> 5) & 1;
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+            if (begin[stage][u] + 15 > p) {
+#pragma unroll
+                for (int k = 0; k < 8; k++)
+                    if (begin[stage][u] + 8 * (k / 4) + 4 * hh + k % 4 > p) z[8 * u + k] = -INFINITY;
+            }
+        rows.move_to(rows.largest(z, rows.unit_of(a)));
+        rows.weights(w, z, rows.unit_of(a));
+        rows.values(w, kt + BYTES);
+    };
+    for (int t = t0; t < t1; t += 2) {
+        step(t, 0);
+        if (t + 1 < t1) step(t + 1, 1);
+    }
+    rows.finish(a, y, part);
+}
+
+int check_bounds(const char *what, const void *bounds) {
+    if (!bounds) { vla_set_error("%s: bounds is NULL", what); return VLA_EINVAL; }
+    if ((uintptr_t)bounds % 16) { vla_set_error("%s: bounds is not 16-byte aligned", what); return VLA_EINVAL; }
+    return VLA_OK;
+}
+int check_pages(const PagedView &pv, SelectArgs *a) {
+    a->pv = pv;
+    a->pages = (pv.max_len + (1 << pv.page_log) - 1) >> pv.page_log;
+    if (a->pages > VLA_SELECT_PAGES) { vla_set_error("paged_select: %d pages of a sequence (at most %d)", a->pages, VLA_SELECT_PAGES); return VLA_ESHAPE; }
+    if ((long)pv.n_rows * pv.n_kv > 0x7fffffffL / 256) { vla_set_error("paged_select: %d rows of %d key heads are too many", pv.n_rows, pv.n_kv); return VLA_ESHAPE; }
+    return VLA_OK;
+}
+size_t select_bytes(const SelectArgs &a) { return round_up((size_t)a.pv.n_rows * a.pv.n_kv * a.pages * 8 + 1); }
+
+int check_sparse(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, int n_heads, int n_select, SparseArgs *x) {
+    AttnArgs &a = x->a;
+    const char *what = "paged_sparse_attention";
+    if (int rc = vla_check_paged(what, cache, batch, &a.pv)) return rc;
+    if (!mask) { vla_set_error("%s: mask is NULL", what); return VLA_EINVAL; }
+    if (n_heads <= 0 || n_heads % cache->n_kv_heads) { vla_set_error("%s: n_heads %d is no multiple of n_kv_heads %d", what, n_heads, cache->n_kv_heads); return VLA_ESHAPE; }
+    if (n_heads > 4096) { vla_set_error("%s: n_heads %d unsupported (at most 4096)", what, n_heads); return VLA_ESHAPE; }
+    if (!(mask->scale > 0.f) || !(mask->softcap >= 0.f) || !(mask->scale < INFINITY) || !(mask->softcap < INFINITY)) {
+        vla_set_error("%s: scale must be positive, softcap not negative, both finite", what);
+        return VLA_EINVAL;
+    }
+    if (mask->slopes || mask->prefix_len || mask->window || mask->shared_len) {
+        vla_set_error("%s: slopes, prefix_len, window and shared_len have no meaning here", what);
+        return VLA_EINVAL;
+    }
+    if (n_select < 1 || n_select > VLA_SELECT_PAGES) { vla_set_error("%s: n_select %d unsupported (1 .. %d)", what, n_select, VLA_SELECT_PAGES); return VLA_ESHAPE; }
+    a.n_heads = n_heads; a.group = n_heads / cache->n_kv_heads;
+    a.scale = mask->scale; a.cap = mask->softcap;
+    x->n_select = n_select;
+    x->heads_tiles = (a.group + 31) / 32;
+    if ((long)batch->n_rows * cache->n_kv_heads * x->heads_tiles > 0x7fffffffL / 256 || (long)batch->n_rows * n_heads > 0x7fffffffL / 2) {
+        vla_set_error("%s: %d rows of %d heads are too many", what, batch->n_rows, n_heads);
+        return VLA_ESHAPE;
+    }
+    return VLA_OK;
+}
+// Waves enough to fill the chip, each with two tiles at least.
+void plan_sparse(SparseArgs *x, bool f32) {
+    AttnArgs &a = x->a;
+    const long items = (long)a.pv.n_rows * a.pv.n_kv * x->heads_tiles;
+    long pages = (a.pv.max_len + (1 << a.pv.page_log) - 1) >> a.pv.page_log;
+    if (pages > x->n_select) pages = x->n_select;
+    const long tiles = ((pages << a.pv.page_log) + 31) / 32;
+    const int fit = 128 / ((128 * padded_dim(a.pv.d) * (f32 ? 4 : 2) + 1279) / 1280);
+    const long waves = 256 * (fit > 8 ? 8 : fit);
+    long parts = items > 0 ? waves / items : 1;
+    if (parts > tiles / 2) parts = tiles / 2;
+    a.parts = (int)(parts < 1 ? 1 : parts);
+}
+size_t lay_out(AttnArgs *a, char *base) {
+    if (a->parts <= 1) return 256;
+    const size_t slots = (size_t)a->pv.n_rows * a->n_heads * a->parts, ml = round_up(slots * sizeof(float2));
+    a->ml = (float2 *)base;
+    a->o_part = (float *)(base + ml);
+    return ml + round_up(slots * a->pv.d * sizeof(float));
+}
+
+template <typename T, int DP, int MODE>
+int launch(const SparseArgs &x, hipStream_t st) {
+    const AttnArgs &a = x.a;
+    constexpr size_t bytes = 2 * 2 * 32 * Tile<T, DP>::ROW;
+    if (int rc = vla_allow_lds((const void *)paged_sparse_kernel<T, DP, MODE>, bytes)) return rc;
+    paged_sparse_kernel<T, DP, MODE><<<dim3(a.pv.n_rows * a.pv.n_kv * x.heads_tiles, a.parts), 64, bytes, st>>>(x);
+    if (int rc = vla_check_launch("paged_sparse_attention")) return rc;
+    if (a.parts == 1) return VLA_OK;
+    const int heads = (2048 + a.pv.n_rows - 1) / a.pv.n_rows;
+    paged_join_kernel<T, DP><<<dim3(a.pv.n_rows, heads < a.n_heads ? heads : a.n_heads), 256, 0, st>>>(a);
+    return vla_check_launch("paged_sparse_attention join");
+}
+template <typename T, int MODE>
+int launch_sized(const SparseArgs &x, hipStream_t st) {
+    switch (padded_dim(x.a.pv.d)) {
+        case 64: return launch<T, 64, MODE>(x, st);
+        case 128: return launch<T, 128, MODE>(x, st);
+        default: return launch<T, 256, MODE>(x, st);
+    }
+}
+template <typename T> int launch_typed(const SparseArgs &x, hipStream_t st) { return x.a.cap > 0.f ? launch_sized<T, CAPPED>(x, st) : launch_sized<T, 0>(x, st); }
+
+}  // namespace
+
+extern "C" {
+
+int vla_paged_bounds(const vla_paged_cache *cache, const vla_paged_batch *batch, void *bounds, void *stream) {
+    PagedView pv;
+    if (int rc = vla_check_paged("paged_bounds", cache, batch, &pv)) return rc;
+    if (int rc = check_bounds("paged_bounds", bounds)) return rc;
+    if (pv.n_rows == 0 || pv.max_rows == 0 || pv.max_len == 0) return VLA_OK;
+    // pages that max_rows rows may touch, whatever the first one's place in its page
+    const int size = 1 << pv.page_log, all = (pv.max_len + size - 1) >> pv.page_log, some = (int)(((long)pv.max_rows + size - 2) >> pv.page_log) + 1, pages = some < all ? some : all;
+    if (pages > 65535) { vla_set_error("paged_bounds: rows on %d pages of a sequence (at most 65,535)", pages); return VLA_ESHAPE; }
+    hipStream_t st = (hipStream_t)stream;
+    ProfScope ps("paged_bounds", 0.0, st);
+    if (cache->dtype == VLA_DTYPE_F32) paged_bounds_kernel<float><<<dim3(pv.n_seq, pages), 256, 0, st>>>(pv, (float *)bounds);
+    else paged_bounds_kernel<bf16_t><<<dim3(pv.n_seq, pages), 256, 0, st>>>(pv, (bf16_t *)bounds);
+    return vla_check_launch("paged_bounds");
+}
+
+size_t vla_paged_select_workspace_bytes(const vla_paged_cache *cache, const vla_paged_batch *batch) {
+    PagedView pv;
+    SelectArgs a{};
+    if (vla_check_paged("paged_select", cache, batch, &pv) || check_pages(pv, &a)) return 0;
+    return select_bytes(a);
+}
+
+int vla_paged_select(const vla_paged_cache *cache, const vla_paged_batch *batch, const void *bounds, const void *q, int n_heads,
+                     int64_t q_stride, int n_select, int first, int recent, int32_t *selected, void *ws, size_t ws_bytes, void *stream) {
+    PagedView pv;
+    SelectArgs a{};
+    if (int rc = vla_check_paged("paged_select", cache, batch, &pv)) return rc;
+    if (int rc = check_pages(pv, &a)) return rc;
+    if (int rc = check_bounds("paged_select", bounds)) return rc;
+    if (n_heads <= 0 || n_heads % cache->n_kv_heads) { vla_set_error("paged_select: n_heads %d is no multiple of n_kv_heads %d", n_heads, cache->n_kv_heads); return VLA_ESHAPE; }
+    if (n_heads > 4096) { vla_set_error("paged_select: n_heads %d unsupported (at most 4096)", n_heads); return VLA_ESHAPE; }
+    if (first < 0 || recent < 1 || n_select > VLA_SELECT_PAGES || (long)first + recent > n_select) {
+        vla_set_error("paged_select: n_select %d, first %d, recent %d (recent at least 1, n_select from first + recent to %d)", n_select, first, recent, VLA_SELECT_PAGES);
+        return VLA_EINVAL;
+    }
+    if (batch->n_rows > 0 && (!q || !selected || !ws)) { vla_set_error("paged_select: q, selected or ws is NULL"); return VLA_EINVAL; }
+    if ((uintptr_t)ws % 16) { vla_set_error("paged_select: ws is not 16-byte aligned"); return VLA_EINVAL; }
+    if (q_stride < (int64_t)n_heads * cache->head_dim) { vla_set_error("paged_select: a row stride is shorter than its heads"); return VLA_ESHAPE; }
+    if (batch->n_rows > 0 && ws_bytes < select_bytes(a)) { vla_set_error("paged_select: workspace %zu bytes, need %zu", ws_bytes, select_bytes(a)); return VLA_EWORKSPACE; }
+    if (batch->n_rows == 0 || batch->max_rows == 0) return VLA_OK;
+    a.bounds = bounds; a.q = q; a.q_stride = q_stride; a.group = n_heads / cache->n_kv_heads;
+    a.n_select = n_select; a.first = first; a.recent = recent; a.keys = (unsigned long long *)ws; a.selected = selected;
+    hipStream_t st = (hipStream_t)stream;
+    ProfScope ps("paged_select", 0.0, st);
+    const int items = pv.n_rows * pv.n_kv;
+    if (a.pages > n_select) {
+        int y = (4096 + items - 1) / items;
+        if (y > (a.pages + 3) / 4) y = (a.pages + 3) / 4;
+        if (cache->dtype == VLA_DTYPE_F32) paged_score_kernel<float><<<dim3(items, y), 256, 0, st>>>(a);
+        else paged_score_kernel<bf16_t><<<dim3(items, y), 256, 0, st>>>(a);
+        if (int rc = vla_check_launch("paged_select scores")) return rc;
+    }
+    const size_t lds = (size_t)a.pages * 8;
+    if (int rc = vla_allow_lds((const void *)paged_select_kernel, VLA_SELECT_PAGES * 8)) return rc;
+    paged_select_kernel<<<items, 256, lds, st>>>(a);
+    return vla_check_launch("paged_select");
+}
+
+size_t vla_paged_sparse_attention_workspace_bytes(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask,
+                                                  int n_heads, int n_select) {
+    SparseArgs x{};
+    if (check_sparse(cache, batch, mask, n_heads, n_select, &x)) return 0;
+    plan_sparse(&x, cache->dtype == VLA_DTYPE_F32);
+    return lay_out(&x.a, nullptr);
+}
+
+int vla_paged_sparse_attention(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask,
+                               const int32_t *selected, int n_select, const void *q, int n_heads, int64_t q_stride, void *out,
+                               int64_t out_stride, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    SparseArgs x{};
+    AttnArgs &a = x.a;
+    if (int rc = check_sparse(cache, batch, mask, n_heads, n_select, &x)) return rc;
+    const bool f32 = cache->dtype == VLA_DTYPE_F32;
+    if (batch->n_rows > 0 && (!selected || !q || !out || !ws)) { vla_set_error("paged_sparse_attention: selected, q, out or ws is NULL"); return VLA_EINVAL; }
+    if ((uintptr_t)ws % 16) { vla_set_error("paged_sparse_attention: ws is not 16-byte aligned"); return VLA_EINVAL; }
+    if (q_stride < (int64_t)n_heads * cache->head_dim || out_stride < (int64_t)n_heads * cache->head_dim) {
+        vla_set_error("paged_sparse_attention: a row stride is shorter than its heads");
+        return VLA_ESHAPE;
+    }
+    plan_sparse(&x, f32);
+    const size_t need = lay_out(&a, (char *)ws);
+    if (batch->n_rows > 0 && ws_bytes < need) { vla_set_error("paged_sparse_attention: workspace %zu bytes, need %zu", ws_bytes, need); return VLA_EWORKSPACE; }
+    if (batch->n_rows == 0 || batch->max_rows == 0) return VLA_OK;
+    const size_t es = f32 ? 4 : 2;
+    x.selected = selected;
+    a.q = (const char *)q; a.out = (char *)out; a.lse = lse; a.q_stride = q_stride; a.o_stride = out_stride;
+    a.aligned = ((uintptr_t)q | (uintptr_t)out | (size_t)q_stride * es | (size_t)out_stride * es) % 16 == 0;
+    a.offset = !f32 ? a.cap * LOG2E : 0.f;
+    hipStream_t st = (hipStream_t)stream;
+    ProfScope ps("paged_sparse_attention", 0.0, st);
+    return f32 ? launch_typed<float>(x, st) : launch_typed<bf16_t>(x, st);
+}
+
+}  // extern "C"
