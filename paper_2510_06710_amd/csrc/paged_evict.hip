@@ -6,108 +6,357 @@ namespace {
 
 // ---- weights -----------------------------------------------------------------------------------------------------------------
 // One product, S = Q K^T (rows queries, columns keys, on 32 x 32 matrix instructions), so a lane owns a key: its weights' sum over the queries is a
-// sum over the lane's registers (and lane ^ 32).  A wave keeps 32 keys in registers and takes the packed rows (query r / group, head
-// r % group of a key head's group) that may see them 32 at a time.
+// sum over the lane's registers (and lane ^ 32).  The packed rows are those of paged_attention.hip: query r / group, head r % group of a key head's
+// group.  Two forms: few packed rows stay in registers and the keys stream by (paged_weights_step_kernel); of many, the keys stay and the
+// rows stream (paged_weights_rows_kernel), in parts that paged_weights_join_kernel adds up in order.
 struct WeightArgs {
     AttnArgs a;
     const float *lse_in;
-    float *mass;
+    float *mass, *part;      // part: [parts][n_seq][n_kv][max_len]
     long mass_stride;
+    int chunk;               // tiles of keys (step) or of packed rows (rows) of one workgroup
+    int parts;
 };
 
-constexpr int WEIGHT_WAVES = 4;
+// The packed rows of a sequence, as tiles of 32, that may see one of the keys key0 .. key0 + n - 1: positions key0 on, below key0 + n - 1 + window; all where the prefix reaches.
+struct RowTiles { int t0, t1; };
+__device__ __forceinline__ int prefix_of(const AttnArgs &a, int s, const PagedSeq &sq) { return a.prefix_len ? min(max(paged_int(a.prefix_len, s), 0), sq.keys) : 0; }
+__device__ __forceinline__ RowTiles row_tiles(const AttnArgs &a, const PagedSeq &sq, int prefix, int key0, int n) {
+    const int base = sq.len - sq.n;
+    int i0 = max(0, key0 - base), i1 = sq.rows;
+    if (a.window) i1 = min(i1, max(0, key0 + n - 1 + a.window - base));
+    if (key0 < prefix) { i0 = 0; i1 = sq.rows; }
+    if (i0 >= i1) return {0, 0};
+    return {i0 * a.group / 32, (i1 * a.group + 31) / 32};
+}
+
+// The weights of one tile, in a lane sixteen rows' for its key: register 4 g + e is packed row 8 g + 4 hh + e.  l: lse in log2 units less the scores' offset; p: positions; masked: not all of them may
+// count.  Summed by fours first, so that a long sum has few steps of its own.
 template <typename T, int DP, int MODE>
-__global__ void __launch_bounds__(64 * WEIGHT_WAVES) paged_weights_kernel(WeightArgs w) {
-    typedef typename FragOf<T>::type frag;
-    constexpr int KS = DP / 16;
-    __shared__ __attribute__((aligned(16))) float lse_at[WEIGHT_WAVES][32], slope_at[WEIGHT_WAVES][32];
-    __shared__ __attribute__((aligned(16))) int pos_at[WEIGHT_WAVES][32];
+__device__ __forceinline__ float tile_weight(const AttnArgs &a, const f32x16_t &x, const float (&l)[16], const int (&p)[16], const float (&slope)[16], int key, int keys, int prefix, bool masked) {
+    const float unit = Rows<T, DP, MODE, false>::unit_of(a);
+    float sum[4];
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        float z = x[i];
+        if (MODE & CAPPED) z = sizeof(T) == 4 ? tanhf(z * (a.scale / a.cap)) : -__builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * (2.f * LOG2E * a.scale / a.cap)));
+        if (MODE & BIASED) {
+            const float factor = MODE & CAPPED ? (sizeof(T) == 4 ? 1.f : 2.f) * a.cap * LOG2E : a.scale * LOG2E;
+            z = __builtin_fmaf(-slope[i], fabsf((float)(p[i] - key)), z * factor);
+        }
+        float w = __builtin_amdgcn_exp2f(__builtin_fmaf(z, unit, -l[i]));
+        if (masked) {
+            const bool see = key < keys && ((key <= p[i] && (a.window == 0 || key > p[i] - a.window)) || key < prefix) && l[i] != -INFINITY;
+            w = see ? w : 0.f;
+        }
+        sum[i % 4] = i < 4 ? w : sum[i % 4] + w;
+    }
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+// One wave a workgroup: up to 32 packed rows of a sequence in registers, `chunk` tiles of 32 keys through a ring of three in LDS (rows of 16 keys of a page, as in
+// paged_attention.hip); the sums go to LDS and to memory at the end, when nothing else is on its way.
+constexpr int STEP_TILES = 16;               // of a chunk at most
+template <typename T, int DP, int MODE>
+__global__ void __launch_bounds__(64) paged_weights_step_kernel(WeightArgs w) {
+    typedef Tile<T, DP> TL;
+    typedef Rows<T, DP, MODE, false> R;
+    constexpr int KS = DP / 16, BYTES = 32 * TL::ROW, LOADS = 2 * 16 / TL::RPI;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ __attribute__((aligned(16))) float sums[STEP_TILES * 32], info[3][32];
+    const unsigned ring0 = (unsigned)(size_t)(lds_void *)lds;
     const AttnArgs &a = w.a;
     const PagedView &pv = a.pv;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, hh = lane >> 5;
-    int id = blockIdx.x;
-    const int kvh = id % pv.n_kv;
-    id /= pv.n_kv;
-    const int s = id % pv.n_seq, key0 = (id / pv.n_seq * WEIGHT_WAVES + wave) * 32;
+    const int lane = threadIdx.x, col = lane & 31, hh = lane >> 5;
+    const unsigned id = blockIdx.x / (unsigned)pv.n_kv;
+    const int kvh = blockIdx.x % (unsigned)pv.n_kv, s = id % (unsigned)pv.n_seq, chunk0 = __builtin_amdgcn_readfirstlane(id / (unsigned)pv.n_seq * w.chunk);
     const PagedSeq sq = paged_seq(pv, s);
-    if (key0 >= sq.keys) return;                              // (no barriers below)
-    const int base = sq.len - sq.n, key = key0 + col;
-    const int prefix = a.prefix_len ? min(max(paged_int(a.prefix_len, s), 0), sq.keys) : 0;
-    // rows that may see one of the keys: positions key0 on, below key0 + 31 + window; all where the prefix reaches
-    int i0 = max(0, key0 - base), i1 = sq.rows;
-    if (a.window) i1 = min(i1, max(0, key0 + 31 + a.window - base));
-    if (key0 < prefix) { i0 = 0; i1 = sq.rows; }
-    if (i0 >= i1 && base > key0 + 31) return;                 // nothing to add, and no new position to set
-    frag k[KS];
-    {
-        const int at = min(key, sq.keys - 1), page = paged_int(pv.table, (size_t)s * pv.table_stride + (min(key0 + (col & 16), sq.keys - 1) >> pv.page_log));
-        const bool ok = (unsigned)page < (unsigned)pv.n_pages;
-        const T *src = (const T *)(ok ? pv.k : (const char *)zero_rows) + (ok ? (((size_t)page * pv.n_kv + kvh << pv.page_log) + (at & ((1 << pv.page_log) - 1))) * pv.d : 0);
-#pragma unroll
-        for (int kk = 0; kk < KS; kk++) {
-            const int dim = kk * 16 + hh * 8;
-#pragma unroll
-            for (int e = 0; e < 8; e++) k[kk][e] = (T)0.f;
-            if (dim < pv.d) k[kk] = *(const frag *)(src + dim);
+    const int base = sq.len - sq.n, prefix = prefix_of(a, s, sq);
+    // tiles that a row sees or that hold new positions: all behind the first row's window, and before the prefix's end
+    const int from = a.window && prefix == 0 ? max(0, base + 1 - a.window) / 32 : 0;
+    const int t0 = max(from, chunk0), t1 = min(chunk0 + w.chunk, (sq.keys + 31) / 32);
+    if (t0 >= t1 || sq.rows == 0) return;
+    const Span sp{0, sq.keys, 0, 0};
+    const int32_t *table = pv.table + (size_t)s * pv.table_stride;
+    typename TL::template Offsets<false, 16> off;
+    off.start(pv, 0);
+    const Place place(pv, kvh, sizeof(T));
+    int p0 = sp.page(table, pv.page_log, t0 * 32), p1 = sp.page(table, pv.page_log, t0 * 32 + 16);
+    auto load = [&](int t, int stage) __attribute__((always_inline)) {
+        const unsigned at = ring0 + stage * BYTES;
+        if ((t + 1) * 32 <= sq.keys) {
+            off.load(at, place.in(pv, pv.k, p0, place.at(pv, p0, t * 32)));
+            off.load(at + 16 * TL::ROW, place.in(pv, pv.k, p1, place.at(pv, p1, t * 32 + 16)));
+        } else {
+            TL::template load<false, 16>(at, pv.k, pv, p0, kvh, t * 32, sp);
+            TL::template load<false, 16>(at + 16 * TL::ROW, pv.k, pv, p1, kvh, t * 32 + 16, sp);
         }
+        p0 = sp.page(table, pv.page_log, t * 32 + 32);
+        p1 = sp.page(table, pv.page_log, t * 32 + 48);
+    };
+    load(t0, 0);
+    if (t0 + 1 < t1) load(t0 + 1, 1);
+    Query y{};
+    const int i = col / a.group, hg = col - i * a.group;
+    y.valid = i < sq.rows;
+    y.row = sq.r0 + (y.valid ? i : 0);
+    y.head = kvh * a.group + hg;
+    if (hh == 0) {
+        const float l = y.valid ? w.lse_in[(size_t)y.row * a.n_heads + y.head] : -INFINITY;
+        info[0][col] = l == -INFINITY ? INFINITY : l * LOG2E - a.offset;          // (such a row's weights are exp2 of -inf)
+        info[1][col] = __builtin_bit_cast(float, y.valid ? base + i : 0x7fffffff);
+        info[2][col] = (MODE & BIASED) && y.valid ? a.slopes[y.head] * LOG2E : 0.f;
     }
-    const float unit = Rows<T, DP, MODE, false>::unit_of(a);
-    float sum = 0.f;
-    for (int r0 = i0 * a.group & ~31; r0 < i1 * a.group; r0 += 32) {
-        // a lane's packed row of the 32
-        const int r = r0 + col, i = r / a.group, head = kvh * a.group + r - i * a.group, row = sq.r0 + i;
-        const bool in = r < sq.rows * a.group;
-        if (hh == 0) {
-            float l = in ? w.lse_in[(size_t)row * a.n_heads + head] : -INFINITY;
-            // (a row that sees nothing adds nothing: its weights are exp2(x - inf))
-            lse_at[wave][col] = l == -INFINITY ? INFINITY : l * LOG2E - a.offset;
-            pos_at[wave][col] = base + i;
-            if (MODE & BIASED) slope_at[wave][col] = in ? a.slopes[head] * LOG2E : 0.f;
-        }
-        const T *src = (const T *)a.q + (size_t)(in ? row : sq.r0) * a.q_stride + (size_t)(in ? head : 0) * pv.d;
+    R rows;
+    rows.start(a, y);
+    float l[16], slope[16];
+    int p[16], low = 0x7fffffff;                              // low: the first row's position
+    bool odd = false;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+        const int at = 8 * (r / 4) + 4 * hh + r % 4;
+        l[r] = info[0][at];
+        p[r] = __builtin_bit_cast(int, info[1][at]);
+        slope[r] = info[2][at];
+        low = min(low, p[r]);
+        odd |= !(l[r] < INFINITY);
+    }
+    low = wave_min(low);
+    odd = __any(odd);
+    int stage = 0;
+    for (int t = t0; t < t1; t++) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // the reads of the stage that is loaded again are through
+        if (t + 2 < t1) { load(t + 2, stage >= 1 ? stage - 1 : 2); vm_wait<2 * LOADS>(); }
+        else if (t + 1 < t1) vm_wait<LOADS>();
+        else vm_wait<0>();
+        const char *kt = lds + stage * BYTES;
         f32x16_t x;
 #pragma unroll
         for (int e = 0; e < 16; e++) x[e] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < KS; kk++) {
-            const int dim = kk * 16 + hh * 8;
-            frag q;
+        for (int kk = 0; kk < KS; kk++) x = mma(rows.q[kk], R::key(kt, kk), x);
+        const bool masked = odd || t * 32 + 31 > low || (t + 1) * 32 > sq.keys || a.window;
+        float sum = tile_weight<T, DP, MODE>(a, x, l, p, slope, t * 32 + col, sq.keys, prefix, masked);
+        sum = vla_fold_step<32>(sum, VlaAdd());
+        if (hh == 0) sums[(t - chunk0) * 32 + col] = sum;
+        stage = stage == 2 ? 0 : stage + 1;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    float *mass = w.mass + ((size_t)s * pv.n_kv + kvh) * w.mass_stride;
+    for (int key = t0 * 32 + lane; key < min(t1 * 32, sq.keys); key += 64) {
+        const float sum = sums[key - chunk0 * 32];
+        mass[key] = key < base ? mass[key] + sum : sum;
+    }
+}
+
+// Four waves, each with KW tiles of 32 keys in registers; tiles of 32 packed rows of q come through a ring of four in LDS, a quarter loaded by each wave, with the rows' lse
+// beside them (a copy for each wave: no register is loaded inside the loop).  A row of q may start anywhere: where rows are no multiples of 16 bytes they go through registers.
+template <typename T, int DP, int MODE> constexpr int KEY_TILES = sizeof(T) * DP <= 256 ? 2 : 1;
+template <typename T, int DP, int MODE>
+__global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_weights_rows_kernel(WeightArgs w) {
+    typedef Tile<T, DP> TL;
+    typedef Rows<T, DP, MODE, false> R;
+    typedef typename FragOf<T>::type frag;
+    constexpr int KS = DP / 16, BYTES = 32 * TL::ROW, RG = 4, EACH = 8 / TL::RPI, LOADS = EACH + 1, KW = KEY_TILES<T, DP, MODE>, KEYS = 128 * KW;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ __attribute__((aligned(16))) float lse_at[RG][4][64];
+    const unsigned lds0 = (unsigned)(size_t)(lds_void *)lds, lse0 = (unsigned)(size_t)(lds_void *)&lse_at[0][0][0];
+    const AttnArgs &a = w.a;
+    const PagedView &pv = a.pv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, hh = lane >> 5;
+    const unsigned id = blockIdx.x / (unsigned)pv.n_kv;
+    const int kvh = blockIdx.x % (unsigned)pv.n_kv, s = id % (unsigned)pv.n_seq, block0 = (int)(id / (unsigned)pv.n_seq) * KEYS;
+    const PagedSeq sq = paged_seq(pv, s);
+    if (block0 >= sq.keys) return;
+    const int base = sq.len - sq.n, prefix = prefix_of(a, s, sq), rows = sq.rows * a.group;
+    const RowTiles all = row_tiles(a, sq, prefix, block0, KEYS);
+    const int t0 = max(all.t0, (int)blockIdx.y * w.chunk), t1 = min(all.t1, ((int)blockIdx.y + 1) * w.chunk), key0 = block0 + wave * 32 * KW;
+    if (w.parts > 1 ? t0 >= t1 : sq.rows == 0 || (all.t0 == all.t1 && base >= block0 + KEYS)) return;
+    // the keys, through the ring's place
+    const Span sp{0, sq.keys, 0, 0};
+    const int32_t *table = pv.table + (size_t)s * pv.table_stride;
+    frag k[KW][KS];
 #pragma unroll
-            for (int e = 0; e < 8; e++) q[e] = (T)0.f;
-            if (dim < pv.d && in) {
-                if (a.aligned) {
-                    q = *(const frag *)(src + dim);
-                } else {
+    for (int b = 0; b < KW; b++) {
 #pragma unroll
-                    for (int e = 0; e < 8; e++) q[e] = src[dim + e];
-                }
-            }
-            x = mma(q, k[kk], x);
+        for (int u = 0; u < 2; u++) {
+            const int at = key0 + b * 32 + u * 16;
+            TL::template load<false, 16>(lds0 + wave * BYTES + u * 16 * TL::ROW, pv.k, pv, sp.page(table, pv.page_log, at), kvh, at, sp);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // one wave's own LDS
+        vm_wait<0>();
 #pragma unroll
-        for (int g = 0; g < 4; g++) {                         // register 4 g + e is packed row r0 + 8 g + 4 hh + e
-            const f32x4_t l = *(const f32x4_t *)&lse_at[wave][8 * g + 4 * hh];
-            const i32x4_v p = *(const i32x4_v *)&pos_at[wave][8 * g + 4 * hh];
+        for (int kk = 0; kk < KS; kk++) {
+            k[b][kk] = R::key(lds + wave * BYTES, kk);
+            if (kk * 16 >= pv.d)                              // (LDS holds repeated values there, of q too)
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                float z = x[4 * g + e];
-                if (MODE & CAPPED) z = sizeof(T) == 4 ? tanhf(z * (a.scale / a.cap)) : -__builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * (2.f * LOG2E * a.scale / a.cap)));
-                if (MODE & BIASED) {
-                    const float factor = MODE & CAPPED ? (sizeof(T) == 4 ? 1.f : 2.f) * a.cap * LOG2E : a.scale * LOG2E;
-                    z = __builtin_fmaf(-slope_at[wave][8 * g + 4 * hh + e], fabsf((float)(p[e] - key)), z * factor);
-                }
-                const bool see = key < sq.keys && ((key <= p[e] && (a.window == 0 || key > p[e] - a.window)) || key < prefix);
-                sum += see ? __builtin_amdgcn_exp2f(__builtin_fmaf(z, unit, -l[e])) : 0.f;
-            }
+                for (int e = 0; e < 8; e++) k[b][kk][e] = (T)0.f;
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    sum = vla_fold_step<32>(sum, VlaAdd());
-    if (hh == 0 && key < sq.keys) {
-        float *m = w.mass + ((size_t)s * pv.n_kv + kvh) * w.mass_stride + key;
-        *m = key < base ? *m + sum : sum;
+    __syncthreads();
+    // a lane's part of a tile of rows: the row of each of its loads, and the row whose lse it loads
+    int at_i[EACH], at_h[EACH], l_i, l_h;
+    const int step_i = 32 / a.group, step_h = 32 % a.group;
+    {
+        int r = t0 * 32 + wave * 8 + lane / TL::CPR;
+#pragma unroll
+        for (int e = 0; e < EACH; e++, r += TL::RPI) { at_i[e] = r / a.group; at_h[e] = r - at_i[e] * a.group; }
+        r = t0 * 32 + col;
+        l_i = r / a.group;
+        l_h = r - l_i * a.group;
     }
+    auto load = [&](int t, int stage) __attribute__((always_inline)) {
+        if (t >= t1) return;
+        const unsigned at = lds0 + stage * BYTES + wave * 8 * TL::ROW;
+#pragma unroll
+        for (int e = 0; e < EACH; e++) {
+            const int r = wave * 8 + e * TL::RPI + lane / TL::CPR, c = min((lane % TL::CPR) ^ TL::fk(r), pv.d * (int)sizeof(T) / 16 - 1);
+            const int i = min(at_i[e], sq.rows - 1);          // (rows behind the last: the last's, which count for nothing)
+            const T *src = (const T *)a.q + (size_t)(sq.r0 + i) * a.q_stride + (size_t)(kvh * a.group + at_h[e]) * pv.d + c * (16 / (int)sizeof(T));
+            if (a.aligned) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at + e * 1024), "v"(src) : "memory");
+            else {
+                T x[16 / sizeof(T)];
+#pragma unroll
+                for (int z = 0; z < 16 / (int)sizeof(T); z++) x[z] = src[z];
+                __builtin_memcpy(lds + stage * BYTES + wave * 8 * TL::ROW + e * 1024 + lane * 16, x, 16);
+            }
+            at_i[e] += step_i;
+            at_h[e] += step_h;
+            if (at_h[e] >= a.group) { at_h[e] -= a.group; at_i[e]++; }
+        }
+        const float *l = w.lse_in + (size_t)(sq.r0 + min(l_i, sq.rows - 1)) * a.n_heads + kvh * a.group + l_h;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lse0 + (stage * 4 + wave) * 256), "v"(l) : "memory");
+        l_i += step_i;
+        l_h += step_h;
+        if (l_h >= a.group) { l_h -= a.group; l_i++; }
+    };
+#pragma unroll
+    for (int t = 0; t < RG - 1; t++) load(t0 + t, t);
+    float sum[KW];
+#pragma unroll
+    for (int b = 0; b < KW; b++) sum[b] = 0.f;
+    auto step = [&](int t, int stage) __attribute__((always_inline)) {
+        if (a.aligned) {
+            if (t + RG - 2 < t1) vm_wait<(RG - 2) * LOADS>();
+            else vm_wait<0>();
+        } else vm_wait<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        load(t + RG - 1, stage == 0 ? RG - 1 : stage - 1);
+        const char *qt = lds + stage * BYTES;
+        f32x16_t x[KW];
+#pragma unroll
+        for (int b = 0; b < KW; b++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) x[b][e] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KS; kk++) {
+            const frag q = R::key(qt, kk);
+#pragma unroll
+            for (int b = 0; b < KW; b++) x[b] = mma(q, k[b][kk], x[b]);
+        }
+        const float mine = lse_at[stage][wave][col];
+        float l[16], slope[16];
+        int p[16];
+        // every row there, its lse finite, and its position behind all of the wave's keys
+        const bool masked = t * 32 + 32 > rows || base + (int)((unsigned)(t * 32) / (unsigned)a.group) < key0 + 32 * KW - 1 || key0 + 32 * KW > sq.keys || a.window || __any(!(fabsf(mine) < INFINITY));
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+            const f32x4_t v = *(const f32x4_t *)&lse_at[stage][wave][8 * g + 4 * hh];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                l[4 * g + e] = MODE & CAPPED ? __builtin_fmaf(v[e], LOG2E, -a.offset) : v[e] * LOG2E;
+                p[4 * g + e] = 0;
+                slope[4 * g + e] = 0.f;
+            }
+        }
+        if (masked || (MODE & BIASED)) {
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                const int at = t * 32 + 8 * (r / 4) + 4 * hh + r % 4, i = at / a.group;
+                if (at >= rows) l[r] = -INFINITY;
+                p[r] = base + i;
+                if (MODE & BIASED) slope[r] = at < rows ? a.slopes[kvh * a.group + at - i * a.group] * LOG2E : 0.f;
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < KW; b++) sum[b] += tile_weight<T, DP, MODE>(a, x[b], l, p, slope, key0 + b * 32 + col, sq.keys, prefix, masked);
+    };
+    for (int t = t0; t < t1; t += RG) {
+        step(t, 0);
+        if (t + 1 < t1) step(t + 1, 1);
+        if (t + 2 < t1) step(t + 2, 2);
+        if (t + 3 < t1) step(t + 3, 3);
+    }
+#pragma unroll
+    for (int b = 0; b < KW; b++) {
+        const float all_of = vla_fold_step<32>(sum[b], VlaAdd());
+        const int key = key0 + b * 32 + col;
+        if (hh || key >= sq.keys) continue;
+        if (w.parts > 1) w.part[(((size_t)blockIdx.y * pv.n_seq + s) * pv.n_kv + kvh) * pv.max_len + key] = all_of;
+        else {
+            float *m = w.mass + ((size_t)s * pv.n_kv + kvh) * w.mass_stride + key;
+            *m = key < base ? *m + all_of : all_of;
+        }
+    }
+}
+
+// The parts of each position, in order.  keys: of a block of paged_weights_rows_kernel.
+__global__ void __launch_bounds__(256) paged_weights_join_kernel(WeightArgs w, int keys) {
+    const AttnArgs &a = w.a;
+    const PagedView &pv = a.pv;
+    const unsigned id = blockIdx.x / (unsigned)pv.n_kv;
+    const int kvh = blockIdx.x % (unsigned)pv.n_kv, s = id % (unsigned)pv.n_seq, key = (int)(id / (unsigned)pv.n_seq) * 256 + threadIdx.x;
+    const PagedSeq sq = paged_seq(pv, s);
+    if (key >= sq.keys || sq.rows == 0) return;
+    const int base = sq.len - sq.n;
+    const RowTiles all = row_tiles(a, sq, prefix_of(a, s, sq), key / keys * keys, keys);
+    float sum = 0.f;
+    const size_t step = (size_t)pv.n_seq * pv.n_kv * pv.max_len;
+    const float *part = w.part + ((size_t)s * pv.n_kv + kvh) * pv.max_len + key;
+    if (all.t0 < all.t1)
+#pragma unroll 8
+        for (int z = all.t0 / w.chunk; z <= (all.t1 - 1) / w.chunk; z++) sum += part[z * step];
+    float *m = w.mass + ((size_t)s * pv.n_kv + kvh) * w.mass_stride + key;
+    if (key >= base) *m = sum;
+    else if (all.t0 < all.t1) *m += sum;
+}
+
+// How a call is divided.
+struct WeightPlan {
+    bool step;
+    int chunk, parts;
+    long items;              // workgroups of a part
+};
+int weight_keys(int d, bool f32) { return 128 * (padded_dim(d) * (f32 ? 4 : 2) <= 256 ? 2 : 1); }
+WeightPlan plan_weights(const AttnArgs &a, bool f32) {
+    WeightPlan p{};
+    const PagedView &pv = a.pv;
+    const long pairs = (long)pv.n_kv * pv.n_seq, packed = (long)pv.max_rows * a.group;
+    p.step = packed <= 32;
+    p.parts = 1;
+    if (p.step) {
+        // waves that stay (their rings of 24 KB: six a CU) with a few tiles each, where there are so many
+        const long tiles = (pv.max_len + 31) / 32, all = pairs * tiles;
+        p.chunk = (int)(all / (6 * 256));
+        p.chunk = p.chunk < 2 ? 2 : p.chunk > STEP_TILES ? STEP_TILES : p.chunk;
+        p.items = pairs * ((tiles + p.chunk - 1) / p.chunk);
+        return p;
+    }
+    const int keys = weight_keys(pv.d, f32);
+    const long tiles = (packed + 31) / 32, blocks = pairs * ((pv.max_len + keys - 1) / keys);
+    // workgroups for four rounds of two a CU, with eight tiles of rows at least
+    long parts = blocks > 0 ? (4 * 512 + blocks - 1) / blocks : 1;
+    if (parts > tiles / 8) parts = tiles / 8;
+    if (parts > 256) parts = 256;
+    if (parts < 1) parts = 1;
+    p.chunk = (int)((tiles + parts - 1) / parts);
+    p.parts = (int)((tiles + p.chunk - 1) / p.chunk);
+    p.items = blocks;
+    return p;
+}
+size_t weight_bytes(const AttnArgs &a, const WeightPlan &p) {
+    return p.parts > 1 ? round_up((size_t)p.parts * a.pv.n_seq * a.pv.n_kv * a.pv.max_len * sizeof(float)) : 256;
 }
 
 int check_weights(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, int n_heads, AttnArgs *a) {
@@ -124,29 +373,45 @@ int check_weights(const vla_paged_cache *cache, const vla_paged_batch *batch, co
     if ((long)batch->n_rows * n_heads > 0x7fffffffL / 2) { vla_set_error("%s: %d rows of %d heads are too many", what, batch->n_rows, n_heads); return VLA_ESHAPE; }
     a->n_heads = n_heads; a->group = n_heads / cache->n_kv_heads;
     a->scale = mask->scale; a->cap = mask->softcap; a->slopes = mask->slopes; a->prefix_len = mask->prefix_len; a->window = mask->window;
-    const long items = (long)cache->n_kv_heads * batch->n_seq * ((batch->max_len + 32 * WEIGHT_WAVES - 1) / (32 * WEIGHT_WAVES));
-    if (items > 0x7fffffffL / 256) { vla_set_error("%s: %ld tiles of positions are too many: split the batch", what, items); return VLA_ESHAPE; }
+    const long items = plan_weights(*a, cache->dtype == VLA_DTYPE_F32).items, joins = (long)cache->n_kv_heads * batch->n_seq * ((batch->max_len + 255) / 256);
+    if (items > 0x7fffffffL / 256 || joins > 0x7fffffffL / 256) { vla_set_error("%s: %ld tiles of positions are too many: split the batch", what, items); return VLA_ESHAPE; }
     return VLA_OK;
 }
 
-template <typename T, int DP>
-int launch_weights(const WeightArgs &w, hipStream_t st) {
+template <typename T, int DP, int MODE>
+int launch_weights(WeightArgs w, const WeightPlan &p, hipStream_t st) {
     const PagedView &pv = w.a.pv;
-    const unsigned blocks = (unsigned)pv.n_kv * pv.n_seq * ((pv.max_len + 32 * WEIGHT_WAVES - 1) / (32 * WEIGHT_WAVES));
-    switch ((w.a.cap > 0.f ? CAPPED : 0) | (w.a.slopes ? BIASED : 0)) {
-        case 0: paged_weights_kernel<T, DP, 0><<<blocks, 64 * WEIGHT_WAVES, 0, st>>>(w); break;
-        case CAPPED: paged_weights_kernel<T, DP, CAPPED><<<blocks, 64 * WEIGHT_WAVES, 0, st>>>(w); break;
-        case BIASED: paged_weights_kernel<T, DP, BIASED><<<blocks, 64 * WEIGHT_WAVES, 0, st>>>(w); break;
-        default: paged_weights_kernel<T, DP, CAPPED | BIASED><<<blocks, 64 * WEIGHT_WAVES, 0, st>>>(w); break;
+    w.chunk = p.chunk;
+    w.parts = p.parts;
+    if (p.step) {
+        constexpr size_t bytes = 3 * 32 * Tile<T, DP>::ROW;
+        if (int rc = vla_allow_lds((const void *)paged_weights_step_kernel<T, DP, MODE>, bytes)) return rc;
+        paged_weights_step_kernel<T, DP, MODE><<<(unsigned)p.items, 64, bytes, st>>>(w);
+        return vla_check_launch("paged_weights");
     }
-    return vla_check_launch("paged_weights");
+    constexpr size_t bytes = 4 * 32 * Tile<T, DP>::ROW;
+    if (int rc = vla_allow_lds((const void *)paged_weights_rows_kernel<T, DP, MODE>, bytes)) return rc;
+    paged_weights_rows_kernel<T, DP, MODE><<<dim3((unsigned)p.items, p.parts), 256, bytes, st>>>(w);
+    if (int rc = vla_check_launch("paged_weights")) return rc;
+    if (p.parts == 1) return VLA_OK;
+    paged_weights_join_kernel<<<(unsigned)(pv.n_kv * pv.n_seq * ((pv.max_len + 255) / 256)), 256, 0, st>>>(w, 128 * KEY_TILES<T, DP, MODE>);
+    return vla_check_launch("paged_weights join");
+}
+template <typename T, int DP>
+int launch_weights_masked(const WeightArgs &w, const WeightPlan &p, hipStream_t st) {
+    switch ((w.a.cap > 0.f ? CAPPED : 0) | (w.a.slopes ? BIASED : 0)) {
+        case 0: return launch_weights<T, DP, 0>(w, p, st);
+        case CAPPED: return launch_weights<T, DP, CAPPED>(w, p, st);
+        case BIASED: return launch_weights<T, DP, BIASED>(w, p, st);
+        default: return launch_weights<T, DP, CAPPED | BIASED>(w, p, st);
+    }
 }
 template <typename T>
-int launch_weights_sized(const WeightArgs &w, hipStream_t st) {
+int launch_weights_sized(const WeightArgs &w, const WeightPlan &p, hipStream_t st) {
     switch (padded_dim(w.a.pv.d)) {
-        case 64: return launch_weights<T, 64>(w, st);
-        case 128: return launch_weights<T, 128>(w, st);
-        default: return launch_weights<T, 256>(w, st);
+        case 64: return launch_weights_masked<T, 64>(w, p, st);
+        case 128: return launch_weights_masked<T, 128>(w, p, st);
+        default: return launch_weights_masked<T, 256>(w, p, st);
     }
 }
 
@@ -285,7 +550,7 @@ extern "C" {
 
 size_t vla_paged_weights_workspace_bytes(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, int n_heads) {
     AttnArgs a{};
-    return check_weights(cache, batch, mask, n_heads, &a) ? 0 : 256;
+    return check_weights(cache, batch, mask, n_heads, &a) ? 0 : weight_bytes(a, plan_weights(a, cache->dtype == VLA_DTYPE_F32));
 }
 
 int vla_paged_weights(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_mask *mask, const void *q, int n_heads,
@@ -299,16 +564,17 @@ int vla_paged_weights(const vla_paged_cache *cache, const vla_paged_batch *batch
         vla_set_error("paged_weights: a row of q is shorter than its heads, or one of mass than max_len");
         return VLA_ESHAPE;
     }
-    if (batch->n_rows > 0 && ws_bytes < 256) { vla_set_error("paged_weights: workspace %zu bytes, need %d", ws_bytes, 256); return VLA_EWORKSPACE; }
-    if (batch->n_rows == 0 || batch->max_rows == 0 || batch->max_len == 0) return VLA_OK;
     const bool f32 = cache->dtype == VLA_DTYPE_F32;
+    const WeightPlan p = plan_weights(a, f32);
+    if (batch->n_rows > 0 && ws_bytes < weight_bytes(a, p)) { vla_set_error("paged_weights: workspace %zu bytes, need %zu", ws_bytes, weight_bytes(a, p)); return VLA_EWORKSPACE; }
+    if (batch->n_rows == 0 || batch->max_rows == 0 || batch->max_len == 0) return VLA_OK;
     a.q = (const char *)q; a.q_stride = q_stride;
     a.aligned = ((uintptr_t)q | (size_t)q_stride * (f32 ? 4 : 2)) % 16 == 0;
     a.offset = !f32 ? a.cap * LOG2E : 0.f;
-    w.lse_in = lse; w.mass = mass; w.mass_stride = mass_stride;
+    w.lse_in = lse; w.mass = mass; w.mass_stride = mass_stride; w.part = (float *)ws;
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps("paged_weights", 0.0, st);
-    return f32 ? launch_weights_sized<float>(w, st) : launch_weights_sized<bf16_t>(w, st);
+    return f32 ? launch_weights_sized<float>(w, p, st) : launch_weights_sized<bf16_t>(w, p, st);
 }
 
 int vla_paged_evict(const vla_paged_cache *cache, const vla_paged_batch *batch, const float *mass, int64_t mass_stride, int keep, int first,

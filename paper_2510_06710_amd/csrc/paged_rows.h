@@ -99,7 +99,7 @@ template <typename T, int DP> struct Tile {
     // ROWS rows from row r0 on of the 16 keys from key0 on (a multiple of 16: one page), of K or V.  Keys that no query of the tile sees are not read: outside [lo, hi)
     // the nearest one inside takes their place, in [g0, g1) the nearest one outside.
     template <bool V, int ROWS>
-    __device__ static void load(unsigned at, const char *pool, const PagedView &pv, int page, int kvh, int key0, const Span &sp, int r0 = 0) {
+    __device__ __forceinline__ static void load(unsigned at, const char *pool, const PagedView &pv, int page, int kvh, int key0, const Span &sp, int r0 = 0) {
         const int lane = threadIdx.x & 63, row_bytes = pv.d * (int)sizeof(T), chunks = row_bytes >> 4;
         const bool ok = (unsigned)page < (unsigned)pv.n_pages;
         const char *base = ok ? pool + (((size_t)page * pv.n_kv + kvh) << pv.page_log) * row_bytes : (const char *)zero_rows;
