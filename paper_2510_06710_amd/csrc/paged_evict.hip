@@ -30,23 +30,29 @@ __device__ __forceinline__ RowTiles row_tiles(const AttnArgs &a, const PagedSeq 
     return {i0 * a.group / 32, (i1 * a.group + 31) / 32};
 }
 
-// The weights of one tile, in a lane sixteen rows' for its key: register 4 g + e is packed row 8 g + 4 hh + e.  l: lse in log2 units less the scores' offset; p: positions; masked: not all of them may
-// count.  Summed by fours first, so that a long sum has few steps of its own.
-template <typename T, int DP, int MODE>
-__device__ __forceinline__ float tile_weight(const AttnArgs &a, const f32x16_t &x, const float (&l)[16], const int (&p)[16], const float (&slope)[16], int key, int keys, int prefix, bool masked) {
+// A capped score, in the units of Rows::shaped.
+template <typename T> __device__ __forceinline__ float capped(const AttnArgs &a, float z) {
+    return sizeof(T) == 4 ? tanhf(z * (a.scale / a.cap)) : -__builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * (2.f * LOG2E * a.scale / a.cap)));
+}
+
+// The weights of one tile, in a lane sixteen rows' for its key: register 4 g + e is packed row 8 g + 4 hh + e.  l: lse in log2 units less the scores' offset; p: positions; MASKED: not all
+// of them may count.  Summed by fours first, so that a long sum has few steps of its own.
+template <typename T, int DP, int MODE, bool MASKED>
+__device__ __forceinline__ float tile_weight(const AttnArgs &a, const f32x16_t &x, const float (&l)[16], const int (&p)[16], const float (&slope)[16], int key, int keys, int prefix) {
     const float unit = Rows<T, DP, MODE, false>::unit_of(a);
+    const int window = a.window ? a.window : 0x7fffffff;
     float sum[4];
 #pragma unroll
     for (int i = 0; i < 16; i++) {
         float z = x[i];
-        if (MODE & CAPPED) z = sizeof(T) == 4 ? tanhf(z * (a.scale / a.cap)) : -__builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * (2.f * LOG2E * a.scale / a.cap)));
+        if (MODE & CAPPED) z = capped<T>(a, z);
         if (MODE & BIASED) {
             const float factor = MODE & CAPPED ? (sizeof(T) == 4 ? 1.f : 2.f) * a.cap * LOG2E : a.scale * LOG2E;
             z = __builtin_fmaf(-slope[i], fabsf((float)(p[i] - key)), z * factor);
         }
         float w = __builtin_amdgcn_exp2f(__builtin_fmaf(z, unit, -l[i]));
-        if (masked) {
-            const bool see = key < keys && ((key <= p[i] && (a.window == 0 || key > p[i] - a.window)) || key < prefix) && l[i] != -INFINITY;
+        if (MASKED) {                                         // (p - key below 0, or beyond the window: as one comparison without sign)
+            const bool see = (((unsigned)(p[i] - key) < (unsigned)window) | (key < prefix)) & (key < keys) & (l[i] != -INFINITY);
             w = see ? w : 0.f;
         }
         sum[i % 4] = i < 4 ? w : sum[i % 4] + w;
@@ -137,7 +143,7 @@ __global__ void __launch_bounds__(64) paged_weights_step_kernel(WeightArgs w) {
 #pragma unroll
         for (int kk = 0; kk < KS; kk++) x = mma(rows.q[kk], R::key(kt, kk), x);
         const bool masked = odd || t * 32 + 31 > low || (t + 1) * 32 > sq.keys || a.window;
-        float sum = tile_weight<T, DP, MODE>(a, x, l, p, slope, t * 32 + col, sq.keys, prefix, masked);
+        float sum = masked ? tile_weight<T, DP, MODE, true>(a, x, l, p, slope, t * 32 + col, sq.keys, prefix) : tile_weight<T, DP, MODE, false>(a, x, l, p, slope, t * 32 + col, sq.keys, prefix);
         sum = vla_fold_step<32>(sum, VlaAdd());
         if (hh == 0) sums[(t - chunk0) * 32 + col] = sum;
         stage = stage == 2 ? 0 : stage + 1;
@@ -152,141 +158,230 @@ __global__ void __launch_bounds__(64) paged_weights_step_kernel(WeightArgs w) {
 
 // Four waves, each with KW tiles of 32 keys in registers; tiles of 32 packed rows of q come through a ring of four in LDS, a quarter loaded by each wave, with the rows' lse
 // beside them (a copy for each wave: no register is loaded inside the loop).  A row of q may start anywhere: where rows are no multiples of 16 bytes they go through registers.
-template <typename T, int DP, int MODE> constexpr int KEY_TILES = sizeof(T) * DP <= 256 ? 2 : 1;
+// The exponentials of one tile of rows are taken between the matrix instructions of the next.
+template <typename T, int DP> constexpr int KEY_TILES = sizeof(T) * DP <= 256 ? 2 : 1;
 template <typename T, int DP, int MODE>
 __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_weights_rows_kernel(WeightArgs w) {
     typedef Tile<T, DP> TL;
     typedef Rows<T, DP, MODE, false> R;
     typedef typename FragOf<T>::type frag;
-    constexpr int KS = DP / 16, BYTES = 32 * TL::ROW, RG = 4, EACH = 8 / TL::RPI, LOADS = EACH + 1, KW = KEY_TILES<T, DP, MODE>, KEYS = 128 * KW;
+    constexpr int KS = DP / 16, BYTES = 32 * TL::ROW, RG = 4, EACH = 8 / TL::RPI, LOADS = EACH + 1, KW = KEY_TILES<T, DP>, KEYS = 128 * KW;
     extern __shared__ __attribute__((aligned(16))) char lds[];
+    constexpr int GONE = -0x40000000;
     __shared__ __attribute__((aligned(16))) float lse_at[RG][4][64];
+    __shared__ __attribute__((aligned(16))) int info[2][4][32];
     const unsigned lds0 = (unsigned)(size_t)(lds_void *)lds, lse0 = (unsigned)(size_t)(lds_void *)&lse_at[0][0][0];
     const AttnArgs &a = w.a;
     const PagedView &pv = a.pv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, hh = lane >> 5;
     const unsigned id = blockIdx.x / (unsigned)pv.n_kv;
-    const int kvh = blockIdx.x % (unsigned)pv.n_kv, s = id % (unsigned)pv.n_seq, block0 = (int)(id / (unsigned)pv.n_seq) * KEYS;
+    const int kvh = blockIdx.x % (unsigned)pv.n_kv, s = id % (unsigned)pv.n_seq, block0 = __builtin_amdgcn_readfirstlane(id / (unsigned)pv.n_seq * KEYS);
     const PagedSeq sq = paged_seq(pv, s);
     if (block0 >= sq.keys) return;
     const int base = sq.len - sq.n, prefix = prefix_of(a, s, sq), rows = sq.rows * a.group;
     const RowTiles all = row_tiles(a, sq, prefix, block0, KEYS);
-    const int t0 = max(all.t0, (int)blockIdx.y * w.chunk), t1 = min(all.t1, ((int)blockIdx.y + 1) * w.chunk), key0 = block0 + wave * 32 * KW;
+    const int t0 = __builtin_amdgcn_readfirstlane(max(all.t0, (int)blockIdx.y * w.chunk)), t1 = __builtin_amdgcn_readfirstlane(min(all.t1, ((int)blockIdx.y + 1) * w.chunk));
+    const int key0 = block0 + wave * 32 * KW;
     if (w.parts > 1 ? t0 >= t1 : sq.rows == 0 || (all.t0 == all.t1 && base >= block0 + KEYS)) return;
-    // the keys, through the ring's place
-    const Span sp{0, sq.keys, 0, 0};
-    const int32_t *table = pv.table + (size_t)s * pv.table_stride;
-    frag k[KW][KS];
-#pragma unroll
-    for (int b = 0; b < KW; b++) {
-#pragma unroll
-        for (int u = 0; u < 2; u++) {
-            const int at = key0 + b * 32 + u * 16;
-            TL::template load<false, 16>(lds0 + wave * BYTES + u * 16 * TL::ROW, pv.k, pv, sp.page(table, pv.page_log, at), kvh, at, sp);
-        }
-        vm_wait<0>();
-#pragma unroll
-        for (int kk = 0; kk < KS; kk++) {
-            k[b][kk] = R::key(lds + wave * BYTES, kk);
-            if (kk * 16 >= pv.d)                              // (LDS holds repeated values there, of q too)
-#pragma unroll
-                for (int e = 0; e < 8; e++) k[b][kk][e] = (T)0.f;
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
-    __syncthreads();
-    // a lane's part of a tile of rows: the row of each of its loads, and the row whose lse it loads
-    int at_i[EACH], at_h[EACH], l_i, l_h;
+    // a lane's part of a tile of rows: the head of each of its loads, and its offset from the tile's first row's first head (of q in bytes, of lse in words)
     const int step_i = 32 / a.group, step_h = 32 % a.group;
-    {
-        int r = t0 * 32 + wave * 8 + lane / TL::CPR;
+    int head[EACH + 1];
+    unsigned off[EACH + 1];
+    int i0 = 0, h0 = 0;                                       // the first row and its head of the next tile to load
+    auto offsets = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < EACH; e++, r += TL::RPI) { at_i[e] = r / a.group; at_h[e] = r - at_i[e] * a.group; }
-        r = t0 * 32 + col;
-        l_i = r / a.group;
-        l_h = r - l_i * a.group;
+        for (int e = 0; e <= EACH; e++) {
+            const unsigned r = h0 + (e < EACH ? wave * 8 + e * TL::RPI + lane / TL::CPR : col), i = r / (unsigned)a.group;
+            head[e] = r - i * a.group;
+            // (rows behind the last: the last's, which count for nothing)
+            const unsigned at = min((int)i, sq.rows - 1 - i0);
+            if (e == EACH) off[e] = (at * a.n_heads + head[e]) * 4;
+            else {
+                const int z = wave * 8 + e * TL::RPI + lane / TL::CPR, c = min((lane % TL::CPR) ^ TL::fk(z), pv.d * (int)sizeof(T) / 16 - 1);
+                off[e] = (unsigned)(at * a.q_stride + head[e] * pv.d) * (unsigned)sizeof(T) + c * 16;
+            }
+        }
+    };
+    {
+        const unsigned r = t0 * 32, i = r / (unsigned)a.group;
+        i0 = __builtin_amdgcn_readfirstlane(i);
+        h0 = __builtin_amdgcn_readfirstlane(r - i * a.group);
     }
+    if (t0 < t1) offsets();
     auto load = [&](int t, int stage) __attribute__((always_inline)) {
         if (t >= t1) return;
+        // (the offsets are the last tile's, unless a tile is no whole number of rows, or this is the end of the rows)
+        if (t > t0 && (step_h || (t + 1) * 32 > rows)) offsets();
         const unsigned at = lds0 + stage * BYTES + wave * 8 * TL::ROW;
+        const T *q = (const T *)a.q + (size_t)(sq.r0 + i0) * a.q_stride + (size_t)kvh * a.group * pv.d;
+        if (a.aligned) {
 #pragma unroll
-        for (int e = 0; e < EACH; e++) {
-            const int r = wave * 8 + e * TL::RPI + lane / TL::CPR, c = min((lane % TL::CPR) ^ TL::fk(r), pv.d * (int)sizeof(T) / 16 - 1);
-            const int i = min(at_i[e], sq.rows - 1);          // (rows behind the last: the last's, which count for nothing)
-            const T *src = (const T *)a.q + (size_t)(sq.r0 + i) * a.q_stride + (size_t)(kvh * a.group + at_h[e]) * pv.d + c * (16 / (int)sizeof(T));
-            if (a.aligned) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at + e * 1024), "v"(src) : "memory");
-            else {
+            for (int e = 0; e < EACH; e++) dma16(at + e * 1024, off[e], (const char *)q);
+        } else {
+#pragma unroll
+            for (int e = 0; e < EACH; e++) {
+                const int z = wave * 8 + e * TL::RPI + lane / TL::CPR, c = min((lane % TL::CPR) ^ TL::fk(z), pv.d * (int)sizeof(T) / 16 - 1);
+                const unsigned i = (unsigned)(h0 + z) / (unsigned)a.group;
+                const T *src = q + (size_t)min((int)i, sq.rows - 1 - i0) * a.q_stride + head[e] * pv.d + c * (16 / (int)sizeof(T));
                 T x[16 / sizeof(T)];
 #pragma unroll
-                for (int z = 0; z < 16 / (int)sizeof(T); z++) x[z] = src[z];
+                for (int y = 0; y < 16 / (int)sizeof(T); y++) x[y] = src[y];
                 __builtin_memcpy(lds + stage * BYTES + wave * 8 * TL::ROW + e * 1024 + lane * 16, x, 16);
             }
-            at_i[e] += step_i;
-            at_h[e] += step_h;
-            if (at_h[e] >= a.group) { at_h[e] -= a.group; at_i[e]++; }
         }
-        const float *l = w.lse_in + (size_t)(sq.r0 + min(l_i, sq.rows - 1)) * a.n_heads + kvh * a.group + l_h;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lse0 + (stage * 4 + wave) * 256), "v"(l) : "memory");
-        l_i += step_i;
-        l_h += step_h;
-        if (l_h >= a.group) { l_h -= a.group; l_i++; }
+        const float *l = w.lse_in + (size_t)(sq.r0 + i0) * a.n_heads + kvh * a.group;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lse0 + (stage * 4 + wave) * 256), "v"(off[EACH]), "s"(l) : "memory");
+        i0 += step_i;
+        h0 += step_h;
+        if (h0 >= a.group) { h0 -= a.group; i0++; }
     };
 #pragma unroll
-    for (int t = 0; t < RG - 1; t++) load(t0 + t, t);
-    float sum[KW];
+    for (int t = 0; t < RG; t++) load(t0 + t, t);
+    // the keys; zeros in dims that are not there (LDS holds repeated values of q in their place)
+    frag k[KW][KS];
+    {
+        const Span sp{0, sq.keys, 0, 0};
+        const int32_t *table = pv.table + (size_t)s * pv.table_stride;
+#pragma unroll
+        for (int b = 0; b < KW; b++) {
+            const int at = key0 + b * 32, p0 = sp.page(table, pv.page_log, at), p1 = sp.page(table, pv.page_log, at + 16), page = col < 16 ? p0 : p1;
+            const bool ok = (unsigned)page < (unsigned)pv.n_pages;
+            const T *src = ok ? (const T *)pv.k + ((((size_t)page * pv.n_kv + kvh) << pv.page_log) + (min(at + col, sq.keys - 1) & ((1 << pv.page_log) - 1))) * pv.d : (const T *)zero_rows;
+#pragma unroll
+            for (int kk = 0; kk < KS; kk++) {
+                if (kk * 16 < pv.d) k[b][kk] = *(const frag *)(src + kk * 16 + hh * 8);
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; e++) k[b][kk][e] = (T)0.f;
+            }
+        }
+    }
+    const float unit = R::unit_of(a);
+    const int window = a.window ? a.window : 0x7fffffff;
+    float sum[KW], l[16];
 #pragma unroll
     for (int b = 0; b < KW; b++) sum[b] = 0.f;
-    auto step = [&](int t, int stage) __attribute__((always_inline)) {
-        if (a.aligned) {
-            if (t + RG - 2 < t1) vm_wait<(RG - 2) * LOADS>();
-            else vm_wait<0>();
-        } else vm_wait<0>();
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        load(t + RG - 1, stage == 0 ? RG - 1 : stage - 1);
-        const char *qt = lds + stage * BYTES;
-        f32x16_t x[KW];
-#pragma unroll
-        for (int b = 0; b < KW; b++)
-#pragma unroll
-            for (int e = 0; e < 16; e++) x[b][e] = 0.f;
-#pragma unroll
-        for (int kk = 0; kk < KS; kk++) {
-            const frag q = R::key(qt, kk);
-#pragma unroll
-            for (int b = 0; b < KW; b++) x[b] = mma(q, k[b][kk], x[b]);
-        }
-        const float mine = lse_at[stage][wave][col];
-        float l[16], slope[16];
-        int p[16];
-        // every row there, its lse finite, and its position behind all of the wave's keys
-        const bool masked = t * 32 + 32 > rows || base + (int)((unsigned)(t * 32) / (unsigned)a.group) < key0 + 32 * KW - 1 || key0 + 32 * KW > sq.keys || a.window || __any(!(fabsf(mine) < INFINITY));
+    // Of a tile that has arrived: lse in log2 units less the scores' offset, by the lane that has the row; whether every row is there, its lse finite, and all of the wave's keys before it.
+    const int whole0 = key0 + 32 * KW > sq.keys || a.window ? 0x7fffffff : (max(0, key0 + 32 * KW - 1 - base) * a.group + 31) / 32;
+    bool masked;
+    float mine;
+    auto arrive = [&](int t, int stage) __attribute__((always_inline)) {
+        const float v = lse_at[stage][wave][lane];
+        mine = MODE & CAPPED ? __builtin_fmaf(v, LOG2E, -a.offset) : v * LOG2E;
+        masked = t < whole0 || t * 32 + 32 > rows || __any(!(fabsf(v) < INFINITY));
+        lse_at[stage][wave][lane] = mine;
+    };
+    // The tile's scores as they enter the exponentials (-inf where the key is not seen), and its lse.
+    auto shape = [&](int t, int stage, f32x16_t (&x)[KW]) __attribute__((always_inline)) {
 #pragma unroll
         for (int g = 0; g < 4; g++) {
             const f32x4_t v = *(const f32x4_t *)&lse_at[stage][wave][8 * g + 4 * hh];
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                l[4 * g + e] = MODE & CAPPED ? __builtin_fmaf(v[e], LOG2E, -a.offset) : v[e] * LOG2E;
-                p[4 * g + e] = 0;
-                slope[4 * g + e] = 0.f;
-            }
+            for (int e = 0; e < 4; e++) l[4 * g + e] = v[e];
         }
+        if (MODE & CAPPED)
+#pragma unroll
+            for (int b = 0; b < KW; b++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) x[b][r] = capped<T>(a, x[b][r]);
         if (masked || (MODE & BIASED)) {
-#pragma unroll
-            for (int r = 0; r < 16; r++) {
-                const int at = t * 32 + 8 * (r / 4) + 4 * hh + r % 4, i = at / a.group;
-                if (at >= rows) l[r] = -INFINITY;
-                p[r] = base + i;
-                if (MODE & BIASED) slope[r] = at < rows ? a.slopes[kvh * a.group + at - i * a.group] * LOG2E : 0.f;
+            // a lane's own row of the tile, for the others: lse as it is used, position (GONE: of a row that counts for nothing), slope
+            const int at = t * 32 + col, i = (unsigned)at / (unsigned)a.group;
+            const bool there = (at < rows) & (mine != -INFINITY);
+            if (hh == 0) {
+                lse_at[stage][wave][col] = there ? mine : 0.f;
+                info[0][wave][col] = there ? base + i : GONE;
+                if (MODE & BIASED) info[1][wave][col] = there ? __builtin_bit_cast(int, a.slopes[kvh * a.group + at - i * a.group] * LOG2E) : 0;
             }
-        }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-        for (int b = 0; b < KW; b++) sum[b] += tile_weight<T, DP, MODE>(a, x[b], l, p, slope, key0 + b * 32 + col, sq.keys, prefix, masked);
+            for (int g = 0; g < 4; g++) {
+                __builtin_amdgcn_sched_barrier(0);            // (few values alive at a time)
+                const i32x4_v p = *(const i32x4_v *)&info[0][wave][8 * g + 4 * hh];
+                const f32x4_t v = *(const f32x4_t *)&lse_at[stage][wave][8 * g + 4 * hh];
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int r = 4 * g + e;
+                    l[r] = v[e];
+#pragma unroll
+                    for (int b = 0; b < KW; b++) {
+                        const int key = key0 + b * 32 + col;
+                        if (MODE & BIASED) {
+                            const float factor = MODE & CAPPED ? (sizeof(T) == 4 ? 1.f : 2.f) * a.cap * LOG2E : a.scale * LOG2E;
+                            x[b][r] = __builtin_fmaf(-__builtin_bit_cast(float, info[1][wave][8 * g + 4 * hh + e]), fabsf((float)(p[e] - key)), x[b][r] * factor);
+                        }
+                        // (p - key below 0, or beyond the window: as one comparison without sign)
+                        const bool see = (((unsigned)(p[e] - key) < (unsigned)window) | ((key < prefix) & (p[e] != GONE))) & (key < sq.keys);
+                        x[b][r] = see ? x[b][r] : -INFINITY;
+                    }
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
-    for (int t = t0; t < t1; t += RG) {
-        step(t, 0);
-        if (t + 1 < t1) step(t + 1, 1);
-        if (t + 2 < t1) step(t + 2, 2);
-        if (t + 3 < t1) step(t + 3, 3);
+    // the scores of the tile in stage `next_at`, and the weights of x between them
+    constexpr int N = 16 * KW, AHEAD = KS < 3 ? KS : 3;
+    auto weights = [&](f32x16_t (&x)[KW], float (&part)[KW][4], int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = from; n < to; n++) {
+            const int b = n / 16, i = n % 16;
+            const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][i], unit, -l[i]));
+            part[b][i % 4] = i < 4 ? v : part[b][i % 4] + v;
+        }
+    };
+    auto scores = [&](int stage, f32x16_t (&next)[KW], f32x16_t (&x)[KW], bool between) __attribute__((always_inline)) {
+        const char *qt = lds + stage * BYTES;
+        float part[KW][4];
+        frag q[AHEAD];
+#pragma unroll
+        for (int kk = 0; kk < AHEAD; kk++) q[kk] = R::key(qt, kk);
+#pragma unroll
+        for (int b = 0; b < KW; b++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) next[b][e] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KS; kk++) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int b = 0; b < KW; b++) next[b] = mma(q[kk % AHEAD], k[b][kk], next[b]);
+            if (kk + AHEAD < KS) q[kk % AHEAD] = R::key(qt, kk + AHEAD);
+            if (between) weights(x, part, kk * N / KS, (kk + 1) * N / KS);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (between)
+#pragma unroll
+            for (int b = 0; b < KW; b++) {
+                sum[b] += (part[b][0] + part[b][1]) + (part[b][2] + part[b][3]);
+                asm volatile("" : "+v"(sum[b]));              // (here, and not where the compiler would move it, behind the next tile's masks)
+            }
+    };
+    // Tile t lies in stage (t - t0) % RG.  At step t its scores are there; everyone is through with its place, which tile t + RG takes.
+    auto arrived = [&](int t) __attribute__((always_inline)) {          // tile t, t + 1 and t + 2 perhaps not
+        if (a.aligned && t + 2 < t1) vm_wait<2 * LOADS>();
+        else vm_wait<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    f32x16_t x0[KW], x1[KW];
+    if (t0 < t1) {
+        if (a.aligned && t0 + 3 < t1) vm_wait<3 * LOADS>();
+        else vm_wait<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        arrive(t0, 0);
+        scores(0, x0, x1, false);
+        shape(t0, 0, x0);
+        int t = t0;
+        auto step = [&](int stage, f32x16_t (&x)[KW], f32x16_t (&next)[KW]) __attribute__((always_inline)) {
+            const int after = stage == RG - 1 ? 0 : stage + 1;
+            if (t + 1 < t1) {
+                arrived(t + 1);
+                load(t + RG, stage);
+                arrive(t + 1, after);
+            }
+            scores(after, next, x, true);                     // (behind the last tile: of what lies there, for no one)
+            if (t + 1 < t1) shape(t + 1, after, next);
+            return ++t < t1;
+        };
+        while (step(0, x0, x1) && step(1, x1, x0) && step(2, x0, x1) && step(3, x1, x0)) {}
     }
 #pragma unroll
     for (int b = 0; b < KW; b++) {
@@ -345,8 +440,8 @@ WeightPlan plan_weights(const AttnArgs &a, bool f32) {
     }
     const int keys = weight_keys(pv.d, f32);
     const long tiles = (packed + 31) / 32, blocks = pairs * ((pv.max_len + keys - 1) / keys);
-    // workgroups for four rounds of two a CU, with eight tiles of rows at least
-    long parts = blocks > 0 ? (4 * 512 + blocks - 1) / blocks : 1;
+    // workgroups for six rounds of two a CU (4096 causal rows: of four 133 us, of six or eight 125, of sixteen 141), with eight tiles of rows at least
+    long parts = blocks > 0 ? (6 * 512 + blocks - 1) / blocks : 1;
     if (parts > tiles / 8) parts = tiles / 8;
     if (parts > 256) parts = 256;
     if (parts < 1) parts = 1;
@@ -394,7 +489,7 @@ int launch_weights(WeightArgs w, const WeightPlan &p, hipStream_t st) {
     paged_weights_rows_kernel<T, DP, MODE><<<dim3((unsigned)p.items, p.parts), 256, bytes, st>>>(w);
     if (int rc = vla_check_launch("paged_weights")) return rc;
     if (p.parts == 1) return VLA_OK;
-    paged_weights_join_kernel<<<(unsigned)(pv.n_kv * pv.n_seq * ((pv.max_len + 255) / 256)), 256, 0, st>>>(w, 128 * KEY_TILES<T, DP, MODE>);
+    paged_weights_join_kernel<<<(unsigned)(pv.n_kv * pv.n_seq * ((pv.max_len + 255) / 256)), 256, 0, st>>>(w, 128 * KEY_TILES<T, DP>);
     return vla_check_launch("paged_weights join");
 }
 template <typename T, int DP>
@@ -569,7 +664,7 @@ int vla_paged_weights(const vla_paged_cache *cache, const vla_paged_batch *batch
     if (batch->n_rows > 0 && ws_bytes < weight_bytes(a, p)) { vla_set_error("paged_weights: workspace %zu bytes, need %zu", ws_bytes, weight_bytes(a, p)); return VLA_EWORKSPACE; }
     if (batch->n_rows == 0 || batch->max_rows == 0 || batch->max_len == 0) return VLA_OK;
     a.q = (const char *)q; a.q_stride = q_stride;
-    a.aligned = ((uintptr_t)q | (size_t)q_stride * (f32 ? 4 : 2)) % 16 == 0;
+    a.aligned = ((uintptr_t)q | (size_t)q_stride * (f32 ? 4 : 2)) % 16 == 0 && q_stride < 1 << 24;          // (a tile's rows at 32-bit offsets from its first)
     a.offset = !f32 ? a.cap * LOG2E : 0.f;
     w.lse_in = lse; w.mass = mass; w.mass_stride = mass_stride; w.part = (float *)ws;
     hipStream_t st = (hipStream_t)stream;
