@@ -1,6 +1,7 @@
 // Eviction from a paged KV cache by accumulated attention weight: the weights of a call's rows summed per position, and a cache cut to the
 // heaviest positions.
 #include "paged_rows.h"
+#include "paged_select.h"
 
 namespace {
 
@@ -529,26 +530,11 @@ __device__ __forceinline__ unsigned order_of(float x) {
     return u >> 31 ? ~u : u | 1u << 31;
 }
 
+// A workgroup for each (sequence, key head): the least mass that stays, then the positions of what is above it and of the first that equal it, then their masses, a thousand
+// at a time, read before they are written: no mass lands behind its place, so mass_out may be mass.
 constexpr int EVICT_THREADS = 1024;
-__device__ __forceinline__ int evict_scan(int v, int *all, int *red) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int in = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const int x = __shfl_up(in, o, 64); if (lane >= o) in += x; }
-    __syncthreads();
-    if (lane == 63) red[wave] = in;
-    __syncthreads();
-    int before = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < EVICT_THREADS / 64; w++) { if (w < wave) before += red[w]; total += red[w]; }
-    *all = total;
-    return before + in - v;
-}
-
-// A workgroup for each (sequence, key head): the least mass that stays, digit by digit (eight bits a pass over the masses), then what is above it
-// and the first of what equals it, in order.  A chunk's masses are read before any of it is written, and land no further back: mass_out may be mass.
 __global__ void __launch_bounds__(EVICT_THREADS) paged_evict_select_kernel(EvictArgs a) {
-    __shared__ int bins[256], red[EVICT_THREADS / 64], digit, rest;
+    __shared__ CutLds cut;
     const PagedView &pv = a.pv;
     const int h = blockIdx.x % pv.n_kv, s = blockIdx.x / pv.n_kv, t = threadIdx.x;
     const PagedSeq sq = paged_seq(pv, s);
@@ -564,40 +550,26 @@ __global__ void __launch_bounds__(EVICT_THREADS) paged_evict_select_kernel(Evict
             for (int i = t; i < n; i += EVICT_THREADS) out[i] = mass[i];
         return;
     }
-    const int lo = a.first, hi = n - a.recent;
-    int want = a.keep - a.first - a.recent;
-    unsigned prefix = 0, mask = 0;
-    for (int shift = 24; shift >= 0 && want > 0; shift -= 8) {
-        if (t < 256) bins[t] = 0;
+    const int lo = a.first, hi = n - a.recent, want = a.keep - a.first - a.recent;
+    Cut<unsigned> c{~0u, ~0u, 0};                             // (no mass is that: none is taken)
+    if (want > 0)
+        c = cut_keys<EVICT_THREADS, unsigned>([&](auto f) {
+#pragma unroll 8
+            for (int i = lo + t; i < hi; i += EVICT_THREADS) f(order_of(mass[i]));
+        }, want, 32, 0u, cut);
+    auto takes = [&](int i, bool *tie) {
+        const bool open = i >= lo && i < hi;
+        const unsigned key = open ? order_of(mass[i]) & c.mask : 0u;
+        *tie = open && key == c.prefix;
+        return !open || key > c.prefix;
+    };
+    cut_numbers<EVICT_THREADS>(n, c.want, takes, [&](int place, int i) { kept[place] = i; }, cut);
+    for (int i0 = 0; i0 < a.keep; i0 += EVICT_THREADS) {
         __syncthreads();
-        for (int i = lo + t; i < hi; i += EVICT_THREADS) {
-            const unsigned key = order_of(mass[i]);
-            if ((key & mask) == prefix) atomicAdd(&bins[key >> shift & 255], 1);
-        }
-        __syncthreads();
-        int all;
-        const int c = t < 256 ? bins[255 - t] : 0, above = evict_scan(c, &all, red);
-        if (t < 256 && above < want && above + c >= want) { digit = 255 - t; rest = want - above; }
-        __syncthreads();
-        want = rest;
-        prefix |= (unsigned)digit << shift;
-        mask |= 255u << shift;
-        __syncthreads();
-    }
-    if (a.keep == a.first + a.recent) prefix = ~0u;          // (no mass is that: none is taken)
-    int done = 0, equal = 0;
-    for (int i0 = 0; i0 < n; i0 += EVICT_THREADS) {
         const int i = i0 + t;
-        const float m = i < n ? mass[i] : 0.f;
-        const unsigned key = order_of(m);
-        const bool open = i >= lo && i < hi, tie = open && key == prefix;
-        int ties, taken;
-        const int e = evict_scan(tie, &ties, red);
-        const bool take = i < n && (!open || key > prefix || (tie && equal + e < want));
-        const int to = evict_scan(take, &taken, red);
-        if (take) { kept[done + to] = i; out[done + to] = m; }
-        done += taken;
-        equal += ties;
+        const float m = i < a.keep ? mass[kept[i]] : 0.f;
+        __syncthreads();
+        if (i < a.keep) out[i] = m;
     }
 }
 

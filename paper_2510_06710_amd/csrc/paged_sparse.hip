@@ -4,6 +4,7 @@
 // (sum_h max(q_h, 0)) . hi + (sum_h min(q_h, 0)) . lo: two products a dim whatever the group, in fp64, where the sums of bf16 products are exact
 // but for the last bits and the order of additions decides no border.
 #include "paged_rows.h"
+#include "paged_select.h"
 
 namespace {
 
@@ -23,14 +24,17 @@ __global__ void __launch_bounds__(256) paged_bounds_kernel(PagedView pv, T *boun
     for (int x = threadIdx.x; x < pv.n_kv * chunks; x += 256) {
         const int h = x / chunks, c = x - h * chunks;
         const T *k = (const T *)pv.k + (((size_t)page * pv.n_kv + h) << pv.page_log) * pv.d + c * 8;
-        t8 v = *(const t8 *)k;
         float lo[8], hi[8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) lo[e] = hi[e] = (float)v[e];
-        for (int i = 1; i < n; i++) {
-            v = *(const t8 *)(k + (size_t)i * pv.d);
+        for (int e = 0; e < 8; e++) { lo[e] = INFINITY; hi[e] = -INFINITY; }
+        for (int i = 0; i < n; i += 8) {                      // eight rows on their way at once (behind the last: the last again)
+            t8 v[8];
 #pragma unroll
-            for (int e = 0; e < 8; e++) { lo[e] = fminf(lo[e], (float)v[e]); hi[e] = fmaxf(hi[e], (float)v[e]); }
+            for (int u = 0; u < 8; u++) v[u] = *(const t8 *)(k + (size_t)min(i + u, n - 1) * pv.d);
+#pragma unroll
+            for (int u = 0; u < 8; u++)
+#pragma unroll
+                for (int e = 0; e < 8; e++) { lo[e] = fminf(lo[e], (float)v[u][e]); hi[e] = fmaxf(hi[e], (float)v[u][e]); }
         }
         T *to = bounds + ((size_t)page * pv.n_kv + h) * 2 * pv.d + c * 8;
         t8 a, b;
@@ -69,15 +73,19 @@ __device__ __forceinline__ int page_of_row(const PagedView &pv, int row, int *s)
     return p < 0 ? -1 : p >> pv.page_log;
 }
 
-// One wave a page, its lanes each some dims of lo or hi; four pages of a (row, key head) a workgroup at a time.
+// A page's bounds are 2 d values of lo and hi, 16 bytes a lane: `lanes` lanes (a power of two, at most 64) hold a page, so a wave's load has 64 / lanes of them, and four loads are on their way at once
+// (an fp32 page of more than 128 dims takes two loads a lane).  The parts of q that a lane multiplies by are the same for all pages.
+// 8 x 2048 pages of 512 bytes: 5 us; 32 ragged rows of up to 1024 pages of 8 heads: 20.  (One wave a page and load, q again for every four pages: 12 and 81.)
 template <typename T>
-__global__ void __launch_bounds__(256) paged_score_kernel(SelectArgs a) {
-    __shared__ double part[2][256];                          // the group's positive and negative parts of q
+__global__ void __launch_bounds__(256) paged_score_kernel(SelectArgs a, int lanes_log, int per_block) {
+    constexpr int E = 16 / sizeof(T), U = 4, R = sizeof(T) == 4 ? 2 : 1;          // values of a load; pages of a lane at once; loads of a page
+    typedef T vec __attribute__((ext_vector_type(E)));
+    __shared__ double part[2 * 256];                         // what lo and hi are multiplied by: the group's negative and positive parts of q
     const PagedView &pv = a.pv;
-    const int h = blockIdx.x % pv.n_kv, row = blockIdx.x / pv.n_kv, t = threadIdx.x, lane = t & 63;
+    const int h = blockIdx.x % (unsigned)pv.n_kv, row = blockIdx.x / (unsigned)pv.n_kv, t = threadIdx.x, lanes = 1 << lanes_log;
     int s;
-    const int last = page_of_row(pv, row, &s);
-    if (last < 0) return;
+    const int last = page_of_row(pv, row, &s), n0 = blockIdx.y * per_block, n1 = min(n0 + per_block, last + 1);
+    if (n0 >= n1) return;
     for (int e = t; e < pv.d; e += 256) {
         const T *q = (const T *)a.q + row * a.q_stride + (size_t)h * a.group * pv.d + e;
         double up = 0.0, down = 0.0;
@@ -86,47 +94,61 @@ __global__ void __launch_bounds__(256) paged_score_kernel(SelectArgs a) {
             up += x > 0.0 ? x : 0.0;
             down += x > 0.0 ? 0.0 : x;
         }
-        part[0][e] = down;
-        part[1][e] = up;
+        part[e] = down;
+        part[pv.d + e] = up;
     }
     __syncthreads();
+    const int lane = t & (lanes - 1), chunks = 2 * pv.d / E;
+    double w[R][E];
+#pragma unroll
+    for (int r = 0; r < R; r++)
+#pragma unroll
+        for (int e = 0; e < E; e++) w[r][e] = lane + r * lanes < chunks ? part[(lane + r * lanes) * E + e] : 0.0;
     const int32_t *table = pv.table + (size_t)s * pv.table_stride;
-    for (int n = blockIdx.y * 4 + (t >> 6); n <= last; n += gridDim.y * 4) {
-        const int page = table[n];
-        double x = 0.0;
-        if ((unsigned)page < (unsigned)pv.n_pages) {
-            const T *b = (const T *)a.bounds + ((size_t)page * pv.n_kv + h) * 2 * pv.d;
-            for (int e = lane; e < 2 * pv.d; e += 64) x += (double)(float)b[e] * (e < pv.d ? part[0][e] : part[1][e - pv.d]);
+    unsigned long long *keys = a.keys + ((size_t)row * pv.n_kv + h) * a.pages;
+    const int step = 256 >> lanes_log;                       // pages of one load of the workgroup
+    for (int p0 = n0 + (t >> lanes_log); __any(p0 < n1); p0 += U * step) {
+        int page[U];
+        vec b[U][R];
+#pragma unroll
+        for (int u = 0; u < U; u++) page[u] = p0 + u * step < n1 ? table[p0 + u * step] : -1;
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int r = 0; r < R; r++)
+                if ((unsigned)page[u] < (unsigned)pv.n_pages && lane + r * lanes < chunks)
+                    b[u][r] = *(const vec *)((const T *)a.bounds + ((size_t)page[u] * pv.n_kv + h) * 2 * pv.d + (lane + r * lanes) * E);
+                else
+#pragma unroll
+                    for (int e = 0; e < E; e++) b[u][r][e] = (T)0.f;          // (a page that is not there: zeros)
+        double x[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            x[u] = 0.0;
+#pragma unroll
+            for (int r = 0; r < R; r++)
+                if (r == 0 || lanes + lane < chunks)          // (a zero times an infinite bound of no dim)
+#pragma unroll
+                    for (int e = 0; e < E; e++) x[u] = __builtin_fma((double)(float)b[u][r][e], w[r][e], x[u]);
         }
-        for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-        if (lane == 0) a.keys[((size_t)row * pv.n_kv + h) * a.pages + n] = order_of(x);
+        for (int o = lanes >> 1; o > 0; o >>= 1)
+#pragma unroll
+            for (int u = 0; u < U; u++) x[u] += __shfl_xor(x[u], o, 64);
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (lane == 0 && p0 + u * step < n1) keys[p0 + u * step] = order_of(x[u]);
     }
 }
 
-// Exclusive sum over a workgroup's threads; *all: the total.  red: one int a wave.
-template <int THREADS> __device__ __forceinline__ int block_scan(int v, int *all, int *red) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int in = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const int x = __shfl_up(in, o, 64); if (lane >= o) in += x; }
-    __syncthreads();
-    if (lane == 63) red[wave] = in;
-    __syncthreads();
-    int before = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; w++) { if (w < wave) before += red[w]; total += red[w]; }
-    *all = total;
-    return before + in - v;
-}
-
-// A workgroup for each (row, key head): the keys to LDS, the smallest that is taken digit by digit (eight bits a time, counted in LDS), then the
-// numbers of what is above it and of the first that equal it, in order.
+// A workgroup for each (row, key head): the keys to LDS, then the cut among those that are free to choose, [first, n - recent).  The bits that all of them share are found first: scores of one
+// sign and about one size have a dozen, which no digit need be spent on.
 __global__ void __launch_bounds__(256) paged_select_kernel(SelectArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ int bins[256], red[4], digit, rest;
+    __shared__ CutLds cut;
+    __shared__ unsigned long long differ[4];
     unsigned long long *key = (unsigned long long *)lds;
     const PagedView &pv = a.pv;
-    const int h = blockIdx.x % pv.n_kv, row = blockIdx.x / pv.n_kv, t = threadIdx.x;
+    const int h = blockIdx.x % (unsigned)pv.n_kv, row = blockIdx.x / (unsigned)pv.n_kv, t = threadIdx.x;
     int s;
     const int last = page_of_row(pv, row, &s), n = last + 1;
     if (last < -1) return;
@@ -135,41 +157,33 @@ __global__ void __launch_bounds__(256) paged_select_kernel(SelectArgs a) {
         for (int i = t; i < a.n_select; i += 256) out[i] = i < n ? i : -1;
         return;
     }
-    // free to choose: [first, n - recent); of these `want` (more than there are pages by one at least are left out)
-    const int lo = min(a.first, n), hi = n - a.recent;
+    const int lo = a.first, hi = n - a.recent, want = a.n_select - a.first - a.recent;
     const unsigned long long *src = a.keys + ((size_t)row * pv.n_kv + h) * a.pages;
-    for (int i = lo + t; i < hi; i += 256) key[i] = src[i];
-    int want = a.n_select - a.first - a.recent;
-    unsigned long long prefix = 0, mask = 0;
-    for (int shift = 56; shift >= 0 && want > 0; shift -= 8) {
-        bins[t] = 0;
+    Cut<unsigned long long> c{~0ull, ~0ull, 0};              // (no key is that: none is taken)
+    if (want > 0) {
+        const unsigned long long one = src[lo];
+        unsigned long long x = 0;
+#pragma unroll 8
+        for (int i = lo + t; i < hi; i += 256) {
+            const unsigned long long k = src[i];
+            key[i] = k;
+            x |= k ^ one;
+        }
+        for (int o = 32; o > 0; o >>= 1) x |= __shfl_xor(x, o, 64);
+        if ((t & 63) == 0) differ[t >> 6] = x;
         __syncthreads();
-        for (int i = lo + t; i < hi; i += 256)
-            if ((key[i] & mask) == prefix) atomicAdd(&bins[key[i] >> shift & 255], 1);
-        __syncthreads();
-        // the digit at which the count from above reaches `want`: thread t has digit 255 - t
-        int all;
-        const int c = bins[255 - t], above = block_scan<256>(c, &all, red);
-        if (above < want && above + c >= want) { digit = 255 - t; rest = want - above; }
-        __syncthreads();
-        want = rest;
-        prefix |= (unsigned long long)digit << shift;
-        mask |= 255ull << shift;
-        __syncthreads();
+        x = differ[0] | differ[1] | differ[2] | differ[3];
+        c = cut_keys<256, unsigned long long>([&](auto f) {
+            for (int i = lo + t; i < hi; i += 256) f(key[i]);
+        }, want, x ? 64 - __builtin_clzll(x) : 0, one, cut);
     }
-    if (a.n_select == a.first + a.recent) prefix = ~0ull;    // (no key is that: none is taken)
-    int done = 0, equal = 0;
-    for (int i0 = 0; i0 < n; i0 += 256) {
-        const int i = i0 + t;
-        const bool open = i >= lo && i < hi, tie = open && key[i] == prefix;
-        int ties, taken;
-        const int e = block_scan<256>(tie, &ties, red);
-        const bool take = i < n && (!open || key[i] > prefix || (tie && equal + e < want));
-        const int at = block_scan<256>(take, &taken, red);
-        if (take) out[done + at] = i;
-        done += taken;
-        equal += ties;
-    }
+    auto takes = [&](int i, bool *tie) {
+        const bool open = i >= lo && i < hi;
+        const unsigned long long k = open ? key[i] & c.mask : 0ull;
+        *tie = open && k == c.prefix && c.want > 0;
+        return !open || k > c.prefix;
+    };
+    cut_numbers<256>(n, c.want, takes, [&](int place, int i) { out[place] = i; }, cut);
 }
 
 // ---- attention over the selected pages ----------------------------------------------------------------------------------------
@@ -413,10 +427,18 @@ int vla_paged_select(const vla_paged_cache *cache, const vla_paged_batch *batch,
     ProfScope ps("paged_select", 0.0, st);
     const int items = pv.n_rows * pv.n_kv;
     if (a.pages > n_select) {
-        int y = (4096 + items - 1) / items;
-        if (y > (a.pages + 3) / 4) y = (a.pages + 3) / 4;
-        if (cache->dtype == VLA_DTYPE_F32) paged_score_kernel<float><<<dim3(items, y), 256, 0, st>>>(a);
-        else paged_score_kernel<bf16_t><<<dim3(items, y), 256, 0, st>>>(a);
+        // workgroups for two rounds of four a CU, each with one step of the loop at least
+        const bool f32 = cache->dtype == VLA_DTYPE_F32;
+        const int chunks = 2 * pv.d * (f32 ? 4 : 2) / 16;
+        int lanes_log = 0;
+        while (lanes_log < 6 && (1 << lanes_log) < chunks) lanes_log++;
+        const int step = 4 * (256 >> lanes_log);
+        int y = (2048 + items - 1) / items;
+        if (y > (a.pages + step - 1) / step) y = (a.pages + step - 1) / step;
+        const int per_block = ((a.pages + y - 1) / y + step - 1) / step * step;
+        y = (a.pages + per_block - 1) / per_block;
+        if (f32) paged_score_kernel<float><<<dim3(items, y), 256, 0, st>>>(a, lanes_log, per_block);
+        else paged_score_kernel<bf16_t><<<dim3(items, y), 256, 0, st>>>(a, lanes_log, per_block);
         if (int rc = vla_check_launch("paged_select scores")) return rc;
     }
     const size_t lds = (size_t)a.pages * 8;

@@ -41,6 +41,7 @@ struct AcceptArgs {
 };
 __global__ void __launch_bounds__(256) paged_accept_kernel(AcceptArgs a) {
     __shared__ int32_t up[VLA_TREE_ROWS], id[VLA_TREE_ROWS], want[VLA_TREE_ROWS], path[VLA_TREE_ROWS + 1];
+    __shared__ long from[VLA_TREE_ROWS], to[VLA_TREE_ROWS];
     __shared__ int found;
     const PagedView &pv = a.pv;
     const int s = blockIdx.x, t = threadIdx.x;
@@ -80,14 +81,20 @@ __global__ void __launch_bounds__(256) paged_accept_kernel(AcceptArgs a) {
     int first = 0;                                            // rows before it stay where they are
     while (first < n && path[first] == first) first++;
     if (first == n || base + first < 0) return;
+    // where the rows that move are, and go: bytes within a key head's pages; below 0: nowhere
     const int32_t *table = pv.table + (size_t)s * pv.table_stride;
     const int row_bytes = pv.d * a.es, chunks = row_bytes / 16;
-    auto at = [&](int pos) -> long {                          // of a position's row in a key head's pages; -1: it is nowhere
+    auto at = [&](int pos) -> long {
         if (pos >= pv.max_len) return -1;
         const int page = table[pos >> pv.page_log];
         if ((unsigned)page >= (unsigned)pv.n_pages) return -1;
         return (((long)page * pv.n_kv << pv.page_log) + (pos & ((1 << pv.page_log) - 1))) * row_bytes;
     };
+    for (int i = first + t; i < n; i += 256) {
+        from[i] = at(base + path[i]);
+        to[i] = at(base + i);
+    }
+    __syncthreads();
     const int u0 = blockIdx.y * a.per_block, u1 = min(u0 + a.per_block, a.units);
     for (int x = u0 * chunks + t; x < u1 * chunks; x += 256) {
         const int unit = x / chunks, c = x - unit * chunks, pair = unit >> 1;
@@ -96,14 +103,12 @@ __global__ void __launch_bounds__(256) paged_accept_kernel(AcceptArgs a) {
             i32x4_v v[8];
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                const long from = i0 + j < n ? at(base + path[i0 + j]) : -1;
-                v[j] = from < 0 ? i32x4_v{0, 0, 0, 0} : *(const i32x4_v *)(rows + from);
+                const long src = i0 + j < n ? from[i0 + j] : -1;
+                v[j] = src < 0 ? i32x4_v{0, 0, 0, 0} : *(const i32x4_v *)(rows + src);
             }
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                const long to = i0 + j < n ? at(base + i0 + j) : -1;
-                if (to >= 0) *(i32x4_v *)(rows + to) = v[j];
-            }
+            for (int j = 0; j < 8; j++)
+                if (i0 + j < n && to[i0 + j] >= 0) *(i32x4_v *)(rows + to[i0 + j]) = v[j];
         }
     }
 }
