@@ -356,6 +356,8 @@ def _want(t, kind: str, name: str, shape=None):
     """An array argument the library reads as packed values of one type: another type, shape or layout would be read wrongly."""
     if t is None:
         return None
+    if t.dtype is _codes.get(kind) and (shape is None or t.shape == shape) and t.is_contiguous():          # (a call has a dozen of these: half a microsecond each)
+        return t.data_ptr()
     if t.dtype is not _known()[kind] or not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise VlaError(VLA_EINVAL, f"{name}: contiguous {kind}{'' if shape is None else ' ' + str(list(shape))} wanted, "
                                    f"{t.dtype} {list(t.shape)} given")
@@ -409,11 +411,11 @@ def make_paged_cache(k, v) -> vla_paged_cache:
 
 def make_paged_batch(row_start, kv_len, page_table, n_rows: int, max_rows: int, max_len: int) -> vla_paged_batch:
     """``row_start`` [n_seq + 1], ``kv_len`` [n_seq], ``page_table`` [n_seq, entries]: int32 device tensors."""
-    n_seq = kv_len.shape[0]
-    if page_table.dim() != 2:
-        raise VlaError(VLA_ESHAPE, f"page_table is {list(page_table.shape)}, wanted [n_seq, entries]")
-    b = vla_paged_batch(n_seq, n_rows, max_rows, max_len, page_table.shape[1], _want(row_start, "int32", "row_start", (n_seq + 1,)),
-                        _want(kv_len, "int32", "kv_len", (n_seq,)), _want(page_table, "int32", "page_table", (n_seq, page_table.shape[1])))
+    n_seq, table = kv_len.shape[0], page_table.shape
+    if len(table) != 2:
+        raise VlaError(VLA_ESHAPE, f"page_table is {list(table)}, wanted [n_seq, entries]")
+    b = vla_paged_batch(n_seq, n_rows, max_rows, max_len, table[1], _want(row_start, "int32", "row_start", (n_seq + 1,)),
+                        _want(kv_len, "int32", "kv_len", (n_seq,)), _want(page_table, "int32", "page_table", (n_seq, table[1])))
     b.keep, b.device = (row_start, kv_len, page_table), _device_of(row_start, kv_len, page_table)
     return b
 
@@ -539,6 +541,8 @@ def _ws(ws):
 
 
 def _ints(t, name, *shape):
+    if t is not None and t.dtype is _codes.get("int32") and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
     return _want(t, "int32", name, shape)
 
 

@@ -149,6 +149,8 @@ __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_prom
         else vm_wait<0>();
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         f32x16_t x, next;
+        // (a tree's packed rows may be few: a wave without any loads its share of the tiles, and leaves the matrix pipe to the others)
+        const bool idle = (MODE & TREE) && !__any(y.valid);
         rows.scores(x, lds);
 #pragma unroll
         for (int i = 0; i < 16; i++) x[i] = R::shaped(x[i], a, y, t0 * KT, i);
@@ -180,6 +182,7 @@ __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_prom
                 page_v = page_k;
                 page_k = page_of(t + 1 + RG);
             }
+            if (idle) return ++t < t1;
             rows.move_to(top);
             rows.scores_and_weights(next, lds + after, p, x, unit);
             top = rows.values_and_largest(p, lds + RG * BYTES + now, next, a, y, (t + 1) * KT);

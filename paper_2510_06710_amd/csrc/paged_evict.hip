@@ -17,6 +17,7 @@ struct WeightArgs {
     long mass_stride;
     int chunk;               // tiles of keys (step) or of packed rows (rows) of one workgroup
     int parts;
+    int waves;               // step: among which a key head's tiles are divided (0: by chunks)
 };
 
 // The packed rows of a sequence, as tiles of 32, that may see one of the keys key0 .. key0 + n - 1: positions key0 on, below key0 + n - 1 + window; all where the prefix reaches.
@@ -61,9 +62,17 @@ __device__ __forceinline__ float tile_weight(const AttnArgs &a, const f32x16_t &
     return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
-// One wave a workgroup: up to 32 packed rows of a sequence in registers, `chunk` tiles of 32 keys through a ring of three in LDS (rows of 16 keys of a page, as in
-// paged_attention.hip); the sums go to LDS and to memory at the end, when nothing else is on its way.
-constexpr int STEP_TILES = 16;               // of a chunk at most
+// One wave a workgroup, as many as their rings fit the chip; each takes one key head's equal run of the key tiles of all sequences, whatever their lengths.  Up to 32 packed rows of a
+// sequence are in registers, its tiles of 32 keys come through a ring of three in LDS (rows of 16 keys of a page, as in paged_attention.hip); their sums go to LDS and to memory eight tiles at a time.
+// Of more than 2048 sequences a wave takes `chunk` tiles of one (every wave looks at all sequences' lengths to find its run).
+constexpr int STEP_TILES = 8;
+struct StepTiles { int from, n; };           // of a sequence: those that a row sees or that hold new positions (all behind the first row's window, and before the prefix's end)
+__device__ __forceinline__ StepTiles step_tiles(const AttnArgs &a, int s) {
+    const PagedSeq sq = paged_seq(a.pv, s);
+    if (sq.rows == 0) return {0, 0};
+    const int from = a.window && prefix_of(a, s, sq) == 0 ? max(0, sq.len - sq.n + 1 - a.window) / 32 : 0;
+    return {from, max(0, (sq.keys + 31) / 32 - from)};
+}
 template <typename T, int DP, int MODE>
 __global__ void __launch_bounds__(64) paged_weights_step_kernel(WeightArgs w) {
     typedef Tile<T, DP> TL;
@@ -76,87 +85,124 @@ __global__ void __launch_bounds__(64) paged_weights_step_kernel(WeightArgs w) {
     const PagedView &pv = a.pv;
     const int lane = threadIdx.x, col = lane & 31, hh = lane >> 5;
     const unsigned id = blockIdx.x / (unsigned)pv.n_kv;
-    const int kvh = blockIdx.x % (unsigned)pv.n_kv, s = id % (unsigned)pv.n_seq, chunk0 = __builtin_amdgcn_readfirstlane(id / (unsigned)pv.n_seq * w.chunk);
-    const PagedSeq sq = paged_seq(pv, s);
-    const int base = sq.len - sq.n, prefix = prefix_of(a, s, sq);
-    // tiles that a row sees or that hold new positions: all behind the first row's window, and before the prefix's end
-    const int from = a.window && prefix == 0 ? max(0, base + 1 - a.window) / 32 : 0;
-    const int t0 = max(from, chunk0), t1 = min(chunk0 + w.chunk, (sq.keys + 31) / 32);
-    if (t0 >= t1 || sq.rows == 0) return;
-    const Span sp{0, sq.keys, 0, 0};
-    const int32_t *table = pv.table + (size_t)s * pv.table_stride;
+    const int kvh = blockIdx.x % (unsigned)pv.n_kv;
+    int s = 0, skip = 0, left;                               // the sequence it is in; tiles of it that are not its own; tiles of its run that are left
+    if (w.waves) {
+        int all = 0, c = 0;
+        for (int z = lane; z < pv.n_seq; z += 64) all += c = step_tiles(a, z).n;
+        all = __builtin_amdgcn_readfirstlane(wave_sum(all));
+        const int share = max(2, (int)((unsigned)(all + w.waves - 1) / (unsigned)w.waves));
+        int rest = __builtin_amdgcn_readfirstlane(id * share);
+        left = __builtin_amdgcn_readfirstlane(min(share, all - rest));
+        if (left <= 0) return;
+        for (int s0 = 0; s0 < pv.n_seq; s0 += 64) {
+            if (pv.n_seq > 64) c = s0 + lane < pv.n_seq ? step_tiles(a, s0 + lane).n : 0;
+            int in = c;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(in, o, 64); if (lane >= o) in += v; }
+            const unsigned long long past = __ballot(in > rest);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                s = __builtin_amdgcn_readfirstlane(s0 + l);
+                skip = __builtin_amdgcn_readfirstlane(rest - __shfl(in - c, l, 64));
+                break;
+            }
+            rest -= __builtin_amdgcn_readlane(in, 63);
+        }
+    } else {
+        s = __builtin_amdgcn_readfirstlane(id % (unsigned)pv.n_seq);
+        skip = __builtin_amdgcn_readfirstlane(id / (unsigned)pv.n_seq * w.chunk);
+        left = min(w.chunk, step_tiles(a, s).n - skip);
+        if (left <= 0) return;
+    }
     typename TL::template Offsets<false, 16> off;
     off.start(pv, 0);
     const Place place(pv, kvh, sizeof(T));
-    int p0 = sp.page(table, pv.page_log, t0 * 32), p1 = sp.page(table, pv.page_log, t0 * 32 + 16);
-    auto load = [&](int t, int stage) __attribute__((always_inline)) {
-        const unsigned at = ring0 + stage * BYTES;
-        if ((t + 1) * 32 <= sq.keys) {
-            off.load(at, place.in(pv, pv.k, p0, place.at(pv, p0, t * 32)));
-            off.load(at + 16 * TL::ROW, place.in(pv, pv.k, p1, place.at(pv, p1, t * 32 + 16)));
-        } else {
-            TL::template load<false, 16>(at, pv.k, pv, p0, kvh, t * 32, sp);
-            TL::template load<false, 16>(at + 16 * TL::ROW, pv.k, pv, p1, kvh, t * 32 + 16, sp);
+    for (; left > 0 && s < pv.n_seq; s++, skip = 0) {
+        const StepTiles its = step_tiles(a, s);
+        const int take = min(its.n - skip, left), t0 = its.from + skip, t1 = t0 + take;
+        if (take <= 0) continue;
+        left -= take;
+        const PagedSeq sq = paged_seq(pv, s);
+        const int base = sq.len - sq.n, prefix = prefix_of(a, s, sq);
+        const Span sp{0, sq.keys, 0, 0};
+        const int32_t *table = pv.table + (size_t)s * pv.table_stride;
+        int p0 = sp.page(table, pv.page_log, t0 * 32), p1 = sp.page(table, pv.page_log, t0 * 32 + 16);
+        auto load = [&](int t, int stage) __attribute__((always_inline)) {
+            const unsigned at = ring0 + stage * BYTES;
+            if ((t + 1) * 32 <= sq.keys) {
+                off.load(at, place.in(pv, pv.k, p0, place.at(pv, p0, t * 32)));
+                off.load(at + 16 * TL::ROW, place.in(pv, pv.k, p1, place.at(pv, p1, t * 32 + 16)));
+            } else {
+                TL::template load<false, 16>(at, pv.k, pv, p0, kvh, t * 32, sp);
+                TL::template load<false, 16>(at + 16 * TL::ROW, pv.k, pv, p1, kvh, t * 32 + 16, sp);
+            }
+            p0 = sp.page(table, pv.page_log, t * 32 + 32);
+            p1 = sp.page(table, pv.page_log, t * 32 + 48);
+        };
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // the reads of the last sequence's tiles are through
+        load(t0, 0);
+        if (t0 + 1 < t1) load(t0 + 1, 1);
+        Query y{};
+        const int i = col / a.group, hg = col - i * a.group;
+        y.valid = i < sq.rows;
+        y.row = sq.r0 + (y.valid ? i : 0);
+        y.head = kvh * a.group + hg;
+        if (hh == 0) {
+            const float l = y.valid ? w.lse_in[(size_t)y.row * a.n_heads + y.head] : -INFINITY;
+            info[0][col] = l == -INFINITY ? INFINITY : l * LOG2E - a.offset;          // (such a row's weights are exp2 of -inf)
+            info[1][col] = __builtin_bit_cast(float, y.valid ? base + i : 0x7fffffff);
+            info[2][col] = (MODE & BIASED) && y.valid ? a.slopes[y.head] * LOG2E : 0.f;
         }
-        p0 = sp.page(table, pv.page_log, t * 32 + 32);
-        p1 = sp.page(table, pv.page_log, t * 32 + 48);
-    };
-    load(t0, 0);
-    if (t0 + 1 < t1) load(t0 + 1, 1);
-    Query y{};
-    const int i = col / a.group, hg = col - i * a.group;
-    y.valid = i < sq.rows;
-    y.row = sq.r0 + (y.valid ? i : 0);
-    y.head = kvh * a.group + hg;
-    if (hh == 0) {
-        const float l = y.valid ? w.lse_in[(size_t)y.row * a.n_heads + y.head] : -INFINITY;
-        info[0][col] = l == -INFINITY ? INFINITY : l * LOG2E - a.offset;          // (such a row's weights are exp2 of -inf)
-        info[1][col] = __builtin_bit_cast(float, y.valid ? base + i : 0x7fffffff);
-        info[2][col] = (MODE & BIASED) && y.valid ? a.slopes[y.head] * LOG2E : 0.f;
-    }
-    R rows;
-    rows.start(a, y);
-    float l[16], slope[16];
-    int p[16], low = 0x7fffffff;                              // low: the first row's position
-    bool odd = false;
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        R rows;
+        rows.start(a, y);
+        float l[16], slope[16];
+        int p[16], low = 0x7fffffff;                          // low: the first row's position
+        bool odd = false;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int r = 0; r < 16; r++) {
-        const int at = 8 * (r / 4) + 4 * hh + r % 4;
-        l[r] = info[0][at];
-        p[r] = __builtin_bit_cast(int, info[1][at]);
-        slope[r] = info[2][at];
-        low = min(low, p[r]);
-        odd |= !(l[r] < INFINITY);
-    }
-    low = wave_min(low);
-    odd = __any(odd);
-    int stage = 0;
-    for (int t = t0; t < t1; t++) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // the reads of the stage that is loaded again are through
-        if (t + 2 < t1) { load(t + 2, stage >= 1 ? stage - 1 : 2); vm_wait<2 * LOADS>(); }
-        else if (t + 1 < t1) vm_wait<LOADS>();
-        else vm_wait<0>();
-        const char *kt = lds + stage * BYTES;
-        f32x16_t x;
+        for (int r = 0; r < 16; r++) {
+            const int at = 8 * (r / 4) + 4 * hh + r % 4;
+            l[r] = info[0][at];
+            p[r] = __builtin_bit_cast(int, info[1][at]);
+            slope[r] = info[2][at];
+            low = min(low, p[r]);
+            odd |= !(l[r] < INFINITY);
+        }
+        low = wave_min(low);
+        odd = __any(odd);
+        float *mass = w.mass + ((size_t)s * pv.n_kv + kvh) * w.mass_stride;
+        int stage = 0, first = t0;                            // of the tiles whose sums are in LDS
+        for (int t = t0; t < t1; t++) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // the reads of the stage that is loaded again are through
+            if (t + 2 < t1) { load(t + 2, stage >= 1 ? stage - 1 : 2); vm_wait<2 * LOADS>(); }
+            else if (t + 1 < t1) vm_wait<LOADS>();
+            else vm_wait<0>();
+            const char *kt = lds + stage * BYTES;
+            f32x16_t x;
 #pragma unroll
-        for (int e = 0; e < 16; e++) x[e] = 0.f;
+            for (int e = 0; e < 16; e++) x[e] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < KS; kk++) x = mma(rows.q[kk], R::key(kt, kk), x);
-        const bool masked = odd || t * 32 + 31 > low || (t + 1) * 32 > sq.keys || a.window;
-        float sum = masked ? tile_weight<T, DP, MODE, true>(a, x, l, p, slope, t * 32 + col, sq.keys, prefix) : tile_weight<T, DP, MODE, false>(a, x, l, p, slope, t * 32 + col, sq.keys, prefix);
-        sum = vla_fold_step<32>(sum, VlaAdd());
-        if (hh == 0) sums[(t - chunk0) * 32 + col] = sum;
-        stage = stage == 2 ? 0 : stage + 1;
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    float *mass = w.mass + ((size_t)s * pv.n_kv + kvh) * w.mass_stride;
-    for (int key = t0 * 32 + lane; key < min(t1 * 32, sq.keys); key += 64) {
-        const float sum = sums[key - chunk0 * 32];
-        mass[key] = key < base ? mass[key] + sum : sum;
+            for (int kk = 0; kk < KS; kk++) x = mma(rows.q[kk], R::key(kt, kk), x);
+            const bool masked = odd || t * 32 + 31 > low || (t + 1) * 32 > sq.keys || a.window;
+            float sum = masked ? tile_weight<T, DP, MODE, true>(a, x, l, p, slope, t * 32 + col, sq.keys, prefix) : tile_weight<T, DP, MODE, false>(a, x, l, p, slope, t * 32 + col, sq.keys, prefix);
+            sum = vla_fold_step<32>(sum, VlaAdd());
+            if (hh == 0) sums[(t - first) * 32 + col] = sum;
+            stage = stage == 2 ? 0 : stage + 1;
+            if (t + 1 == t1 || t + 1 - first == STEP_TILES) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                for (int key = first * 32 + lane; key < min((t + 1) * 32, sq.keys); key += 64) {
+                    const float add = sums[key - first * 32];
+                    mass[key] = key < base ? mass[key] + add : add;
+                }
+                first = t + 1;
+            }
+        }
     }
 }
 
+// (Tried: four tiles of keys a wave with the lse subtracted by a matrix instruction, which halves what is read of LDS, 130 us and more: one tile's products wait for each other.  Vector and matrix work
+// share the time of a CU's units here: without the exponentials a call of 140 us took 122, without the products 106, without loads 127.)
 // Four waves, each with KW tiles of 32 keys in registers; tiles of 32 packed rows of q come through a ring of four in LDS, a quarter loaded by each wave, with the rows' lse
 // beside them (a copy for each wave: no register is loaded inside the loop).  A row of q may start anywhere: where rows are no multiples of 16 bytes they go through registers.
 // The exponentials of one tile of rows are taken between the matrix instructions of the next.
@@ -209,32 +255,37 @@ __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_weig
         h0 = __builtin_amdgcn_readfirstlane(r - i * a.group);
     }
     if (t0 < t1) offsets();
+    const T *q_at = (const T *)a.q + (size_t)(sq.r0 + i0) * a.q_stride + (size_t)kvh * a.group * pv.d;
+    const float *l_at = w.lse_in + (size_t)(sq.r0 + i0) * a.n_heads + kvh * a.group;
+    const size_t q_step = step_i * a.q_stride, l_step = (size_t)step_i * a.n_heads;
     auto load = [&](int t, int stage) __attribute__((always_inline)) {
         if (t >= t1) return;
         // (the offsets are the last tile's, unless a tile is no whole number of rows, or this is the end of the rows)
-        if (t > t0 && (step_h || (t + 1) * 32 > rows)) offsets();
+        if (step_h || (t + 1) * 32 > rows) offsets();
         const unsigned at = lds0 + stage * BYTES + wave * 8 * TL::ROW;
-        const T *q = (const T *)a.q + (size_t)(sq.r0 + i0) * a.q_stride + (size_t)kvh * a.group * pv.d;
         if (a.aligned) {
 #pragma unroll
-            for (int e = 0; e < EACH; e++) dma16(at + e * 1024, off[e], (const char *)q);
+            for (int e = 0; e < EACH; e++) dma16(at + e * 1024, off[e], (const char *)q_at);
         } else {
 #pragma unroll
             for (int e = 0; e < EACH; e++) {
                 const int z = wave * 8 + e * TL::RPI + lane / TL::CPR, c = min((lane % TL::CPR) ^ TL::fk(z), pv.d * (int)sizeof(T) / 16 - 1);
                 const unsigned i = (unsigned)(h0 + z) / (unsigned)a.group;
-                const T *src = q + (size_t)min((int)i, sq.rows - 1 - i0) * a.q_stride + head[e] * pv.d + c * (16 / (int)sizeof(T));
+                const T *src = q_at + (size_t)min((int)i, sq.rows - 1 - i0) * a.q_stride + head[e] * pv.d + c * (16 / (int)sizeof(T));
                 T x[16 / sizeof(T)];
 #pragma unroll
                 for (int y = 0; y < 16 / (int)sizeof(T); y++) x[y] = src[y];
                 __builtin_memcpy(lds + stage * BYTES + wave * 8 * TL::ROW + e * 1024 + lane * 16, x, 16);
             }
         }
-        const float *l = w.lse_in + (size_t)(sq.r0 + i0) * a.n_heads + kvh * a.group;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lse0 + (stage * 4 + wave) * 256), "v"(off[EACH]), "s"(l) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lse0 + (stage * 4 + wave) * 256), "v"(off[EACH]), "s"(l_at) : "memory");
         i0 += step_i;
-        h0 += step_h;
-        if (h0 >= a.group) { h0 -= a.group; i0++; }
+        q_at += q_step;
+        l_at += l_step;
+        if (step_h) {
+            h0 += step_h;
+            if (h0 >= a.group) { h0 -= a.group; i0++; q_at += a.q_stride; l_at += a.n_heads; }
+        }
     };
 #pragma unroll
     for (int t = 0; t < RG; t++) load(t0 + t, t);
@@ -264,6 +315,7 @@ __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_weig
     for (int b = 0; b < KW; b++) sum[b] = 0.f;
     // Of a tile that has arrived: lse in log2 units less the scores' offset, by the lane that has the row; whether every row is there, its lse finite, and all of the wave's keys before it.
     const int whole0 = key0 + 32 * KW > sq.keys || a.window ? 0x7fffffff : (max(0, key0 + 32 * KW - 1 - base) * a.group + 31) / 32;
+    const int hidden = key0 < prefix ? 0 : max(0, key0 - base) * a.group / 32;
     bool masked;
     float mine;
     auto arrive = [&](int t, int stage) __attribute__((always_inline)) {
@@ -285,6 +337,15 @@ __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_weig
             for (int b = 0; b < KW; b++)
 #pragma unroll
                 for (int r = 0; r < 16; r++) x[b][r] = capped<T>(a, x[b][r]);
+        if (t < hidden) {                                     // none of the rows sees any of the wave's keys
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                l[r] = 0.f;
+#pragma unroll
+                for (int b = 0; b < KW; b++) x[b][r] = -INFINITY;
+            }
+            return;
+        }
         if (masked || (MODE & BIASED)) {
             // a lane's own row of the tile, for the others: lse as it is used, position (GONE: of a row that counts for nothing), slope
             const int at = t * 32 + col, i = (unsigned)at / (unsigned)a.group;
@@ -421,7 +482,7 @@ __global__ void __launch_bounds__(256) paged_weights_join_kernel(WeightArgs w, i
 // How a call is divided.
 struct WeightPlan {
     bool step;
-    int chunk, parts;
+    int chunk, parts, waves;
     long items;              // workgroups of a part
 };
 int weight_keys(int d, bool f32) { return 128 * (padded_dim(d) * (f32 ? 4 : 2) <= 256 ? 2 : 1); }
@@ -432,16 +493,19 @@ WeightPlan plan_weights(const AttnArgs &a, bool f32) {
     p.step = packed <= 32;
     p.parts = 1;
     if (p.step) {
-        // waves that stay (their rings of 24 KB: six a CU) with a few tiles each, where there are so many
         const long tiles = (pv.max_len + 31) / 32, all = pairs * tiles;
-        p.chunk = (int)(all / (6 * 256));
-        p.chunk = p.chunk < 2 ? 2 : p.chunk > STEP_TILES ? STEP_TILES : p.chunk;
-        p.items = pairs * ((tiles + p.chunk - 1) / p.chunk);
+        // (LDS is handed out in units of 1280 bytes)
+        const int units = (3 * 32 * padded_dim(pv.d) * (f32 ? 4 : 2) + (STEP_TILES + 3) * 128 + 1279) / 1280, fit = 128 / units;
+        p.waves = pv.n_seq <= 2048 && all < 1L << 30 ? 256 * (fit > 8 ? 8 : fit) / pv.n_kv : 0;
+        if (p.waves == 0 && pv.n_seq <= 2048 && all < 1L << 30) p.waves = 1;
+        if (p.waves > all / pv.n_kv) p.waves = all / pv.n_kv > 0 ? (int)(all / pv.n_kv) : 1;
+        p.chunk = STEP_TILES;
+        p.items = pv.n_seq <= 2048 && all < 1L << 30 ? (long)p.waves * pv.n_kv : pairs * ((tiles + p.chunk - 1) / p.chunk);
         return p;
     }
+    // Workgroups for six rounds of two a CU, with eight tiles of rows at least (4096 causal rows, 8 key heads: one round 141 us, from three to ten 120 to 128).
     const int keys = weight_keys(pv.d, f32);
     const long tiles = (packed + 31) / 32, blocks = pairs * ((pv.max_len + keys - 1) / keys);
-    // workgroups for six rounds of two a CU (4096 causal rows: of four 133 us, of six or eight 125, of sixteen 141), with eight tiles of rows at least
     long parts = blocks > 0 ? (6 * 512 + blocks - 1) / blocks : 1;
     if (parts > tiles / 8) parts = tiles / 8;
     if (parts > 256) parts = 256;
@@ -479,6 +543,7 @@ int launch_weights(WeightArgs w, const WeightPlan &p, hipStream_t st) {
     const PagedView &pv = w.a.pv;
     w.chunk = p.chunk;
     w.parts = p.parts;
+    w.waves = p.waves;
     if (p.step) {
         constexpr size_t bytes = 3 * 32 * Tile<T, DP>::ROW;
         if (int rc = vla_allow_lds((const void *)paged_weights_step_kernel<T, DP, MODE>, bytes)) return rc;
@@ -530,13 +595,16 @@ __device__ __forceinline__ unsigned order_of(float x) {
     return u >> 31 ? ~u : u | 1u << 31;
 }
 
-// A workgroup for each (sequence, key head): the least mass that stays, then the positions of what is above it and of the first that equal it, then their masses, a thousand
-// at a time, read before they are written: no mass lands behind its place, so mass_out may be mass.
-constexpr int EVICT_THREADS = 1024;
+// A workgroup for each (sequence, key head): the least mass that stays, then the positions of what is above it and of the first that equal it, in order.  Up to 32,768 masses are held in
+// LDS (HELD), read once and before any is written, so that mass_out may be mass.  Of more every pass reads them again, and the kept ones' come last, a thousand at a time, read before they are
+// written: none lands behind its place.  Positions without weight, many of a kind, are counted by ballot: as one bin they would be added to one after the other.
+constexpr int EVICT_THREADS = 1024, EVICT_HELD = 32 * 1024;
+template <bool HELD>
 __global__ void __launch_bounds__(EVICT_THREADS) paged_evict_select_kernel(EvictArgs a) {
+    extern __shared__ __attribute__((aligned(16))) float held[];
     __shared__ CutLds cut;
     const PagedView &pv = a.pv;
-    const int h = blockIdx.x % pv.n_kv, s = blockIdx.x / pv.n_kv, t = threadIdx.x;
+    const int h = blockIdx.x % (unsigned)pv.n_kv, s = blockIdx.x / (unsigned)pv.n_kv, t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const PagedSeq sq = paged_seq(pv, s);
     const int n = sq.keys;
     const size_t at = (size_t)s * pv.n_kv + h;
@@ -551,26 +619,48 @@ __global__ void __launch_bounds__(EVICT_THREADS) paged_evict_select_kernel(Evict
         return;
     }
     const int lo = a.first, hi = n - a.recent, want = a.keep - a.first - a.recent;
+    const unsigned zero = order_of(0.f);
+    if constexpr (HELD) {
+#pragma unroll 8
+        for (int i = t; i < n; i += EVICT_THREADS) held[i] = mass[i];
+        __syncthreads();
+        mass = held;
+    }
     Cut<unsigned> c{~0u, ~0u, 0};                             // (no mass is that: none is taken)
     if (want > 0)
         c = cut_keys<EVICT_THREADS, unsigned>([&](auto f) {
-#pragma unroll 8
-            for (int i = lo + t; i < hi; i += EVICT_THREADS) f(order_of(mass[i]));
+            for (int i0 = lo + wave * 64; i0 < hi; i0 += 4 * EVICT_THREADS) {
+                unsigned key[4];
+#pragma unroll
+                for (int u = 0; u < 4; u++) key[u] = order_of(mass[min(i0 + u * EVICT_THREADS + lane, hi - 1)]);
+                int zeros = 0;
+#pragma unroll
+                for (int u = 0; u < 4; u++) {
+                    const bool in = i0 + u * EVICT_THREADS + lane < hi;
+                    zeros += __popcll(__ballot(in & (key[u] == zero)));
+                    if (in & (key[u] != zero)) f(key[u], 1);
+                }
+                if (lane == 0 && zeros) f(zero, zeros);
+            }
         }, want, 32, 0u, cut);
     auto takes = [&](int i, bool *tie) {
-        const bool open = i >= lo && i < hi;
-        const unsigned key = open ? order_of(mass[i]) & c.mask : 0u;
-        *tie = open && key == c.prefix;
-        return !open || key > c.prefix;
+        const bool open = (i >= lo) & (i < hi);
+        const unsigned key = order_of(mass[i]) & c.mask;
+        *tie = open & (key == c.prefix);
+        return !open | (key > c.prefix);
     };
-    cut_numbers<EVICT_THREADS>(n, c.want, takes, [&](int place, int i) { kept[place] = i; }, cut);
-    for (int i0 = 0; i0 < a.keep; i0 += EVICT_THREADS) {
-        __syncthreads();
-        const int i = i0 + t;
-        const float m = i < a.keep ? mass[kept[i]] : 0.f;
-        __syncthreads();
-        if (i < a.keep) out[i] = m;
-    }
+    cut_numbers<EVICT_THREADS>(n, c.want, takes, [&](int place, int i) {
+        kept[place] = i;
+        if (HELD) out[place] = mass[i];
+    }, cut);
+    if constexpr (!HELD)
+        for (int i0 = 0; i0 < a.keep; i0 += EVICT_THREADS) {
+            __syncthreads();
+            const int i = i0 + t;
+            const float m = i < a.keep ? mass[kept[i]] : 0.f;
+            __syncthreads();
+            if (i < a.keep) out[i] = m;
+        }
 }
 
 // K and V of the kept positions to their places: 16 bytes a lane, four rows of one key head on their way at once.
@@ -666,7 +756,10 @@ int vla_paged_evict(const vla_paged_cache *cache, const vla_paged_batch *batch, 
     a.keep = keep; a.first = first; a.recent = recent; a.to_table = to_table; a.to_stride = to_stride; a.kept = kept; a.new_len = new_len;
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps("paged_evict", 0.0, st);
-    paged_evict_select_kernel<<<(unsigned)pairs, EVICT_THREADS, 0, st>>>(a);
+    if (batch->max_len <= EVICT_HELD) {
+        if (int rc = vla_allow_lds((const void *)paged_evict_select_kernel<true>, EVICT_HELD * sizeof(float))) return rc;
+        paged_evict_select_kernel<true><<<(unsigned)pairs, EVICT_THREADS, batch->max_len * sizeof(float), st>>>(a);
+    } else paged_evict_select_kernel<false><<<(unsigned)pairs, EVICT_THREADS, 0, st>>>(a);
     if (int rc = vla_check_launch("paged_evict")) return rc;
     if (least == 0) return VLA_OK;
     const int row_bytes = cache->head_dim * (cache->dtype == VLA_DTYPE_F32 ? 4 : 2), chunks = row_bytes / 16, per = 256 / chunks * 4;

@@ -26,7 +26,7 @@ template <int THREADS> __device__ __forceinline__ int cut_scan(int v, int *all, 
 // Taken are keys with (key & mask) > prefix, and of those with (key & mask) == prefix the first `want`.
 template <typename Key> struct Cut { Key prefix, mask; int want; };
 
-// The cut that leaves `want` (at least 1, at most as many as there are) of the keys that each(f) gives f, every thread its own.  top: the bits above it are the same in all of them, those of `same`.
+// The cut that leaves `want` (at least 1, at most as many as there are) of the keys that each(f) gives f, every thread its own, with how often they occur.  top: the bits above it are the same in all of them, those of `same`.
 template <int THREADS, typename Key, typename Each>
 __device__ __forceinline__ Cut<Key> cut_keys(Each each, int want, int top, Key same, CutLds &s) {
     constexpr int EACH = CUT_BINS / THREADS;
@@ -38,8 +38,8 @@ __device__ __forceinline__ Cut<Key> cut_keys(Each each, int want, int top, Key s
         const int shift = top > CUT_BITS ? top - CUT_BITS : 0, bits = top - shift;
         for (int i = threadIdx.x; i < CUT_BINS; i += THREADS) s.bins[i] = 0;
         __syncthreads();
-        each([&](Key key) {
-            if ((key & c.mask) == c.prefix) atomicAdd(&s.bins[CUT_BINS - 1 - (int)(key >> shift & (((Key)1 << bits) - 1))], 1);
+        each([&](Key key, int times) {
+            if ((key & c.mask) == c.prefix) atomicAdd(&s.bins[CUT_BINS - 1 - (int)(key >> shift & (((Key)1 << bits) - 1))], times);
         });
         __syncthreads();
         // the digit at which the count from above reaches `want` (bins lie largest digit first)
@@ -73,12 +73,20 @@ __device__ __forceinline__ void cut_numbers(int n, int want, Takes takes, Put pu
     constexpr int WAVES = THREADS / 64;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int run = (n + 64 * WAVES - 1) / (64 * WAVES) * 64, i0 = min(wave * run, n), i1 = min(i0 + run, n);
+    constexpr int U = 8;                                     // of a lane at once
     int sure = 0, ties = 0;
-    for (int i = i0; i < i1; i += 64) {
-        bool tie = false;
-        const bool take = i + lane < i1 && takes(i + lane, &tie);
-        sure += __popcll(__ballot(take));
-        ties += __popcll(__ballot(i + lane < i1 && tie));
+    for (int i = i0; i < i1; i += 64 * U) {
+        bool take[U], tie[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int j = i + u * 64 + lane;
+            tie[u] = false;
+            take[u] = takes(min(j, n - 1), &tie[u]);
+            take[u] &= j < i1;
+            tie[u] &= j < i1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) { sure += __popcll(__ballot(take[u])); ties += __popcll(__ballot(tie[u])); }
     }
     __syncthreads();
     if (lane == 0) { s.bins[wave] = sure; s.bins[16 + wave] = ties; }
@@ -87,14 +95,24 @@ __device__ __forceinline__ void cut_numbers(int n, int want, Takes takes, Put pu
     for (int w = 0; w < wave; w++) { place += s.bins[w]; tied += s.bins[16 + w]; }
     place += min(tied, want);
     const unsigned long long below = (1ull << lane) - 1;
-    for (int i = i0; i < i1; i += 64) {
-        bool tie = false;
-        const bool in = i + lane < i1, sure = in && takes(i + lane, &tie);
-        const unsigned long long t = __ballot(in && tie);
-        const bool take = sure || (in && tie && tied + __popcll(t & below) < want);
-        const unsigned long long all = __ballot(take);
-        if (take) put(place + __popcll(all & below), i + lane);
-        place += __popcll(all);
-        tied += __popcll(t);
+    for (int i = i0; i < i1; i += 64 * U) {
+        bool take[U], tie[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int j = i + u * 64 + lane;
+            tie[u] = false;
+            take[u] = takes(min(j, n - 1), &tie[u]);
+            take[u] &= j < i1;
+            tie[u] &= j < i1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const unsigned long long t = __ballot(tie[u]);
+            const bool in = take[u] | (tie[u] & (tied + __popcll(t & below) < want));
+            const unsigned long long all = __ballot(in);
+            if (in) put(place + __popcll(all & below), i + u * 64 + lane);
+            place += __popcll(all);
+            tied += __popcll(t);
+        }
     }
 }

@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(256) paged_select_kernel(SelectArgs a) {
         __syncthreads();
         x = differ[0] | differ[1] | differ[2] | differ[3];
         c = cut_keys<256, unsigned long long>([&](auto f) {
-            for (int i = lo + t; i < hi; i += 256) f(key[i]);
+            for (int i = lo + t; i < hi; i += 256) f(key[i], 1);
         }, want, x ? 64 - __builtin_clzll(x) : 0, one, cut);
     }
     auto takes = [&](int i, bool *tie) {

@@ -40,10 +40,11 @@ struct AcceptArgs {
     int32_t *path, *n_accepted, *next, *new_len;
 };
 __global__ void __launch_bounds__(256) paged_accept_kernel(AcceptArgs a) {
-    __shared__ int32_t up[VLA_TREE_ROWS], id[VLA_TREE_ROWS], want[VLA_TREE_ROWS], path[VLA_TREE_ROWS + 1];
-    __shared__ long from[VLA_TREE_ROWS], to[VLA_TREE_ROWS];
+    extern __shared__ long places[];                         // [max_rows] from, to; then up, id, want, path
     __shared__ int found;
     const PagedView &pv = a.pv;
+    long *from = places, *to = from + pv.max_rows;
+    int32_t *up = (int32_t *)(to + pv.max_rows), *id = up + pv.max_rows, *want = id + pv.max_rows, *path = want + pv.max_rows;
     const int s = blockIdx.x, t = threadIdx.x;
     const PagedSeq sq = paged_seq(pv, s);
     for (int i = t; i < sq.rows; i += 256) {
@@ -155,13 +156,14 @@ int vla_paged_accept(const vla_paged_cache *cache, int n_layers, size_t layer_st
     a.layer_bytes = layer_stride * a.es;
     a.parent = parent; a.ids = ids; a.chosen = chosen; a.path = path; a.n_accepted = n_accepted; a.next = next; a.new_len = new_len;
     a.units = 2 * n_layers * a.pv.n_kv;
-    // a workgroup's lanes each have 16 bytes of a row at a time
+    // a workgroup's lanes each have 16 bytes of a row at a time; as many workgroups as stay on the chip at once (each walks the path again)
     const int chunks = a.pv.d * a.es / 16;
+    const long all = (long)a.units * a.pv.n_seq;
     a.per_block = chunks < 256 ? 256 / chunks : 1;
-    while ((a.units + a.per_block - 1) / a.per_block > 65535) a.per_block *= 2;
+    while (all > 2048L * a.per_block || a.units > 65535L * a.per_block) a.per_block *= 2;
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps("paged_accept", 0.0, st);
-    paged_accept_kernel<<<dim3(a.pv.n_seq, a.units > 0 ? (a.units + a.per_block - 1) / a.per_block : 1), 256, 0, st>>>(a);
+    paged_accept_kernel<<<dim3(a.pv.n_seq, a.units > 0 ? (a.units + a.per_block - 1) / a.per_block : 1), 256, a.pv.max_rows * 32, st>>>(a);
     return vla_check_launch("paged_accept");
 }
 

@@ -171,6 +171,17 @@ def test_evict_ties_and_odd_masses():
             cut(b, "f32", 2, 16, keep, first, recent, masses, in_place=True)
 
 
+def test_evict_of_more_than_are_held():
+    """Above 32,768 positions the masses are read again for every pass; the same by small caches under a loose bound."""
+    b = Batch([(0, 40000), (0, 33000), (0, 70)], 128)
+    g = torch.Generator().manual_seed(5)
+    for masses in (torch.rand(3, 1, b.max_len, generator=g), torch.randint(0, 2, (3, 1, b.max_len), generator=g).float()):
+        for in_place in (False, True):
+            cut(b, "f32", 1, 16, 3000, 2, 1000, masses, in_place=in_place)
+    b = Batch(HELD, 16, max_len=40000)
+    cut(b, "bf16", 2, 16, 40, 4, 10, torch.rand(len(HELD), 2, b.max_len, generator=g), in_place=True)
+
+
 def test_evict_in_place_masses_and_own_pages():
     b = Batch([(0, 50), (0, 10), (0, 500), (0, 64)], 16)
     masses = torch.rand(4, 2, b.max_len, generator=torch.Generator().manual_seed(3))
