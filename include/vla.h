@@ -457,6 +457,23 @@ int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, 
  *   sequence, at least keep / page_size rounded up), mass to mass_out [n_seq][n_kv_heads][mass_out_stride] (mass itself with its stride, or apart
  *   from it; entries behind the last keep what they hold).  new_len [n_seq] out or NULL: min(kv_len, keep).  to_table's pages hold nothing that the call reads, but that a sequence
  *   with no more than `keep` may name its own pages again (nothing moves).  One layer a call.  Of the batch it uses the sequences, not their rows. */
+/* vla_forward_paged_rows: vla_forward_paged with these, and with the logits of every row (a tree's nodes are all read).
+ *   position, seen (words to a row), prefix_len: as above, each or NULL; bounds: [n_layers] of vla_paged_bounds' arrays or NULL: kept up with the
+ *   new rows; n_select above 0 (bounds given): rows read the pages that vla_paged_select takes with first and recent; mass
+ *   [n_layers][n_seq][n_kv_heads][mass_stride] or NULL: vla_paged_weights of every layer.  A tree, selected pages, and weights or a prefix mask exclude each other.
+ *   logits  DEVICE fp32 [n_rows, 256] out (of padding rows: of no meaning).  ws: of vla_forward_paged_rows_workspace_bytes bytes. */
+typedef struct vla_paged_rows {
+    const int32_t *position, *seen, *prefix_len;
+    void *bounds;
+    float *mass;
+    int64_t mass_stride;
+    int32_t words, n_select, first, recent;
+} vla_paged_rows;
+size_t vla_forward_paged_rows_workspace_bytes(const vla_config *cfg, const vla_paged_cache *cache, const vla_paged_batch *batch,
+                                              const vla_paged_rows *rows, int shared_len);
+int vla_forward_paged_rows(vla_model *model, const vla_paged_cache *cache, size_t layer_stride, const vla_paged_batch *batch,
+                           const vla_paged_rows *rows, const int32_t *ids, const void *patch, int n_patch, int shared_len, void *ws,
+                           size_t ws_bytes, float *logits, void *stream);
 int vla_paged_append_at(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_rotary *rotary, const int32_t *position,
                         const void *q, const void *k, const void *v, int in_dtype, int n_heads, int64_t q_stride, int64_t k_stride,
                         int64_t v_stride, void *q_out, int64_t q_out_stride, void *stream);

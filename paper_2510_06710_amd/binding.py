@@ -84,6 +84,12 @@ class vla_paged_mask(C.Structure):
                 ("shared_len", C.c_int32)]
 
 
+class vla_paged_rows(C.Structure):
+    keep, device = (), None
+    _fields_ = [("position", C.c_void_p), ("seen", C.c_void_p), ("prefix_len", C.c_void_p), ("bounds", C.c_void_p), ("mass", C.c_void_p), ("mass_stride", C.c_int64),
+                ("words", C.c_int32), ("n_select", C.c_int32), ("first", C.c_int32), ("recent", C.c_int32)]
+
+
 class VlaError(RuntimeError):
     def __init__(self, code: int, message: str):
         super().__init__(f"libvla error {code}: {message}")
@@ -165,6 +171,10 @@ def lib() -> C.CDLL:
         L.vla_paged_weights_workspace_bytes.restype = sz
         L.vla_paged_weights.argtypes = [cache, batch, mask, vp, i32, i64, vp, vp, i64, vp, sz, vp]
         L.vla_paged_evict.argtypes = [cache, batch, vp, i64, i32, i32, i32, vp, i32, vp, vp, i64, vp, vp]
+        rows = C.POINTER(vla_paged_rows)
+        L.vla_forward_paged_rows_workspace_bytes.argtypes = [C.POINTER(vla_config), cache, batch, rows, i32]
+        L.vla_forward_paged_rows_workspace_bytes.restype = sz
+        L.vla_forward_paged_rows.argtypes = [vp, cache, sz, batch, rows, vp, vp, i32, i32, vp, sz, vp, vp]
         dp = C.POINTER(C.c_double)
         L.vla_pipeline_time.argtypes = [C.c_double, C.c_double, i32, i32, dp]
         L.vla_profile_lookup.argtypes = [dp, i32, C.c_double, dp]
@@ -672,6 +682,43 @@ def vla_paged_evict(cache, batch, mass, first: int, recent: int, to_table, kept,
     pages, which, lens = _ints(to_table, "to_table", n, entries), _ints(kept, "kept", n, cache.n_kv_heads, keep), _ints(new_len, "new_len", n)
     _on_current_device("paged_evict", (cache, batch), (mass, to_table, kept, mass_out, new_len))
     _check(lib().vla_paged_evict(C.byref(cache), C.byref(batch), *sums, keep, first, recent, pages, entries, which, *out, lens, _stream(stream)))
+
+
+def make_paged_rows(position=None, seen=None, prefix_len=None, bounds=None, n_select=0, first=1, recent=1, mass=None) -> vla_paged_rows:
+    """``position`` int32 [n_rows], ``seen`` int32 [n_rows, words], ``prefix_len`` int32 [n_seq], ``bounds`` [n_layers, n_pages, n_kv_heads, 2, head_dim] in the cache's type,
+    ``mass`` fp32 [n_layers, n_seq, n_kv_heads, positions]."""
+    if (seen is not None and seen.dim() != 2) or (bounds is not None and bounds.dim() != 5) or (mass is not None and mass.dim() != 4):
+        raise VlaError(VLA_ESHAPE, "paged_rows: seen is [n_rows, words], bounds [n_layers, n_pages, n_kv_heads, 2, head_dim], mass [n_layers, n_seq, n_kv_heads, positions]")
+    if bounds is not None and not bounds.is_contiguous():
+        raise VlaError(VLA_EINVAL, "paged_rows: bounds is not contiguous")
+    r = vla_paged_rows(_want(position, "int32", "position"), _want(seen, "int32", "seen"), _want(prefix_len, "int32", "prefix_len"), _ptr(bounds), _want(mass, "float32", "mass"),
+                       0 if mass is None else mass.shape[3], 0 if seen is None else seen.shape[1], n_select, first, recent)
+    r.keep, r.device = (position, seen, prefix_len, bounds, mass), _device_of(position, seen, prefix_len, bounds, mass)
+    return r
+
+
+def vla_forward_paged_rows_workspace_bytes(cfg: vla_config, cache, batch, rows, shared_len: int = 0) -> int:
+    return _positive(lib().vla_forward_paged_rows_workspace_bytes(C.byref(cfg), C.byref(cache), C.byref(batch), C.byref(rows), shared_len))
+
+
+def vla_forward_paged_rows(model, cache, layer_stride: int, n_layers: int, batch, rows, ids, ws, logits, patch=None, shared_len=0, stream=None) -> None:
+    """``ids`` int32 [n_rows]; ``logits`` fp32 [n_rows, 256] out; ``n_layers``: the model's, which bounds and mass have to have."""
+    n, hidden = batch.n_rows, cache.n_kv_heads * cache.head_dim
+    if patch is not None and (not patch.is_contiguous() or patch.dim() != 2 or patch.shape[1] != hidden or _dtype(patch) != cache.dtype):
+        raise VlaError(VLA_EINVAL, f"forward_paged_rows: patch is not contiguous [n_patch, {hidden}] of the cache's type")
+    if rows.keep:
+        position, seen, prefix_len, bounds, mass = rows.keep
+        _ints(position, "position", n), _ints(prefix_len, "prefix_len", batch.n_seq)
+        if seen is not None and seen.shape[0] != n:
+            raise VlaError(VLA_ESHAPE, f"forward_paged_rows: seen is {list(seen.shape)}, wanted [{n}, words]")
+        if bounds is not None and (bounds.shape != (n_layers, cache.n_pages, cache.n_kv_heads, 2, cache.head_dim) or _dtype(bounds) != cache.dtype):
+            raise VlaError(VLA_ESHAPE, f"forward_paged_rows: bounds is {bounds.dtype} {list(bounds.shape)}, wanted [{n_layers}, {cache.n_pages}, {cache.n_kv_heads}, 2, {cache.head_dim}] of the cache's type")
+        if mass is not None and mass.shape[:3] != (n_layers, batch.n_seq, cache.n_kv_heads):
+            raise VlaError(VLA_ESHAPE, f"forward_paged_rows: mass is {list(mass.shape)}, wanted [{n_layers}, {batch.n_seq}, {cache.n_kv_heads}, positions]")
+    arrays = _ints(ids, "ids", n), _want(logits, "float32", "logits", (n, VLA_N_BINS))
+    _on_current_device("forward_paged_rows", (cache, batch, rows), (ids, patch, ws, logits))
+    _check(lib().vla_forward_paged_rows(model, C.byref(cache), layer_stride, C.byref(batch), C.byref(rows), arrays[0], _ptr(patch), 0 if patch is None else patch.shape[0], shared_len,
+                                        *_ws(ws), arrays[1], _stream(stream)))
 
 
 def _doubles(values):

@@ -718,24 +718,41 @@ struct PagedWorkspace {
     Workspace w;
     float *last;             // [n_seq, H]
     double *freq;            // [d / 2]
-    int32_t *bins;           // of the head, which samples too: [n_seq]
+    int32_t *bins;           // of the head, which samples too: [head rows]
     float *logp, *ent;
     void *attn;
     size_t attn_bytes, total;
+    // vla_forward_paged_rows: lse of the attention, the pages that rows read, and the workspaces of what chooses and weighs them
+    float *lse;
+    int32_t *selected;
+    void *select, *weights;
+    size_t select_bytes, weights_bytes;
 };
-static PagedWorkspace plan_paged(const vla_config &c, char *base, const vla_paged_batch &b, size_t attn_bytes) {
-    PagedWorkspace p;
+// What the attention operators of a call take of the workspace.
+struct PagedSizes { size_t attn, select, weights; };
+// rows: a head for every row (vla_forward_paged_rows), else for every sequence's last.
+static PagedWorkspace plan_paged(const vla_config &c, char *base, const vla_paged_batch &b, const PagedSizes &sizes, const vla_paged_rows *rows = nullptr) {
+    PagedWorkspace p{};
     const bool step = b.max_rows <= 1;
-    p.w = plan_workspace(c, base, step ? b.n_rows : 1, step ? 1 : b.n_rows, 1, b.n_seq, false);
+    const size_t heads = rows ? b.n_rows : b.n_seq;
+    p.w = plan_workspace(c, base, step ? b.n_rows : 1, step ? 1 : b.n_rows, 1, (int)heads, false);
     size_t off = p.w.total;
     auto take = [&](size_t bytes) { char *at = base ? base + off : nullptr; off += align_up(bytes); return (void *)at; };
-    p.last = (float *)take((size_t)b.n_seq * c.hidden * 4);
+    p.last = (float *)take(heads * c.hidden * 4);
     p.freq = (double *)take((size_t)c.hidden / c.n_heads / 2 * sizeof(double));
-    p.bins = (int32_t *)take((size_t)b.n_seq * 4);
-    p.logp = (float *)take((size_t)b.n_seq * 4);
-    p.ent = (float *)take((size_t)b.n_seq * 4);
-    p.attn = take(attn_bytes);
-    p.attn_bytes = attn_bytes;
+    p.bins = (int32_t *)take(heads * 4);
+    p.logp = (float *)take(heads * 4);
+    p.ent = (float *)take(heads * 4);
+    p.attn = take(sizes.attn);
+    p.attn_bytes = sizes.attn;
+    if (rows) {
+        p.lse = (float *)take((size_t)b.n_rows * c.n_heads * 4);
+        p.selected = (int32_t *)take((size_t)b.n_rows * c.n_heads * rows->n_select * 4);
+        p.select = take(sizes.select);
+        p.weights = take(sizes.weights);
+        p.select_bytes = sizes.select;
+        p.weights_bytes = sizes.weights;
+    }
     p.total = off;
     return p;
 }
@@ -744,11 +761,28 @@ static vla_paged_mask paged_mask(const vla_config &c, const int32_t *prefix_len,
     return vla_paged_mask{1.0f / sqrtf((float)(c.hidden / c.n_heads)), 0.f, nullptr, prefix_len, 0, shared_len};
 }
 
+// One layer's attention of vla_forward_paged_rows: to a tree, to the pages that each row selects, or to all; then the weights that rows gave.
+static int attend_rows(const vla_config &c, const vla_paged_cache &layer, int l, const vla_paged_batch &b, const vla_paged_mask &mask, const vla_paged_rows &rows, const void *q, void *out,
+                       const PagedWorkspace &pw, void *stream) {
+    const int H = c.hidden;
+    int rc;
+    void *bounds = rows.bounds ? (char *)rows.bounds + (size_t)l * layer.n_pages * layer.n_kv_heads * 2 * layer.head_dim * elt_size(c) : nullptr;
+    if (bounds && (rc = vla_paged_bounds(&layer, &b, bounds, stream))) return rc;
+    if (rows.n_select > 0) {
+        if ((rc = vla_paged_select(&layer, &b, bounds, q, c.n_heads, H, rows.n_select, rows.first, rows.recent, pw.selected, pw.select, pw.select_bytes, stream))) return rc;
+        return vla_paged_sparse_attention(&layer, &b, &mask, pw.selected, rows.n_select, q, c.n_heads, H, out, H, nullptr, pw.attn, pw.attn_bytes, stream);
+    }
+    if (rows.seen) return vla_paged_tree_attention(&layer, &b, &mask, rows.seen, rows.words, q, c.n_heads, H, out, H, nullptr, pw.attn, pw.attn_bytes, stream);
+    if ((rc = vla_paged_attention(&layer, &b, &mask, q, c.n_heads, H, out, H, rows.mass ? pw.lse : nullptr, pw.attn, pw.attn_bytes, stream))) return rc;
+    if (!rows.mass) return VLA_OK;
+    return vla_paged_weights(&layer, &b, &mask, q, c.n_heads, H, pw.lse, rows.mass + (size_t)l * b.n_seq * layer.n_kv_heads * rows.mass_stride, rows.mass_stride, pw.weights, pw.weights_bytes, stream);
+}
+
 // Layer by layer as run_layers has it, on row-major activations; rotation and K, V by the paged append, attention on the pages.
 template <typename T>
 static int forward_paged_impl(vla_model *m, const vla_paged_cache &cache, size_t layer_stride, const vla_paged_batch &b, const int32_t *ids,
                               const void *patch, int n_patch, const vla_paged_mask &mask, const PagedWorkspace &pw, float *h_last,
-                              float *logits, float *value, void *stream) {
+                              float *logits, float *value, void *stream, const vla_paged_rows *rows = nullptr) {
     const vla_config &c = m->cfg;
     const Workspace &ws = pw.w;
     const int H = c.hidden, F = c.ffn, M = b.n_rows, d = H / c.n_heads;
@@ -775,12 +809,21 @@ static int forward_paged_impl(vla_model *m, const vla_paged_cache &cache, size_t
         const void *o_kb = pk ? pk->wo : nullptr, *down_kb = pk ? pk->w_down : nullptr;
         if ((rc = run_rmsnorm<T>(c, ws.Nrm, ws.X, lw.attn_norm, M, 0, st))) return rc;
         if ((rc = product(ws.Nrm, H, qkv, pk ? qkv_kb : nullptr, 3, H, ws.QKV, EPI_STORE))) return rc;
-        if ((rc = vla_paged_append(&layer, &b, &rotary, ws.QKV, ws.QKV + H, ws.QKV + 2 * H, VLA_DTYPE_F32, c.n_heads, 3L * H, 3L * H, 3L * H, ws.Q, H, stream))) return rc;
-        if ((rc = vla_paged_attention(&layer, &b, &mask, ws.Q, c.n_heads, H, ws.AO, H, nullptr, pw.attn, pw.attn_bytes, stream))) return rc;
+        if ((rc = rows && rows->position
+                      ? vla_paged_append_at(&layer, &b, &rotary, rows->position, ws.QKV, ws.QKV + H, ws.QKV + 2 * H, VLA_DTYPE_F32, c.n_heads, 3L * H, 3L * H, 3L * H, ws.Q, H, stream)
+                      : vla_paged_append(&layer, &b, &rotary, ws.QKV, ws.QKV + H, ws.QKV + 2 * H, VLA_DTYPE_F32, c.n_heads, 3L * H, 3L * H, 3L * H, ws.Q, H, stream))) return rc;
+        if (!rows) rc = vla_paged_attention(&layer, &b, &mask, ws.Q, c.n_heads, H, ws.AO, H, nullptr, pw.attn, pw.attn_bytes, stream);
+        else rc = attend_rows(c, layer, l, b, mask, *rows, ws.Q, ws.AO, pw, stream);
+        if (rc) return rc;
         if ((rc = product(ws.AO, H, &lw.wo, pk ? &o_kb : nullptr, 1, H, ws.X, EPI_RESIDUAL))) return rc;
         if ((rc = run_rmsnorm<T>(c, ws.Nrm, ws.X, lw.ffn_norm, M, 0, st))) return rc;
         if ((rc = product(ws.Nrm, H, ffn, pk ? ffn_kb : nullptr, 2, F, ws.ACT, EPI_SWIGLU))) return rc;
         if ((rc = product(ws.ACT, F, &lw.w_down, pk ? &down_kb : nullptr, 1, H, ws.X, EPI_RESIDUAL))) return rc;
+    }
+    if (rows) {
+        if ((rc = launch_final_norm_rows(pw.last, ws.X, (const float *)m->w.final_norm, M, 1, 0, 1, H, c.rms_eps, st))) return rc;
+        return launch_head_sample<T>(pw.last, (const T *)m->w.lm_head + (size_t)(c.vocab - VLA_N_BINS) * H, M, H, 1.0f, nullptr, nullptr, pw.bins, pw.logp, pw.ent, logits, 1, 0, nullptr,
+                                     (const T *)nullptr, c.vocab, ws.QKV, st);
     }
     if ((rc = launch_paged_last_rows(pw.last, ws.X, b.row_start, b.n_seq, M, H, st))) return rc;
     if ((rc = launch_final_norm_rows(h_last, pw.last, (const float *)m->w.final_norm, b.n_seq, 1, 0, 1, H, c.rms_eps, st))) return rc;
@@ -803,6 +846,27 @@ static int check_forward_paged(const vla_config &c, const vla_paged_cache *cache
     *attn_bytes = vla_paged_attention_workspace_bytes(cache, b, &mask, c.n_heads);
     return *attn_bytes ? VLA_OK : VLA_EINVAL;
 }
+// ... and those of vla_forward_paged_rows.
+static int check_forward_rows(const vla_config &c, const vla_paged_cache *cache, const vla_paged_batch *b, const vla_paged_mask &mask, const vla_paged_rows *r, PagedSizes *sizes) {
+    if (!r) { vla_set_error("forward_paged_rows: rows is NULL"); return VLA_EINVAL; }
+    if (int rc = check_forward_paged(c, cache, b, mask, &sizes->attn)) return rc;
+    if (r->n_select < 0 || (r->n_select > 0 && !r->bounds)) { vla_set_error("forward_paged_rows: n_select is negative, or without bounds"); return VLA_EINVAL; }
+    if ((r->seen != nullptr) + (r->n_select > 0) + (r->mass || r->prefix_len) > 1) {
+        vla_set_error("forward_paged_rows: a tree, selected pages, and weights or a prefix mask exclude each other");
+        return VLA_EINVAL;
+    }
+    if (r->seen && (r->words < 1 || r->words > VLA_TREE_ROWS / 32 || r->words * 32 < b->max_rows)) { vla_set_error("forward_paged_rows: %d words for trees of up to %d rows", r->words, b->max_rows); return VLA_ESHAPE; }
+    if (r->bounds && (uintptr_t)r->bounds % 16) { vla_set_error("forward_paged_rows: bounds is not 16-byte aligned"); return VLA_EINVAL; }
+    if (r->mass && r->mass_stride < b->max_len) { vla_set_error("forward_paged_rows: mass of %ld positions, max_len is %d", (long)r->mass_stride, b->max_len); return VLA_ESHAPE; }
+    if (r->n_select > 0) {
+        if (r->first < 0 || r->recent < 1 || (long)r->first + r->recent > r->n_select) { vla_set_error("forward_paged_rows: n_select %d, first %d, recent %d", r->n_select, r->first, r->recent); return VLA_EINVAL; }
+        sizes->select = vla_paged_select_workspace_bytes(cache, b);
+        sizes->attn = vla_paged_sparse_attention_workspace_bytes(cache, b, &mask, c.n_heads, r->n_select);
+        if (!sizes->select || !sizes->attn) return VLA_ESHAPE;
+    }
+    if (r->mass && !(sizes->weights = vla_paged_weights_workspace_bytes(cache, b, &mask, c.n_heads))) return VLA_ESHAPE;
+    return VLA_OK;
+}
 
 // ------------------------------------------------------------------------------------------ C ABI
 extern "C" {
@@ -810,7 +874,32 @@ extern "C" {
 size_t vla_forward_paged_workspace_bytes(const vla_config *cfg, const vla_paged_cache *cache, const vla_paged_batch *batch, int shared_len) {
     size_t attn = 0;
     if (check_config(cfg) || check_forward_paged(*cfg, cache, batch, paged_mask(*cfg, nullptr, shared_len), &attn)) return 0;
-    return plan_paged(*cfg, nullptr, *batch, attn).total;
+    return plan_paged(*cfg, nullptr, *batch, PagedSizes{attn, 0, 0}).total;
+}
+
+size_t vla_forward_paged_rows_workspace_bytes(const vla_config *cfg, const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_paged_rows *rows,
+                                              int shared_len) {
+    PagedSizes sizes{};
+    if (check_config(cfg) || check_forward_rows(*cfg, cache, batch, paged_mask(*cfg, rows ? rows->prefix_len : nullptr, shared_len), rows, &sizes)) return 0;
+    return plan_paged(*cfg, nullptr, *batch, sizes, rows).total;
+}
+
+int vla_forward_paged_rows(vla_model *m, const vla_paged_cache *cache, size_t layer_stride, const vla_paged_batch *batch, const vla_paged_rows *rows,
+                           const int32_t *ids, const void *patch, int n_patch, int shared_len, void *ws, size_t ws_bytes, float *logits, void *stream) {
+    if (!m || !ids || !ws || !logits) { vla_set_error("forward_paged_rows: model, ids, ws or logits is NULL"); return VLA_EINVAL; }
+    if (n_patch < 0 || (n_patch > 0 && !patch)) { vla_set_error("forward_paged_rows: n_patch is negative or patch is NULL"); return VLA_EINVAL; }
+    const vla_config &c = m->cfg;
+    const vla_paged_mask mask = paged_mask(c, rows ? rows->prefix_len : nullptr, shared_len);
+    PagedSizes sizes{};
+    if (int rc = check_forward_rows(c, cache, batch, mask, rows, &sizes)) return rc;
+    const size_t layer = (size_t)cache->n_pages * cache->n_kv_heads * cache->page_size * cache->head_dim;
+    if (c.n_layers > 1 && layer_stride < layer) { vla_set_error("forward_paged_rows: layer stride of %zu elements, a layer has %zu", layer_stride, layer); return VLA_ESHAPE; }
+    if (layer_stride * elt_size(c) % 16) { vla_set_error("forward_paged_rows: the layers are not 16-byte aligned"); return VLA_EINVAL; }
+    if ((uintptr_t)ws % 16) { vla_set_error("forward_paged_rows: ws is not 16-byte aligned"); return VLA_EINVAL; }
+    const PagedWorkspace p = plan_paged(c, (char *)ws, *batch, sizes, rows);
+    if (ws_bytes < p.total) { vla_set_error("workspace %zu bytes, need %zu", ws_bytes, p.total); return VLA_EWORKSPACE; }
+    return c.dtype == VLA_DTYPE_F32 ? forward_paged_impl<float>(m, *cache, layer_stride, *batch, ids, patch, n_patch, mask, p, nullptr, logits, nullptr, stream, rows)
+                                    : forward_paged_impl<bf16_t>(m, *cache, layer_stride, *batch, ids, patch, n_patch, mask, p, nullptr, logits, nullptr, stream, rows);
 }
 
 int vla_forward_paged(vla_model *m, const vla_paged_cache *cache, size_t layer_stride, const vla_paged_batch *batch, const int32_t *ids,
@@ -827,7 +916,7 @@ int vla_forward_paged(vla_model *m, const vla_paged_cache *cache, size_t layer_s
     if (c.n_layers > 1 && layer_stride < layer) { vla_set_error("forward_paged: layer stride of %zu elements, a layer has %zu", layer_stride, layer); return VLA_ESHAPE; }
     if (layer_stride * elt_size(c) % 16) { vla_set_error("forward_paged: the layers are not 16-byte aligned"); return VLA_EINVAL; }
     if ((uintptr_t)ws % 16) { vla_set_error("forward_paged: ws is not 16-byte aligned"); return VLA_EINVAL; }
-    const PagedWorkspace p = plan_paged(c, (char *)ws, *batch, attn);
+    const PagedWorkspace p = plan_paged(c, (char *)ws, *batch, PagedSizes{attn, 0, 0});
     if (ws_bytes < p.total) { vla_set_error("workspace %zu bytes, need %zu", ws_bytes, p.total); return VLA_EWORKSPACE; }
     return c.dtype == VLA_DTYPE_F32 ? forward_paged_impl<float>(m, *cache, layer_stride, *batch, ids, patch, n_patch, mask, p, h_last, logits, value, stream)
                                     : forward_paged_impl<bf16_t>(m, *cache, layer_stride, *batch, ids, patch, n_patch, mask, p, h_last, logits, value, stream);
