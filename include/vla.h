@@ -422,7 +422,7 @@ int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, 
  * vla_paged_tree: seen [n_rows][words] out, DEVICE int32: bit j % 32 of word j / 32 says that the row sees its sequence's new row j: its
  *   ancestors and itself; position [n_rows] out or NULL: kv_len - n_s + depth.  words: at least max_rows / 32 rounded up, at most 32.
  * vla_paged_tree_attention: as vla_paged_attention, but a row sees the positions below kv_len - n_s and of the new rows those whose
- *   bits are set in its `seen` (any bits: not only a tree's).  mask: scale, softcap and shared_len (at most kv_len - n_s of every sequence with rows) alone;
+ *   bits are set in its `seen` (any bits: not only a tree's; K and V of the new rows are finite).  mask: scale, softcap and shared_len (at most kv_len - n_s of every sequence with rows) alone;
  *   slopes and prefix_len NULL, window 0.  On a bf16 cache weights enter the products with v with 16 bits whatever the number of rows.
  *   ws: of vla_paged_attention_workspace_bytes bytes.
  * vla_paged_accept: the drafts that the model agrees with.  ids: DEVICE int32 [n_rows], the rows' tokens; chosen: DEVICE int32

@@ -40,8 +40,11 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedView &p, int s) {
     return q;
 }
 
-// The sequence of a row (n_seq: padding), by all 64 lanes of a wave: how many of row_start[1 ..] lie at or before it.
+// The sequence of a row (n_seq: padding), by all 64 lanes of a wave: how many of row_start[1 ..] lie at or before it.  Where sequences have one row each, as in a decode step, it is the row's
+// own number: two words to look at.
 __device__ __forceinline__ int paged_seq_of_row(const PagedView &p, int row) {
+    const int guess = min(row, p.n_seq - 1);
+    if (paged_int(p.row_start, guess) <= row && paged_int(p.row_start, guess + 1) > row) return guess;
     int n = 0;
     for (int s = threadIdx.x & 63; s < p.n_seq; s += 64) n += paged_int(p.row_start, s + 1) <= row;
 #pragma unroll

@@ -595,13 +595,13 @@ __device__ __forceinline__ unsigned order_of(float x) {
     return u >> 31 ? ~u : u | 1u << 31;
 }
 
-// A workgroup for each (sequence, key head): the least mass that stays, then the positions of what is above it and of the first that equal it, in order.  Up to 32,768 masses are held in
-// LDS (HELD), read once and before any is written, so that mass_out may be mass.  Of more every pass reads them again, and the kept ones' come last, a thousand at a time, read before they are
-// written: none lands behind its place.  Positions without weight, many of a kind, are counted by ballot: as one bin they would be added to one after the other.
+// A workgroup for each (sequence, key head): the least mass that stays, then the positions of what is above it and of the first that equal it, in order, then their masses, a thousand at a time, read
+// before they are written: none lands behind its place, so mass_out may be mass.  Up to 32,768 positions' masses are held in LDS as the numbers they are ordered by (HELD); of more every pass reads
+// them again.  The first and last that stay anyway have the largest number.  Positions without weight, many of a kind, are counted by ballot: as one bin they would be added to one after the other.
 constexpr int EVICT_THREADS = 1024, EVICT_HELD = 32 * 1024;
 template <bool HELD>
 __global__ void __launch_bounds__(EVICT_THREADS) paged_evict_select_kernel(EvictArgs a) {
-    extern __shared__ __attribute__((aligned(16))) float held[];
+    extern __shared__ __attribute__((aligned(16))) unsigned held[];
     __shared__ CutLds cut;
     const PagedView &pv = a.pv;
     const int h = blockIdx.x % (unsigned)pv.n_kv, s = blockIdx.x / (unsigned)pv.n_kv, t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -619,48 +619,58 @@ __global__ void __launch_bounds__(EVICT_THREADS) paged_evict_select_kernel(Evict
         return;
     }
     const int lo = a.first, hi = n - a.recent, want = a.keep - a.first - a.recent;
+    constexpr unsigned STAYS = ~0u;                          // (no mass is that)
     const unsigned zero = order_of(0.f);
+    auto number = [&](int i) { return i >= lo && i < hi ? order_of(mass[i]) : STAYS; };
     if constexpr (HELD) {
-#pragma unroll 8
-        for (int i = t; i < n; i += EVICT_THREADS) held[i] = mass[i];
+        for (int i0 = t; i0 < n; i0 += 8 * EVICT_THREADS) {
+            float m[8];
+#pragma unroll
+            for (int u = 0; u < 8; u++) m[u] = mass[min(i0 + u * EVICT_THREADS, n - 1)];
+#pragma unroll
+            for (int u = 0; u < 8; u++) {
+                const int i = i0 + u * EVICT_THREADS;
+                if (i < n) held[i] = i >= lo && i < hi ? order_of(m[u]) : STAYS;
+            }
+        }
         __syncthreads();
-        mass = held;
     }
-    Cut<unsigned> c{~0u, ~0u, 0};                             // (no mass is that: none is taken)
+    auto key_of = [&](int i) { return HELD ? held[i] : number(i); };
+    Cut<unsigned> c{STAYS - 1, ~0u, 0};
     if (want > 0)
         c = cut_keys<EVICT_THREADS, unsigned>([&](auto f) {
-            for (int i0 = lo + wave * 64; i0 < hi; i0 += 4 * EVICT_THREADS) {
+            for (int i0 = wave * 64 + lane; i0 - lane < n; i0 += 4 * EVICT_THREADS) {
                 unsigned key[4];
 #pragma unroll
-                for (int u = 0; u < 4; u++) key[u] = order_of(mass[min(i0 + u * EVICT_THREADS + lane, hi - 1)]);
+                for (int u = 0; u < 4; u++) key[u] = i0 + u * EVICT_THREADS < n ? key_of(i0 + u * EVICT_THREADS) : STAYS;
                 int zeros = 0;
 #pragma unroll
                 for (int u = 0; u < 4; u++) {
-                    const bool in = i0 + u * EVICT_THREADS + lane < hi;
-                    zeros += __popcll(__ballot(in & (key[u] == zero)));
-                    if (in & (key[u] != zero)) f(key[u], 1);
+                    zeros += __popcll(__ballot(key[u] == zero));
+                    if (key[u] != zero && key[u] != STAYS) f(key[u], 1);
                 }
                 if (lane == 0 && zeros) f(zero, zeros);
             }
         }, want, 32, 0u, cut);
     auto takes = [&](int i, bool *tie) {
-        const bool open = (i >= lo) & (i < hi);
-        const unsigned key = order_of(mass[i]) & c.mask;
-        *tie = open & (key == c.prefix);
-        return !open | (key > c.prefix);
+        const unsigned key = key_of(i);
+        *tie = (key & c.mask) == c.prefix && key != STAYS;
+        return (key & c.mask) > c.prefix || key == STAYS;
     };
-    cut_numbers<EVICT_THREADS>(n, c.want, takes, [&](int place, int i) {
-        kept[place] = i;
-        if (HELD) out[place] = mass[i];
-    }, cut);
-    if constexpr (!HELD)
-        for (int i0 = 0; i0 < a.keep; i0 += EVICT_THREADS) {
-            __syncthreads();
-            const int i = i0 + t;
-            const float m = i < a.keep ? mass[kept[i]] : 0.f;
-            __syncthreads();
-            if (i < a.keep) out[i] = m;
+    cut_numbers<EVICT_THREADS>(n, c.want, takes, [&](int place, int i) { kept[place] = i; }, cut);
+    for (int i0 = 0; i0 < a.keep; i0 += 4 * EVICT_THREADS) {
+        __syncthreads();
+        float m[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const int i = i0 + u * EVICT_THREADS + t;
+            m[u] = i < a.keep ? mass[kept[i]] : 0.f;
         }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 4; u++)
+            if (i0 + u * EVICT_THREADS + t < a.keep) out[i0 + u * EVICT_THREADS + t] = m[u];
+    }
 }
 
 // K and V of the kept positions to their places: 16 bytes a lane, four rows of one key head on their way at once.

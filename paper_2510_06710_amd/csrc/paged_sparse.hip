@@ -73,29 +73,59 @@ __device__ __forceinline__ int page_of_row(const PagedView &pv, int row, int *s)
     return p < 0 ? -1 : p >> pv.page_log;
 }
 
-// A page's bounds are 2 d values of lo and hi, 16 bytes a lane: `lanes` lanes (a power of two, at most 64) hold a page, so a wave's load has 64 / lanes of them, and four loads are on their way at once
+// A page's bounds are 2 d values of lo and hi, 16 bytes a lane: `lanes` lanes (a power of two, at most 64) hold a page, so a wave's load has 64 / lanes of them, and eight loads are on their way at once
 // (an fp32 page of more than 128 dims takes two loads a lane).  The parts of q that a lane multiplies by are the same for all pages.
 // 8 x 2048 pages of 512 bytes: 5 us; 32 ragged rows of up to 1024 pages of 8 heads: 20.  (One wave a page and load, q again for every four pages: 12 and 81.)
+// Sum over 2^lanes_log neighbouring lanes, by lane moves (the value of lane ^ o, in halves).
+template <int CTRL> __device__ __forceinline__ double moved(double v) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const unsigned lo = __builtin_bit_cast(unsigned, vla_dpp<CTRL>(__builtin_bit_cast(float, (unsigned)u))), hi = __builtin_bit_cast(unsigned, vla_dpp<CTRL>(__builtin_bit_cast(float, (unsigned)(u >> 32))));
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+template <int O> __device__ __forceinline__ double paired(double v) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const VlaPair lo = vla_pair<O>(__builtin_bit_cast(float, (unsigned)u)), hi = vla_pair<O>(__builtin_bit_cast(float, (unsigned)(u >> 32)));
+    auto join = [](float h, float l) { return __builtin_bit_cast(double, (unsigned long long)__builtin_bit_cast(unsigned, h) << 32 | __builtin_bit_cast(unsigned, l)); };
+    return join(hi.a, lo.a) + join(hi.b, lo.b);
+}
+__device__ __forceinline__ double lanes_sum(double v, int lanes_log) {
+    if (lanes_log > 0) v += moved<0xb1>(v);                  // quad_perm 1 0 3 2
+    if (lanes_log > 1) v += moved<0x4e>(v);                  // quad_perm 2 3 0 1
+    if (lanes_log > 2) v += moved<0x141>(v);                 // row_half_mirror: lane ^ 7, which has what lane ^ 4 has once fours agree
+    if (lanes_log > 3) v += moved<0x140>(v);                 // row_mirror: lane ^ 15
+    if (lanes_log > 4) v = paired<16>(v);
+    if (lanes_log > 5) v = paired<32>(v);
+    return v;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(256) paged_score_kernel(SelectArgs a, int lanes_log, int per_block) {
-    constexpr int E = 16 / sizeof(T), U = 4, R = sizeof(T) == 4 ? 2 : 1;          // values of a load; pages of a lane at once; loads of a page
+    constexpr int E = 16 / sizeof(T), U = 8, R = sizeof(T) == 4 ? 2 : 1;          // values of a load; pages of a lane at once; loads of a page
     typedef T vec __attribute__((ext_vector_type(E)));
     __shared__ double part[2 * 256];                         // what lo and hi are multiplied by: the group's negative and positive parts of q
     const PagedView &pv = a.pv;
     const int h = blockIdx.x % (unsigned)pv.n_kv, row = blockIdx.x / (unsigned)pv.n_kv, t = threadIdx.x, lanes = 1 << lanes_log;
+    // (the first heads' q on their way while the row's place is looked up)
+    constexpr int AHEAD = 8;
+    const T *qs = (const T *)a.q + row * a.q_stride + (size_t)h * a.group * pv.d + min(t, pv.d - 1);
+    float q[AHEAD];
+#pragma unroll
+    for (int g = 0; g < AHEAD; g++) q[g] = (float)qs[(size_t)min(g, a.group - 1) * pv.d];
     int s;
     const int last = page_of_row(pv, row, &s), n0 = blockIdx.y * per_block, n1 = min(n0 + per_block, last + 1);
     if (n0 >= n1) return;
-    for (int e = t; e < pv.d; e += 256) {
-        const T *q = (const T *)a.q + row * a.q_stride + (size_t)h * a.group * pv.d + e;
+    if (t < pv.d) {
         double up = 0.0, down = 0.0;
-        for (int g = 0; g < a.group; g++) {
-            const double x = (double)(float)q[(size_t)g * pv.d];
+        auto add = [&](double x) {
             up += x > 0.0 ? x : 0.0;
             down += x > 0.0 ? 0.0 : x;
-        }
-        part[e] = down;
-        part[pv.d + e] = up;
+        };
+#pragma unroll
+        for (int g = 0; g < AHEAD; g++)
+            if (g < a.group) add((double)q[g]);
+        for (int g = AHEAD; g < a.group; g++) add((double)(float)qs[(size_t)g * pv.d]);
+        part[t] = down;
+        part[pv.d + t] = up;
     }
     __syncthreads();
     const int lane = t & (lanes - 1), chunks = 2 * pv.d / E;
@@ -107,11 +137,14 @@ __global__ void __launch_bounds__(256) paged_score_kernel(SelectArgs a, int lane
     const int32_t *table = pv.table + (size_t)s * pv.table_stride;
     unsigned long long *keys = a.keys + ((size_t)row * pv.n_kv + h) * a.pages;
     const int step = 256 >> lanes_log;                       // pages of one load of the workgroup
-    for (int p0 = n0 + (t >> lanes_log); __any(p0 < n1); p0 += U * step) {
-        int page[U];
-        vec b[U][R];
+    int page[U];
+    auto look = [&](int p0) {
 #pragma unroll
         for (int u = 0; u < U; u++) page[u] = p0 + u * step < n1 ? table[p0 + u * step] : -1;
+    };
+    look(n0 + (t >> lanes_log));
+    for (int p0 = n0 + (t >> lanes_log); __any(p0 < n1); p0 += U * step) {
+        vec b[U][R];
 #pragma unroll
         for (int u = 0; u < U; u++)
 #pragma unroll
@@ -121,6 +154,7 @@ __global__ void __launch_bounds__(256) paged_score_kernel(SelectArgs a, int lane
                 else
 #pragma unroll
                     for (int e = 0; e < E; e++) b[u][r][e] = (T)0.f;          // (a page that is not there: zeros)
+        look(p0 + U * step);                                  // (on their way while the products are formed)
         double x[U];
 #pragma unroll
         for (int u = 0; u < U; u++) {
@@ -131,9 +165,8 @@ __global__ void __launch_bounds__(256) paged_score_kernel(SelectArgs a, int lane
 #pragma unroll
                     for (int e = 0; e < E; e++) x[u] = __builtin_fma((double)(float)b[u][r][e], w[r][e], x[u]);
         }
-        for (int o = lanes >> 1; o > 0; o >>= 1)
 #pragma unroll
-            for (int u = 0; u < U; u++) x[u] += __shfl_xor(x[u], o, 64);
+        for (int u = 0; u < U; u++) x[u] = lanes_sum(x[u], lanes_log);
 #pragma unroll
         for (int u = 0; u < U; u++)
             if (lane == 0 && p0 + u * step < n1) keys[p0 + u * step] = order_of(x[u]);
@@ -149,6 +182,12 @@ __global__ void __launch_bounds__(256) paged_select_kernel(SelectArgs a) {
     unsigned long long *key = (unsigned long long *)lds;
     const PagedView &pv = a.pv;
     const int h = blockIdx.x % (unsigned)pv.n_kv, row = blockIdx.x / (unsigned)pv.n_kv, t = threadIdx.x;
+    const unsigned long long *src = a.keys + ((size_t)row * pv.n_kv + h) * a.pages;
+    constexpr int AHEAD = 8;                                 // of a lane, on their way while the row's place is looked up
+    unsigned long long held[AHEAD];
+    if (a.pages > a.n_select)
+#pragma unroll
+        for (int u = 0; u < AHEAD; u++) held[u] = src[min(t + u * 256, a.pages - 1)];
     int s;
     const int last = page_of_row(pv, row, &s), n = last + 1;
     if (last < -1) return;
@@ -158,17 +197,18 @@ __global__ void __launch_bounds__(256) paged_select_kernel(SelectArgs a) {
         return;
     }
     const int lo = a.first, hi = n - a.recent, want = a.n_select - a.first - a.recent;
-    const unsigned long long *src = a.keys + ((size_t)row * pv.n_kv + h) * a.pages;
     Cut<unsigned long long> c{~0ull, ~0ull, 0};              // (no key is that: none is taken)
     if (want > 0) {
-        const unsigned long long one = src[lo];
         unsigned long long x = 0;
-#pragma unroll 8
-        for (int i = lo + t; i < hi; i += 256) {
-            const unsigned long long k = src[i];
+        const unsigned long long one = src[lo];
+        auto hold = [&](int i, unsigned long long k) {
+            if (i < lo || i >= hi) return;
             key[i] = k;
             x |= k ^ one;
-        }
+        };
+#pragma unroll
+        for (int u = 0; u < AHEAD; u++) hold(t + u * 256, held[u]);
+        for (int i = t + AHEAD * 256; i < hi; i += 256) hold(i, src[i]);
         for (int o = 32; o > 0; o >>= 1) x |= __shfl_xor(x, o, 64);
         if ((t & 63) == 0) differ[t >> 6] = x;
         __syncthreads();
@@ -206,17 +246,19 @@ __global__ void __launch_bounds__(64) paged_sparse_kernel(SparseArgs x) {
     const int lane = threadIdx.x, part = blockIdx.y;
     const unsigned id = blockIdx.x / (unsigned)pv.n_kv;
     const int kvh = blockIdx.x % (unsigned)pv.n_kv, ht = id % (unsigned)x.heads_tiles, row = id / (unsigned)x.heads_tiles;
+    const int32_t *list = x.selected + ((size_t)row * pv.n_kv + kvh) * x.n_select;
+    const int entry = list[min(lane, x.n_select - 1)];       // (on its way while the row's place is looked up)
     const int s = paged_seq_of_row(pv, row);
     if (s >= pv.n_seq) return;
     const PagedSeq sq = paged_seq(pv, s);
     const int i = row - sq.r0;
     if (i < 0 || i >= sq.rows) return;
     const int p = min(sq.len - sq.n + i, sq.keys - 1);       // the last position it sees
-    const int32_t *list = x.selected + ((size_t)row * pv.n_kv + kvh) * x.n_select, *table = pv.table + (size_t)s * pv.table_stride;
+    const int32_t *table = pv.table + (size_t)s * pv.table_stride;
     int m = 0;                                               // entries before the first negative one
     for (; m < x.n_select; m += 64) {
         const int e = m + lane;
-        const unsigned long long ends = __ballot(e >= x.n_select || list[e] < 0);
+        const unsigned long long ends = __ballot(e >= x.n_select || (m == 0 ? entry : list[min(e, x.n_select - 1)]) < 0);
         if (ends) { m += __builtin_ctzll(ends); break; }
     }
     m = __builtin_amdgcn_readfirstlane(min(m, x.n_select));
@@ -432,7 +474,7 @@ int vla_paged_select(const vla_paged_cache *cache, const vla_paged_batch *batch,
         const int chunks = 2 * pv.d * (f32 ? 4 : 2) / 16;
         int lanes_log = 0;
         while (lanes_log < 6 && (1 << lanes_log) < chunks) lanes_log++;
-        const int step = 4 * (256 >> lanes_log);
+        const int step = 8 * (256 >> lanes_log);
         int y = (2048 + items - 1) / items;
         if (y > (a.pages + step - 1) / step) y = (a.pages + step - 1) / step;
         const int per_block = ((a.pages + y - 1) / y + step - 1) / step * step;
