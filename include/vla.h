@@ -431,7 +431,7 @@ int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, 
  *   [n_seq, max_rows] out: the rows of the path, then -1; n_accepted [n_seq] out: how many; next [n_seq] out or NULL: what the last of
  *   them chose (-1 without rows); new_len [n_seq] out or NULL: kv_len - n_s + n_accepted.  In each of n_layers layers, layer l at
  *   cache->k, v + l * layer_stride elements, K and V of row path[i] move to position kv_len - n_s + i (n_layers may be 0: nothing moves).  The rows behind
- *   new_len keep what they hold.  The pages of the new rows belong to their sequence alone.  Without rows, or where rows lie at negative positions, new_len is not below 0.
+ *   new_len keep what they hold.  No output overlaps parent, ids, chosen, kv_len or row_start.  The pages of the new rows belong to their sequence alone.  Rows at negative positions are nowhere, and new_len is not below 0.
  *
  * Sparse attention over pages.
  * vla_paged_bounds: bounds, DEVICE cache's dtype [n_pages][n_kv_heads][2][head_dim], 16-byte aligned: the least and the largest K of each dim over the
@@ -455,7 +455,7 @@ int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, 
  *   mass (ties: lowest position first; NaN comes last); all where there are no more.  kept [n_seq][n_kv_heads][keep] out: positions,
  *   ascending, then -1.  K, V and mass of the i-th go to position i: K and V in page to_table[sequence][i / page_size] (to_stride entries per
  *   sequence, at least keep / page_size rounded up), mass to mass_out [n_seq][n_kv_heads][mass_out_stride] (mass itself with its stride, or apart
- *   from it; entries behind the last keep what they hold).  new_len [n_seq] out or NULL: min(kv_len, keep).  to_table's pages hold nothing that the call reads, but that a sequence
+ *   from it; entries behind the last keep what they hold).  new_len [n_seq] out or NULL: min(kv_len, keep), apart from kv_len.  to_table's pages hold nothing that the call reads, but that a sequence
  *   with no more than `keep` may name its own pages again (nothing moves).  One layer a call.  Of the batch it uses the sequences, not their rows. */
 /* vla_forward_paged_rows: vla_forward_paged with these, and with the logits of every row (a tree's nodes are all read).
  *   position, seen (words to a row), prefix_len: as above, each or NULL; bounds: [n_layers] of vla_paged_bounds' arrays or NULL: kept up with the

@@ -12,6 +12,10 @@ struct PagedView {
 
 // Host: 0 or an error code with the message set.  `what` names the entry point.
 int vla_check_paged(const char *what, const vla_paged_cache *cache, const vla_paged_batch *batch, PagedView *out);
+// Whether two arrays share a byte (NULL: no).
+inline bool paged_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
+    return a && b && (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
 
 // Rows of a ragged batch as the decoder takes and gives them (vla_forward_paged).
 template <typename T>

@@ -54,7 +54,7 @@ __device__ __forceinline__ float tile_weight(const AttnArgs &a, const f32x16_t &
         }
         float w = __builtin_amdgcn_exp2f(__builtin_fmaf(z, unit, -l[i]));
         if (MASKED) {                                         // (p - key below 0, or beyond the window: as one comparison without sign)
-            const bool see = (((unsigned)(p[i] - key) < (unsigned)window) | (key < prefix)) & (key < keys) & (l[i] != -INFINITY);
+            const bool see = (((unsigned)(p[i] - key) < (unsigned)window) | (key < prefix)) & (key < keys) & (l[i] != INFINITY);
             w = see ? w : 0.f;
         }
         sum[i % 4] = i < 4 ? w : sum[i % 4] + w;
@@ -489,7 +489,7 @@ int weight_keys(int d, bool f32) { return 128 * (padded_dim(d) * (f32 ? 4 : 2) <
 WeightPlan plan_weights(const AttnArgs &a, bool f32) {
     WeightPlan p{};
     const PagedView &pv = a.pv;
-    const long pairs = (long)pv.n_kv * pv.n_seq, packed = (long)pv.max_rows * a.group;
+    const long pairs = (long)pv.n_kv * pv.n_seq, packed = (long)(pv.max_rows < pv.n_rows ? pv.max_rows : pv.n_rows) * a.group;
     p.step = packed <= 32;
     p.parts = 1;
     if (p.step) {
@@ -762,6 +762,14 @@ int vla_paged_evict(const vla_paged_cache *cache, const vla_paged_batch *batch, 
     }
     const long pairs = (long)batch->n_seq * cache->n_kv_heads;
     if (pairs > 65535) { vla_set_error("paged_evict: %ld sequences times key heads (at most 65,535): split the batch", pairs); return VLA_ESHAPE; }
+    const int row_bytes = cache->head_dim * (cache->dtype == VLA_DTYPE_F32 ? 4 : 2), chunks = row_bytes / 16, per = 256 / chunks * 4;
+    if ((least + per - 1) / per > 0x7fffffff / 256) { vla_set_error("paged_evict: keep %d is too many", keep); return VLA_ESHAPE; }
+    // every workgroup of a sequence reads kv_len while the first writes new_len
+    if (paged_overlap(new_len, (size_t)batch->n_seq * 4, batch->kv_len, (size_t)batch->n_seq * 4) ||
+        (mass != mass_out && paged_overlap(mass, pairs * mass_stride * 4, mass_out, pairs * mass_out_stride * 4))) {
+        vla_set_error("paged_evict: new_len overlaps kv_len, or mass_out a part of mass");
+        return VLA_EINVAL;
+    }
     a.mass = mass; a.mass_out = mass_out; a.mass_stride = mass_stride; a.out_stride = mass_out_stride;
     a.keep = keep; a.first = first; a.recent = recent; a.to_table = to_table; a.to_stride = to_stride; a.kept = kept; a.new_len = new_len;
     hipStream_t st = (hipStream_t)stream;
@@ -772,7 +780,6 @@ int vla_paged_evict(const vla_paged_cache *cache, const vla_paged_batch *batch, 
     } else paged_evict_select_kernel<false><<<(unsigned)pairs, EVICT_THREADS, 0, st>>>(a);
     if (int rc = vla_check_launch("paged_evict")) return rc;
     if (least == 0) return VLA_OK;
-    const int row_bytes = cache->head_dim * (cache->dtype == VLA_DTYPE_F32 ? 4 : 2), chunks = row_bytes / 16, per = 256 / chunks * 4;
     paged_evict_move_kernel<4><<<dim3((least + per - 1) / per, (unsigned)pairs), 256, 0, st>>>(a, chunks, row_bytes);
     return vla_check_launch("paged_evict move");
 }

@@ -81,12 +81,12 @@ __global__ void __launch_bounds__(256) paged_accept_kernel(AcceptArgs a) {
     }
     int first = 0;                                            // rows before it stay where they are
     while (first < n && path[first] == first) first++;
-    if (first == n || base + first < 0) return;
+    if (first == n) return;
     // where the rows that move are, and go: bytes within a key head's pages; below 0: nowhere
     const int32_t *table = pv.table + (size_t)s * pv.table_stride;
     const int row_bytes = pv.d * a.es, chunks = row_bytes / 16;
     auto at = [&](int pos) -> long {
-        if (pos >= pv.max_len) return -1;
+        if (pos < 0 || pos >= pv.max_len) return -1;
         const int page = table[pos >> pv.page_log];
         if ((unsigned)page >= (unsigned)pv.n_pages) return -1;
         return (((long)page * pv.n_kv << pv.page_log) + (pos & ((1 << pv.page_log) - 1))) * row_bytes;
@@ -149,10 +149,18 @@ int vla_paged_accept(const vla_paged_cache *cache, int n_layers, size_t layer_st
     const size_t layer = (size_t)cache->n_pages * cache->n_kv_heads * cache->page_size * cache->head_dim;
     a.es = cache->dtype == VLA_DTYPE_F32 ? 4 : 2;
     if (n_layers < 0 || n_layers > 65536) { vla_set_error("paged_accept: n_layers %d unsupported (0 .. 65,536)", n_layers); return VLA_EINVAL; }
+    if ((long)n_layers * cache->n_kv_heads > 1 << 20) { vla_set_error("paged_accept: %d layers of %d key heads are too many", n_layers, cache->n_kv_heads); return VLA_ESHAPE; }
     if (n_layers > 1 && layer_stride < layer) { vla_set_error("paged_accept: layer stride of %zu elements, a layer has %zu", layer_stride, layer); return VLA_ESHAPE; }
     if (n_layers > 1 && layer_stride * a.es % 16) { vla_set_error("paged_accept: the layers are not 16-byte aligned"); return VLA_EINVAL; }
     if (!n_accepted || (batch->max_rows > 0 && !path)) { vla_set_error("paged_accept: path or n_accepted is NULL"); return VLA_EINVAL; }
     if (batch->n_rows > 0 && (!parent || !ids || !chosen)) { vla_set_error("paged_accept: parent, ids or chosen is NULL"); return VLA_EINVAL; }
+    // every workgroup of a sequence reads these while the first writes
+    const size_t rows = (size_t)batch->n_rows * 4, seqs = (size_t)batch->n_seq * 4;
+    const struct { const void *at; size_t bytes; } in[] = {{parent, rows}, {ids, rows}, {chosen, rows}, {batch->kv_len, seqs}, {batch->row_start, seqs + 4}},
+                                                   out[] = {{path, seqs * batch->max_rows}, {n_accepted, seqs}, {next, seqs}, {new_len, seqs}};
+    for (auto &x : in)
+        for (auto &y : out)
+            if (paged_overlap(x.at, x.bytes, y.at, y.bytes)) { vla_set_error("paged_accept: an output overlaps an input"); return VLA_EINVAL; }
     a.layer_bytes = layer_stride * a.es;
     a.parent = parent; a.ids = ids; a.chosen = chosen; a.path = path; a.n_accepted = n_accepted; a.next = next; a.new_len = new_len;
     a.units = 2 * n_layers * a.pv.n_kv;

@@ -207,3 +207,19 @@ def test_evict_bad_pages_and_bounds():
     lens = torch.zeros(2, dtype=torch.int32, device=DEV)
     vb.vla_paged_evict(vb.make_paged_cache(k, v), b.on_device(), masses.to(DEV), 0, 4, to_device(to_table), kept, out, lens)
     assert lens.tolist() == [32, 32] and kept[:, 0].max().item() == 63 and kept[:, 0, -4:].tolist() == [[60, 61, 62, 63]] * 2
+
+
+@BOTH
+@pytest.mark.parametrize("n,length", [(2, 90), (40, 150)])
+def test_rows_left_out_read_no_scores(dtype, n, length):
+    """A row whose lse is -inf adds nothing, also where K is NaN or its scores are infinite."""
+    b = Batch([(n, length)], 16)
+    pools = [p.to(DEV) for p in pools_of(b, dtype, 2, 64, 3)]
+    pools[0][:, :, 3] = float("nan")
+    pools[0][:, :, 5] = float("inf")
+    q = torch.randn(b.n_rows, 4, 64, generator=torch.Generator().manual_seed(1)).to(TYPES[dtype]).to(DEV)
+    cache, batch, mask = vb.make_paged_cache(*pools), b.on_device(), vb.make_paged_mask(0.125)
+    old = torch.rand(1, 2, length, generator=torch.Generator().manual_seed(2)).to(DEV)
+    mass, ws = old.clone(), torch.empty(vb.vla_paged_weights_workspace_bytes(cache, batch, mask, 4), dtype=torch.uint8, device=DEV)
+    vb.vla_paged_weights(cache, batch, mask, q, torch.full((n, 4), -float("inf"), device=DEV), mass, ws)
+    assert torch.equal(mass[..., :length - n], old[..., :length - n]) and not mass[..., length - n:].any()

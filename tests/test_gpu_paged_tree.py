@@ -175,6 +175,7 @@ def test_accept_moves_nothing_without_layers_or_pages():
     b.spec[0] = (4, 2)                                        # rows at negative positions
     new_len = count.clone()
     vb.vla_paged_accept(vb.make_paged_cache(k, k), 1, 0, b.on_device(), *args, path, count, None, new_len)
+    before[b.table[0, 0], :, 0] = before[b.table[0, 0], :, 1]          # path[2] = 3 lies at 1 and goes to 0; path[1] would go to -1
     assert torch.equal(k, before) and new_len.tolist() == [1, 0]
 
 
@@ -206,3 +207,20 @@ def test_rotation_by_given_positions(dtype, interleaved):
             assert (np.abs(rows - want[:b.live]) <= (mag * 4 * 2.0 ** -24 + (np.abs(want) * 2.0 ** -8 if dtype == "bf16" else 0))[:b.live]).all()
         got.append((out, *pools))
     assert all(torch.equal(x, y) for x, y in zip(got[0], got[1]))
+
+
+def test_accept_where_rows_lie_before_the_cache():
+    """More rows than positions: rows at negative positions are nowhere, those behind them move as always."""
+    b = Batch([(6, 4)], 16)
+    k = torch.randn(b.n_pages, 2, 16, 16, generator=torch.Generator().manual_seed(1))
+    v, kd = 2 * k, k.to(DEV)
+    vd = v.to(DEV)
+    path, count = torch.zeros(1, 6, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    new_len = torch.zeros(1, dtype=torch.int32, device=DEV)
+    args = [to_device(np.array(x, np.int32)) for x in ([-1, 0, 0, 2, 3, 4], [0, 5, 6, 7, 8, 9], [6, 1, 7, 8, 9, 1])]
+    vb.vla_paged_accept(vb.make_paged_cache(kd, vd), 1, 0, b.on_device(), *args, path, count, None, new_len)
+    assert path.tolist() == [[0, 2, 3, 4, 5, -1]] and count.item() == 5 and new_len.item() == 3
+    for pool, got in ((k, kd), (v, vd)):
+        page = b.table[0, 0]
+        pool[page, :, 0:3] = pool[page, :, 1:4].clone()      # row path[i] is at path[i] - 2 and goes to i - 2
+        assert torch.equal(got.cpu(), pool)

@@ -153,3 +153,22 @@ def test_binding_refuses():
             with pytest.raises(vb.VlaError) as e:
                 f(**k)
             assert "not all on" not in str(e.value), (name, k)
+
+
+def test_outputs_that_overlap_inputs():
+    """Workgroups that read an input while another writes it."""
+    far = dict(path=P + 0x2000, count=P + 0x3000)
+    for k in (dict(far, count=P), dict(far, path=P + 16), dict(far, path=P - 8)):
+        assert call("accept", **k) == E and b"overlaps" in vb.lib().vla_last_error(), k
+    c, b = cache(), batch()
+    at, L = C.byref, vb.lib()
+    for lens in (b.kv_len, b.row_start + 4):
+        assert L.vla_paged_accept(at(c), 1, 0, at(b), P + 0x4000, P + 0x5000, P + 0x6000, P + 0x2000, P + 0x3000, None, lens, None) == E
+    assert L.vla_paged_evict(at(c), at(b), P, 64, 32, 1, 1, P + 0x4000, 2, P + 0x5000, P + 0x100000, 32, b.kv_len, None) == E and b"overlaps" in L.vla_last_error()
+    assert call("evict", mo=P + 4) == E and call("evict", mo=P - 4) == E
+
+
+def test_too_many_layers_or_positions():
+    assert call("accept", c=cache(n_kv_heads=1024, head_dim=16), layers=1025) == S
+    most = batch(max_len=1 << 30, table_stride=1 << 26)
+    assert call("evict", c=cache(head_dim=256, dtype=vb.VLA_DTYPE_F32), b=most, ms=1 << 30, keep=1 << 30, ts=1 << 26, mos=1 << 30) == S
