@@ -595,9 +595,12 @@ __device__ __forceinline__ unsigned order_of(float x) {
     return u >> 31 ? ~u : u | 1u << 31;
 }
 
-// A workgroup for each (sequence, key head): the least mass that stays, then the positions of what is above it and of the first that equal it, in order, then their masses, a thousand at a time, read
+// A workgroup for each (sequence, key head): the least mass that stays, then the positions of what is above it and of the first that equal it, in order, then their masses, 8192 at a time, read
 // before they are written: none lands behind its place, so mass_out may be mass.  Up to 32,768 positions' masses are held in LDS as the numbers they are ordered by (HELD); of more every pass reads
 // them again.  The first and last that stay anyway have the largest number.  Positions without weight, many of a kind, are counted by ballot: as one bin they would be added to one after the other.
+// Bound by the vector instructions of one CU, some fifteen a position and pass: 128 lists of up to 32,768 cut to 4096 take 32 us, of which the masses and the first digit 9.7, the other digits 7 to 10, the
+// positions 8, their masses 3; one of 64,106 cut to 24,377 67 us; one of 1003, 8 us, where every step waits for the one before it.  (Eight loads of a lane on their way, two more comparisons a position and the
+// first digit counted by a pass of its own: 38 us.)
 constexpr int EVICT_THREADS = 1024, EVICT_HELD = 32 * 1024;
 template <bool HELD>
 __global__ void __launch_bounds__(EVICT_THREADS) paged_evict_select_kernel(EvictArgs a) {
@@ -621,59 +624,72 @@ __global__ void __launch_bounds__(EVICT_THREADS) paged_evict_select_kernel(Evict
     const int lo = a.first, hi = n - a.recent, want = a.keep - a.first - a.recent;
     constexpr unsigned STAYS = ~0u;                          // (no mass is that)
     const unsigned zero = order_of(0.f);
-    auto number = [&](int i) { return i >= lo && i < hi ? order_of(mass[i]) : STAYS; };
-    if constexpr (HELD) {
-        for (int i0 = t; i0 < n; i0 += 8 * EVICT_THREADS) {
-            float m[8];
-#pragma unroll
-            for (int u = 0; u < 8; u++) m[u] = mass[min(i0 + u * EVICT_THREADS, n - 1)];
-#pragma unroll
-            for (int u = 0; u < 8; u++) {
-                const int i = i0 + u * EVICT_THREADS;
-                if (i < n) held[i] = i >= lo && i < hi ? order_of(m[u]) : STAYS;
-            }
+    auto number = [&](int i, float m) { return i >= lo && i < hi ? order_of(m) : STAYS; };
+    constexpr int U = 16;                                    // of a lane, on their way at once
+    auto counted = [&](const auto &key, auto f) {
+        int zeros = 0;
+        for (const unsigned k : key) {
+            zeros += __popcll(__ballot(k == zero));
+            if (k != zero && k != STAYS) f(k, 1);
         }
-        __syncthreads();
-    }
-    auto key_of = [&](int i) { return HELD ? held[i] : number(i); };
-    Cut<unsigned> c{STAYS - 1, ~0u, 0};
-    if (want > 0)
-        c = cut_keys<EVICT_THREADS, unsigned>([&](auto f) {
-            for (int i0 = wave * 64 + lane; i0 - lane < n; i0 += 4 * EVICT_THREADS) {
-                unsigned key[4];
-#pragma unroll
-                for (int u = 0; u < 4; u++) key[u] = i0 + u * EVICT_THREADS < n ? key_of(i0 + u * EVICT_THREADS) : STAYS;
-                int zeros = 0;
-#pragma unroll
-                for (int u = 0; u < 4; u++) {
-                    zeros += __popcll(__ballot(key[u] == zero));
-                    if (key[u] != zero && key[u] != STAYS) f(key[u], 1);
-                }
-                if (lane == 0 && zeros) f(zero, zeros);
-            }
-        }, want, 32, 0u, cut);
-    auto takes = [&](int i, bool *tie) {
-        const unsigned key = key_of(i);
-        *tie = (key & c.mask) == c.prefix && key != STAYS;
-        return (key & c.mask) > c.prefix || key == STAYS;
+        if (lane == 0 && zeros) f(zero, zeros);
     };
-    cut_numbers<EVICT_THREADS>(n, c.want, takes, [&](int place, int i) { kept[place] = i; }, cut);
-    for (int i0 = 0; i0 < a.keep; i0 += 4 * EVICT_THREADS) {
-        __syncthreads();
-        float m[4];
+    auto from_memory = [&](auto f) {
+        int i0 = wave * 64 + lane;
+        auto some = [&](auto each) {
+            constexpr int N = decltype(each)::value;
+            float m[N];
+            unsigned key[N];
 #pragma unroll
-        for (int u = 0; u < 4; u++) {
+            for (int u = 0; u < N; u++) m[u] = mass[min(i0 + u * EVICT_THREADS, n - 1)];
+#pragma unroll
+            for (int u = 0; u < N; u++) {
+                const int i = i0 + u * EVICT_THREADS;
+                key[u] = number(i, m[u]);                     // (hi <= n: STAYS behind the last)
+                if (HELD && i < n) held[i] = key[u];
+            }
+            counted(key, f);
+            i0 += N * EVICT_THREADS;
+        };
+        while (i0 - lane + (U - 4) * EVICT_THREADS < n) some(std::integral_constant<int, U>());
+        while (i0 - lane < n) some(std::integral_constant<int, 4>());
+    };
+    Cut<unsigned> c{STAYS - 1, ~0u, 0};
+    for (int i = t; i < CUT_BINS; i += EVICT_THREADS) cut.bins[i] = 0;
+    __syncthreads();
+    from_memory([&](unsigned key, int times) { atomicAdd(&cut.bins[cut_bin(key >> (32 - CUT_BITS))], times); });
+    __syncthreads();
+    if (want > 0)
+        c = cut_keys<EVICT_THREADS, true, unsigned>([&](auto f) {
+            if constexpr (!HELD) from_memory(f);
+            else
+                for (int i0 = wave * 64 + lane; i0 - lane < n; i0 += 4 * EVICT_THREADS) {
+                    unsigned key[4];
+#pragma unroll
+                    for (int u = 0; u < 4; u++) key[u] = i0 + u * EVICT_THREADS < n ? held[i0 + u * EVICT_THREADS] : STAYS;
+                    counted(key, f);
+                }
+        }, want, 32, 0u, cut);
+    auto put = [&](int place, int i) { kept[place] = i; };
+    if constexpr (HELD) cut_numbers<EVICT_THREADS, 8>(n, c, [&](int i) { return held[i]; }, [](int, unsigned key) { return key; }, put, cut);
+    else cut_numbers<EVICT_THREADS, U>(n, c, [&](int i) { return mass[i]; }, number, put, cut);
+    for (int i0 = 0; i0 < a.keep; i0 += 8 * EVICT_THREADS) {
+        __syncthreads();
+        float m[8];
+#pragma unroll
+        for (int u = 0; u < 8; u++) {
             const int i = i0 + u * EVICT_THREADS + t;
             m[u] = i < a.keep ? mass[kept[i]] : 0.f;
         }
         __syncthreads();
 #pragma unroll
-        for (int u = 0; u < 4; u++)
+        for (int u = 0; u < 8; u++)
             if (i0 + u * EVICT_THREADS + t < a.keep) out[i0 + u * EVICT_THREADS + t] = m[u];
     }
 }
 
-// K and V of the kept positions to their places: 16 bytes a lane, four rows of one key head on their way at once.
+// K and V of the kept positions to their places: 16 bytes a lane, four rows of one key head on their way at once.  Bound by memory: 16 x 8 x 4096 rows of 256 bytes (475 MB read and written, rows in any order) in 100 us,
+// the rate of a large copy.
 template <int U>
 __global__ void __launch_bounds__(256) paged_evict_move_kernel(EvictArgs a, int chunks, int row_bytes) {
     const PagedView &pv = a.pv;

@@ -197,33 +197,29 @@ __global__ void __launch_bounds__(256) paged_select_kernel(SelectArgs a) {
         return;
     }
     const int lo = a.first, hi = n - a.recent, want = a.n_select - a.first - a.recent;
-    Cut<unsigned long long> c{~0ull, ~0ull, 0};              // (no key is that: none is taken)
-    if (want > 0) {
+    Cut<unsigned long long> c{~0ull - 1, ~0ull, 0};          // (no score is that: what stays anyway alone is taken)
+    {
         unsigned long long x = 0;
         const unsigned long long one = src[lo];
         auto hold = [&](int i, unsigned long long k) {
-            if (i < lo || i >= hi) return;
-            key[i] = k;
-            x |= k ^ one;
+            if (i >= n) return;
+            const bool open = i >= lo && i < hi;
+            key[i] = open ? k : ~0ull;
+            if (open) x |= k ^ one;
         };
 #pragma unroll
         for (int u = 0; u < AHEAD; u++) hold(t + u * 256, held[u]);
-        for (int i = t + AHEAD * 256; i < hi; i += 256) hold(i, src[i]);
+        for (int i = t + AHEAD * 256; i < n; i += 256) hold(i, src[i]);
         for (int o = 32; o > 0; o >>= 1) x |= __shfl_xor(x, o, 64);
         if ((t & 63) == 0) differ[t >> 6] = x;
         __syncthreads();
         x = differ[0] | differ[1] | differ[2] | differ[3];
-        c = cut_keys<256, unsigned long long>([&](auto f) {
-            for (int i = lo + t; i < hi; i += 256) f(key[i], 1);
-        }, want, x ? 64 - __builtin_clzll(x) : 0, one, cut);
+        if (want > 0)
+            c = cut_keys<256, false, unsigned long long>([&](auto f) {
+                for (int i = lo + t; i < hi; i += 256) f(key[i], 1);
+            }, want, x ? 64 - __builtin_clzll(x) : 0, one, cut);
     }
-    auto takes = [&](int i, bool *tie) {
-        const bool open = i >= lo && i < hi;
-        const unsigned long long k = open ? key[i] & c.mask : 0ull;
-        *tie = open && k == c.prefix && c.want > 0;
-        return !open || k > c.prefix;
-    };
-    cut_numbers<256>(n, c.want, takes, [&](int place, int i) { out[place] = i; }, cut);
+    cut_numbers<256, 8>(n, c, [&](int i) { return key[i]; }, [](int, unsigned long long k) { return k; }, [&](int place, int i) { out[place] = i; }, cut);
 }
 
 // ---- attention over the selected pages ----------------------------------------------------------------------------------------
