@@ -18,6 +18,10 @@
 // bf16 tail (2^-16 of the weight is lost, as in attn_mfma.hip): the step waits for memory, and is 1 % longer (behind a shared prefix 8 %).  A prompt's are rounded to
 // bf16 once (2^-8 of each, as the tolerances count it), for the third product would take 8192 rows from 550 to 745 us: outputs are off by 1.4 times what their own rounding
 // costs (rms 0.0023 of them for 0.0017).  The sum that divides is that of the fp32 weights.
+//
+// Drafted trees (TREE) differ in what is seen alone: all below the sequence's new rows, and of these the ones whose bits are set, a word or two of them for a tile of 32 keys.  Their weights keep
+// the tail in both forms.  8 nodes behind 700 positions, 32 heads, 11.5 us and 4.3 for the join; 61 behind 32,768, 16 heads, capped, 44 and 8.5; 32 sequences of up to 24 nodes behind up to 4096,
+// 280 MB, 91 and 7, where the longest sequence's workgroups end 45 us behind the average.
 #include "paged_rows.h"
 
 namespace {
