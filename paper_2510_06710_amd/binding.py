@@ -594,11 +594,18 @@ def vla_paged_tree_attention(cache, batch, mask, seen, q, out, lse=None, ws=None
                                           _stream(stream)))
 
 
+def _in_pools(what, cache, n_layers, layer_stride):
+    for pool in cache.keep if n_layers > 1 else ():
+        if (pool.storage_offset() + (n_layers - 1) * layer_stride + pool.numel()) * pool.element_size() > pool.untyped_storage().nbytes():
+            raise VlaError(VLA_ESHAPE, f"{what}: {n_layers} layers {layer_stride} elements apart reach beyond the pools")
+
+
 def vla_paged_accept(cache, n_layers: int, layer_stride: int, batch, parent, ids, chosen, path, n_accepted, next=None, new_len=None, stream=None) -> None:
     """``parent``, ``ids``, ``chosen`` int32 [n_rows]; ``path`` int32 [n_seq, max_rows] out; ``n_accepted``, ``next``, ``new_len`` int32 [n_seq] out."""
     rows, n = batch.n_rows, batch.n_seq
     arrays = (_ints(parent, "parent", rows), _ints(ids, "ids", rows), _ints(chosen, "chosen", rows), _ints(path, "path", n, batch.max_rows),
               _ints(n_accepted, "n_accepted", n), _ints(next, "next", n), _ints(new_len, "new_len", n))
+    _in_pools("paged_accept", cache, n_layers, layer_stride)
     _on_current_device("paged_accept", (cache, batch), (n_accepted, parent, ids, chosen, path, next, new_len))
     _check(lib().vla_paged_accept(C.byref(cache), n_layers, layer_stride, C.byref(batch), *arrays, _stream(stream)))
 
@@ -715,6 +722,7 @@ def vla_forward_paged_rows(model, cache, layer_stride: int, n_layers: int, batch
             raise VlaError(VLA_ESHAPE, f"forward_paged_rows: bounds is {bounds.dtype} {list(bounds.shape)}, wanted [{n_layers}, {cache.n_pages}, {cache.n_kv_heads}, 2, {cache.head_dim}] of the cache's type")
         if mass is not None and mass.shape[:3] != (n_layers, batch.n_seq, cache.n_kv_heads):
             raise VlaError(VLA_ESHAPE, f"forward_paged_rows: mass is {list(mass.shape)}, wanted [{n_layers}, {batch.n_seq}, {cache.n_kv_heads}, positions]")
+    _in_pools("forward_paged_rows", cache, n_layers, layer_stride)
     arrays = _ints(ids, "ids", n), _want(logits, "float32", "logits", (n, VLA_N_BINS))
     _on_current_device("forward_paged_rows", (cache, batch, rows), (ids, patch, ws, logits))
     _check(lib().vla_forward_paged_rows(model, C.byref(cache), layer_stride, C.byref(batch), C.byref(rows), arrays[0], _ptr(patch), 0 if patch is None else patch.shape[0], shared_len,

@@ -223,3 +223,12 @@ def test_rows_left_out_read_no_scores(dtype, n, length):
     mass, ws = old.clone(), torch.empty(vb.vla_paged_weights_workspace_bytes(cache, batch, mask, 4), dtype=torch.uint8, device=DEV)
     vb.vla_paged_weights(cache, batch, mask, q, torch.full((n, 4), -float("inf"), device=DEV), mass, ws)
     assert torch.equal(mass[..., :length - n], old[..., :length - n]) and not mass[..., length - n:].any()
+
+
+@BOTH
+@pytest.mark.parametrize("n_seq", [70, 300, 2049])
+def test_weights_of_many_sequences(dtype, n_seq):
+    """Equal shares found behind the first 64 sequences; above 2048 of them, chunks of each."""
+    weigh(Batch([(1 if i % 5 else 0, 1 + 37 * i % (300 if n_seq < 100 else 70)) for i in range(n_seq)], 16, padding=3), dtype, 2, 1, 32)
+    if n_seq == 2049:
+        weigh(Batch([(1, 700)] + [(1, 3)] * 2048, 16), dtype, 1, 1, 16)

@@ -224,3 +224,10 @@ def test_accept_where_rows_lie_before_the_cache():
         page = b.table[0, 0]
         pool[page, :, 0:3] = pool[page, :, 1:4].clone()      # row path[i] is at path[i] - 2 and goes to i - 2
         assert torch.equal(got.cpu(), pool)
+
+
+@BOTH
+def test_attention_of_many_sequences(dtype):
+    for n_seq, rows in ((70, 5), (300, 2), (2049, 1)):
+        b = Batch([((i + 1) % (rows + 1), rows + 37 * i % (200 if n_seq < 100 else 40)) for i in range(n_seq)], 16, padding=2)
+        attend(b, dtype, 2, 1, 32, [ancestors(t)[0] if t else [] for t in trees(b, 5)])

@@ -172,3 +172,16 @@ def test_too_many_layers_or_positions():
     assert call("accept", c=cache(n_kv_heads=1024, head_dim=16), layers=1025) == S
     most = batch(max_len=1 << 30, table_stride=1 << 26)
     assert call("evict", c=cache(head_dim=256, dtype=vb.VLA_DTYPE_F32), b=most, ms=1 << 30, keep=1 << 30, ts=1 << 26, mos=1 << 30) == S
+
+
+def test_binding_refuses_layers_beyond_the_pools():
+    pools = [z(3, 8, 2, 16, 64) for _ in range(2)]
+    b = vb.make_paged_batch(z(3, dtype=I), z(2, dtype=I), z(2, 3, dtype=I), 5, 3, 40)
+    row, each = z(5, dtype=I), pools[0][0].numel()
+    call = lambda first, n, stride: vb.vla_paged_accept(vb.make_paged_cache(pools[0][first], pools[1][first]), n, stride, b, row, row, row, z(2, 3, dtype=I), z(2, dtype=I))
+    for first, n, stride in ((0, 4, each), (1, 3, each), (0, 3, 2 * each)):
+        with pytest.raises(vb.VlaError, match="beyond the pools"):
+            call(first, n, stride)
+    for first, n, stride in ((0, 3, each), (1, 2, each), (0, 2, 2 * each), (2, 1, 0)):
+        with pytest.raises(vb.VlaError, match="not all on the current GPU"):
+            call(first, n, stride)
