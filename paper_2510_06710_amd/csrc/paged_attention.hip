@@ -76,6 +76,7 @@ __device__ __forceinline__ Query find_query(const AttnArgs &a, const Item &it, i
     const int at = i - sq.r0;
     Query q = make_query<MODE>(a, it.kvh, lo, i, at, sq, hg, at >= 0 && at < sq.rows);
     if (q.valid) { q.hi = min(q.hi, a.shared_len); q.pre = min(q.pre, a.shared_len); }
+    if constexpr (MODE & TREE) q.words = 0;                  // (no new row lies there: what a tile of 32 holds behind an odd multiple of 16 is the prefix's last key again)
     return q;
 }
 
