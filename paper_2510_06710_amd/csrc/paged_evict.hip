@@ -26,7 +26,7 @@ __device__ __forceinline__ int prefix_of(const AttnArgs &a, int s, const PagedSe
 __device__ __forceinline__ RowTiles row_tiles(const AttnArgs &a, const PagedSeq &sq, int prefix, int key0, int n) {
     const int base = sq.len - sq.n;
     int i0 = max(0, key0 - base), i1 = sq.rows;
-    if (a.window) i1 = min(i1, max(0, key0 + n - 1 + a.window - base));
+    if (a.window) i1 = (int)min((long)i1, max(0L, (long)key0 + n - 1 + a.window - base));
     if (key0 < prefix) { i0 = 0; i1 = sq.rows; }
     if (i0 >= i1) return {0, 0};
     return {i0 * a.group / 32, (i1 * a.group + 31) / 32};
@@ -535,7 +535,7 @@ int check_weights(const vla_paged_cache *cache, const vla_paged_batch *batch, co
     if (mask->window < 0) { vla_set_error("%s: window must not be negative", what); return VLA_EINVAL; }
     if ((long)batch->n_rows * n_heads > 0x7fffffffL / 2) { vla_set_error("%s: %d rows of %d heads are too many", what, batch->n_rows, n_heads); return VLA_ESHAPE; }
     a->n_heads = n_heads; a->group = n_heads / cache->n_kv_heads;
-    a->scale = mask->scale; a->cap = mask->softcap; a->slopes = mask->slopes; a->prefix_len = mask->prefix_len; a->window = mask->window;
+    a->scale = mask->scale; a->cap = mask->softcap; a->slopes = mask->slopes; a->prefix_len = mask->prefix_len; a->window = mask_window(*mask);
     const long items = plan_weights(*a, cache->dtype == VLA_DTYPE_F32).items, joins = (long)cache->n_kv_heads * batch->n_seq * ((batch->max_len + 255) / 256);
     if (items > 0x7fffffffL / 256 || joins > 0x7fffffffL / 256) { vla_set_error("%s: %ld tiles of positions are too many: split the batch", what, items); return VLA_ESHAPE; }
     return VLA_OK;

@@ -7,6 +7,8 @@
 
 namespace {
 
+// A window that reaches before every position (there are 2^30 at most) is one of 2^30: positions less a window, rows at negative ones among them, stay numbers of 32 bits.
+int mask_window(const vla_paged_mask &mask) { return mask.window < 1 << 30 ? mask.window : 1 << 30; }
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 
