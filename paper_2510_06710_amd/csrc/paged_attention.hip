@@ -377,7 +377,7 @@ int check(const vla_paged_cache *cache, const vla_paged_batch *batch, const vla_
     if ((long)batch->n_rows * n_heads > 0x7fffffffL / 2) { vla_set_error("paged_attention: %d rows of %d heads are too many", batch->n_rows, n_heads); return VLA_ESHAPE; }
     a->n_heads = n_heads; a->group = n_heads / cache->n_kv_heads;
     a->scale = mask->scale; a->cap = mask->softcap; a->slopes = mask->slopes; a->prefix_len = mask->prefix_len;
-    a->window = mask->window; a->shared_len = mask->shared_len;
+    a->window = mask_window(*mask); a->shared_len = mask->shared_len;
     return VLA_OK;
 }
 
