@@ -438,7 +438,7 @@ int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, 
  *   positions below kv_len of a page, for every page that holds one of the batch's rows (positions kv_len - n_s on; a batch whose rows
  *   are all positions: every page).  K of these positions is finite; pages of other rows keep their bounds.
  * vla_paged_select: for each row and key head, the pages to read.  score(page) = sum over the heads h of the group and the dims of
- *   max(q_h lo, q_h hi), no less than the sum of the heads' q.k for any key of the page; fp64.  Of the pages 0 .. p / page_size of a row at
+ *   max(q_h lo, q_h hi), no less than the sum of the heads' q.k for any key of the page; fp64 (bounds are finite; q may not be).  Of the pages 0 .. p / page_size of a row at
  *   position p the first `first` and the last `recent` (at least 1) are taken, then those with the largest scores (ties: lowest page
  *   first; a score that is NaN comes last), until there are n_select (at least first + recent).  selected [n_rows][n_kv_heads][n_select]
  *   out, DEVICE int32: numbers of pages within the sequence, ascending, then -1.  Rows at negative positions get none.  max_len / page_size at most VLA_SELECT_PAGES.

@@ -73,7 +73,8 @@ __device__ __forceinline__ Cut<Key> cut_keys(Each each, int want, int top, Key s
     return c;
 }
 
-// Of numbers 0 .. n - 1 those that the cut takes: put(place, i) for each, in order.  key(i, load(i)): their keys; ~0, which no cut's prefix is, is taken always.  U: of a lane at once.
+// Of numbers 0 .. n - 1 those that the cut takes: put(place, i) for each, in order.  key(i, load(i)): their keys; ~0 is taken always.  U: of a lane at once.
+// (Of every other key one of the highest CUT_BITS bits is zero.  A cut's mask has these at least, so its prefix is not all ones there, and ~0 lies above it.)
 template <int THREADS, int U, typename Key, typename Load, typename KeyOf, typename Put>
 __device__ __forceinline__ void cut_numbers(int n, const Cut<Key> &c, Load load, KeyOf key, Put put, CutLds &s) {
     constexpr int WAVES = THREADS / 64;

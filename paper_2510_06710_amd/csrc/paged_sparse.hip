@@ -57,9 +57,10 @@ struct SelectArgs {
     int32_t *selected;
 };
 
-// Scores as numbers that ascend with them; 0 for NaN.
+// Scores as numbers that ascend with them; 0 for NaN.  Infinity is as 2^1022, above all sums of products of fp32 values: its own number begins with more ones than a cut's keys may (see cut_numbers).
 __device__ __forceinline__ unsigned long long order_of(double x) {
     if (x != x) return 0;
+    x = fmin(x, 0x1p1022);
     const unsigned long long u = __builtin_bit_cast(unsigned long long, x + 0.0);          // (-0 is 0)
     return u >> 63 ? ~u : u | 1ull << 63;
 }
