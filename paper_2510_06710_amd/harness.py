@@ -176,6 +176,16 @@ class PagedRollout:
         batch = self._batch(held, seqs, rows)
         return batch, vb.vla_forward_paged_workspace_bytes(self.run.cfg, self.cache, batch, shared_len)
 
+    def _room(self, n, most):
+        """The summed weights of n sequences, with room for `most` positions."""
+        s, have = self.run.shape, 0 if self.mass is None or self.mass.shape[1] != n else self.mass.shape[3]
+        if have < most:                                      # (a thousand more at a time)
+            more = torch.zeros(s.n_layers, n, s.n_heads, -(-most // 1024) * 1024, device=self.device)
+            if have:
+                more[:, :, :, :have] = self.mass
+            self.mass = more
+        return self.mass
+
     def _run_rows(self, held, seqs, rows, ids, patch=None, shared_len=0, depth=None, **options):
         """Logits of every new row, by vla_forward_paged_rows.  depth [n_rows]: of the rows' positions behind their sequences, where these are not one behind the other."""
         s, n_all = self.run.shape, len(held[0])
@@ -189,13 +199,7 @@ class PagedRollout:
         if self.weigh and options.get("seen") is None:
             if list(seqs) != list(range(n_all)):
                 raise ValueError(f"sequences {list(seqs)}: weights are summed for all {n_all} at once")
-            have = 0 if self.mass is None or self.mass.shape[1] != n_all else self.mass.shape[3]
-            if have < batch.max_len:                         # (room for more, a thousand positions at a time)
-                more = torch.zeros(s.n_layers, n_all, s.n_heads, -(-batch.max_len // 1024) * 1024, device=self.device)
-                if have:
-                    more[:, :, :, :have] = self.mass
-                self.mass = more
-            options["mass"] = self.mass
+            options["mass"] = self._room(n_all, batch.max_len)
         plan = vb.make_paged_rows(**options)
         size = vb.vla_forward_paged_rows_workspace_bytes(self.run.cfg, self.cache, batch, plan, shared_len)
         logits = torch.empty(batch.n_rows, vb.VLA_N_BINS, dtype=torch.float32, device=self.device)
@@ -367,7 +371,8 @@ class PagedRollout:
         following, new_len = torch.empty_like(count), torch.empty_like(count)
         vb.vla_paged_accept(self.cache, run.shape.n_layers, self.layer_stride, batch, parent, ids, chosen, path, count, following, new_len)
         if self.mass is not None:
-            self.mass.masked_fill_(torch.arange(self.mass.shape[3], device=self.device) >= self._int(self.length)[:, None, None], 0.0)
+            mass = self._room(n, max(held[1]))
+            mass.masked_fill_(torch.arange(mass.shape[3], device=self.device) >= self._int(self.length)[:, None, None], 0.0)
         path, following, new_len = path.tolist(), following.tolist(), new_len.tolist()
         self._hold((held[0], new_len, held[2]))
         return [[tokens[i][j] for j in path[i][1:] if j >= 0] + [following[i]] for i in range(n)]
