@@ -113,11 +113,14 @@ class PagedRollout:
     ``weigh``: the weight that rows give each position is summed, for ``evict`` (forwards are then of all sequences, and give no h_last or value).  ``decode`` reads
     ``select`` pages a row and head where that is given; ``decode_drafts`` takes trees of drafted tokens through one forward."""
 
-    def _buf(self, name, nbytes):
-        t = Rollout._buf(self, name, nbytes)
-        if t.is_cuda:                                        # (of the stream it was made on: not given out there before this one is through with it)
+    def _used(self, t):
+        """t, which is not given out again on the stream it was made on before the current one is through with it."""
+        if t.is_cuda:
             t.record_stream(torch.cuda.current_stream(self.device))
         return t
+
+    def _buf(self, name, nbytes):
+        return self._used(Rollout._buf(self, name, nbytes))
 
     def __init__(self, run: Rollout, n_pages: int, page_size: int = 16, weigh: bool = False):
         s = run.shape
@@ -177,8 +180,10 @@ class PagedRollout:
         return batch, vb.vla_forward_paged_workspace_bytes(self.run.cfg, self.cache, batch, shared_len)
 
     def _room(self, n, most):
-        """The summed weights of n sequences, with room for `most` positions."""
+        """The summed weights of n sequences, with room for `most` positions, for the current stream."""
         s, have = self.run.shape, 0 if self.mass is None or self.mass.shape[1] != n else self.mass.shape[3]
+        if have:
+            self._used(self.mass)
         if have < most:                                      # (a thousand more at a time)
             more = torch.zeros(s.n_layers, n, s.n_heads, -(-most // 1024) * 1024, device=self.device)
             if have:
@@ -331,10 +336,10 @@ class PagedRollout:
         pages = [[free.pop() for _ in range(each)] if c else p for c, p in zip(cut, self.pages)]
         to_table = self._int([(p + [-1] * each)[:each] for p in pages])
         batch = self._batch((self.pages, self.length, self.free), list(range(n)), [0] * n)
-        kept = torch.empty(n, s.n_heads, keep, dtype=torch.int32, device=self.device)
+        kept, mass = torch.empty(n, s.n_heads, keep, dtype=torch.int32, device=self.device), self._room(n, max(self.length))
         for l in range(s.n_layers):
             cache = vb.make_paged_cache(self.pools[0][l], self.pools[1][l])
-            vb.vla_paged_evict(cache, batch, self.mass[l], first, recent, to_table, kept, self.mass[l])
+            vb.vla_paged_evict(cache, batch, mass[l], first, recent, to_table, kept, mass[l])
         self.shift = [z + max(0, l - keep) for z, l in zip(self.shift, self.length)]
         used = {q for p in pages for q in p}
         self._hold((pages, [min(l, keep) for l in self.length], [q for q in range(self.n_pages - 1, -1, -1) if q not in used]))
