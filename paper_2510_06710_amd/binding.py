@@ -17,6 +17,7 @@ VLA_DTYPE_F32, VLA_DTYPE_BF16 = 0, 1
 VLA_MODE_AR, VLA_MODE_PARALLEL_CHUNK = 0, 1
 VLA_ENTRY_PREFILL, VLA_ENTRY_DECODE, VLA_ENTRY_RECOMPUTE = 0, 1, 2
 VLA_N_BINS = 256
+VLA_SELECT_PAGES = 8192
 
 
 class vla_config(C.Structure):

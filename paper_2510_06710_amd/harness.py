@@ -388,7 +388,9 @@ class PagedRollout:
             raise ValueError(f"{n_tokens} tokens from logits of {n} sequences: there are {len(self.pages)}")
         if u is not None and (u.dim() != 2 or u.shape[0] < n_tokens or u.shape[1] != n):
             raise ValueError(f"u is {list(u.shape)}, wanted [{n_tokens}, {n}]")
-        self._grown((self.pages, self.length, self.free), list(range(n)), [n_tokens - 1] * n)          # (the pages of all steps, before the first)
+        most = -(-max(self._grown((self.pages, self.length, self.free), list(range(n)), [n_tokens - 1] * n)[1]) // self.page_size)          # (the pages of all steps, before the first)
+        if select and n_tokens > 1 and most > vb.VLA_SELECT_PAGES:
+            raise ValueError(f"{most} pages of a sequence to select from, at most {vb.VLA_SELECT_PAGES}")
         every = lambda v, dtype: torch.full((n,), v, dtype=dtype, device=dev)
         t, k, p, least = every(temperature, torch.float32), every(top_k, torch.int32), every(top_p, torch.float32), every(min_p, torch.float32)
         if select < 0 or (select and self.weigh):
