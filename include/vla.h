@@ -432,6 +432,9 @@ int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, 
  *   them chose (-1 without rows); new_len [n_seq] out or NULL: kv_len - n_s + n_accepted.  In each of n_layers layers, layer l at
  *   cache->k, v + l * layer_stride elements, K and V of row path[i] move to position kv_len - n_s + i (n_layers may be 0: nothing moves).  The rows behind
  *   new_len keep what they hold.  No output overlaps parent, ids, chosen, kv_len or row_start.  The pages of the new rows belong to their sequence alone.  Rows at negative positions are nowhere, and new_len is not below 0.
+ *   Page bounds that a caller keeps (below) are behind it those of rows that have left or moved: vla_paged_bounds, with n_accepted's running sums as row_start, new_len as
+ *   kv_len and the other numbers of this batch, computes those from position kv_len - n_s on again.  Mass (below) of
+ *   these positions is the caller's to set, for no weights of a tree's rows are summed.
  *
  * Sparse attention over pages.
  * vla_paged_bounds: bounds, DEVICE cache's dtype [n_pages][n_kv_heads][2][head_dim], 16-byte aligned: the least and the largest K of each dim over the
@@ -456,10 +459,11 @@ int vla_sample_logits(const void *logits, int dtype, int64_t row_stride, int n, 
  *   ascending, then -1.  K, V and mass of the i-th go to position i: K and V in page to_table[sequence][i / page_size] (to_stride entries per
  *   sequence, at least keep / page_size rounded up), mass to mass_out [n_seq][n_kv_heads][mass_out_stride] (mass itself with its stride, or apart
  *   from it; entries behind the last keep what they hold).  new_len [n_seq] out or NULL: min(kv_len, keep), apart from kv_len.  to_table's pages hold nothing that the call reads, but that a sequence
- *   with no more than `keep` may name its own pages again (nothing moves).  One layer a call.  Of the batch it uses the sequences, not their rows. */
+ *   with no more than `keep` may name its own pages again (nothing moves).  The bounds of to_table's pages are
+ *   to be computed again (vla_paged_bounds of a batch whose rows are all positions).  One layer a call.  Of the batch it uses the sequences, not their rows. */
 /* vla_forward_paged_rows: vla_forward_paged with these, and with the logits of every row (a tree's nodes are all read).
  *   position, seen (words to a row), prefix_len: as above, each or NULL; bounds: [n_layers] of vla_paged_bounds' arrays or NULL: kept up with the
- *   new rows; n_select above 0 (bounds given): rows read the pages that vla_paged_select takes with first and recent; mass
+ *   new rows (behind vla_paged_accept and vla_paged_evict: see there); n_select above 0 (bounds given): rows read the pages that vla_paged_select takes with first and recent; mass
  *   [n_layers][n_seq][n_kv_heads][mass_stride] or NULL: vla_paged_weights of every layer.  A tree, selected pages, and weights or a prefix mask exclude each other.
  *   logits  DEVICE fp32 [n_rows, 256] out (of padding rows: of no meaning).  ws: of vla_forward_paged_rows_workspace_bytes bytes. */
 typedef struct vla_paged_rows {
