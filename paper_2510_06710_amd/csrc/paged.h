@@ -1,4 +1,4 @@
-// What the kernels of the paged KV cache (paged_append.hip, paged_attention.hip) share: the cache and the ragged batch as
+// What the kernels of the paged KV cache (paged_*.hip) share: the cache and the ragged batch as
 // they are handed to a kernel, and the checks of both on the host.
 #pragma once
 #include "vla_internal.h"

@@ -65,7 +65,7 @@ __device__ __forceinline__ float tile_weight(const AttnArgs &a, const f32x16_t &
 // One wave a workgroup, as many as their rings fit the chip; each takes one key head's equal run of the key tiles of all sequences, whatever their lengths.  Up to 32 packed rows of a
 // sequence are in registers, its tiles of 32 keys come through a ring of three in LDS (rows of 16 keys of a page, as in paged_attention.hip); their sums go to LDS and to memory eight tiles at a time.
 // Of more than 2048 sequences a wave takes `chunk` tiles of one (every wave looks at all sequences' lengths to find its run).
-// Bound by memory: 64 rows behind up to 4096 keys, 8 heads of 128, 248 MB in 56 us, 4.4 TB/s.  (Chunks of one sequence's tiles a workgroup: 57 to 67.)  Scores, weights and sums are fp32.
+// Bound by memory: 64 rows behind up to 4096 keys, 8 heads of 128, 248 MB in 56 us, 4.4 TB/s; in fp32 488 MB in 139 us, 3.5 TB/s.  (Chunks of one sequence's tiles a workgroup: 57 to 67.)  Scores, weights and sums are fp32.
 constexpr int STEP_TILES = 8;
 struct StepTiles { int from, n; };           // of a sequence: those that a row sees or that hold new positions (all behind the first row's window, and before the prefix's end)
 __device__ __forceinline__ StepTiles step_tiles(const AttnArgs &a, int s) {
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(64) paged_weights_step_kernel(WeightArgs w) {
 // beside them (a copy for each wave: no register is loaded inside the loop).  A row of q may start anywhere: where rows are no multiples of 16 bytes they go through registers.
 // The exponentials of one tile of rows are taken between the matrix instructions of the next.
 // Bound by the matrix and the vector units together: 4096 causal rows of 32 heads of 128, 8 key heads: 118 us and 5 for the join, 580 TFLOP/s of scores, where a plain product of that
-// size takes 49 us and the vector work of 268 million weights most of the rest.  (The simple kernel, rows kept and keys streamed: 1359 us.)
+// size takes 49 us and the vector work of 268 million weights most of the rest; in fp32 680 us, 101 TFLOP/s of the card's 153.  (The simple kernel, rows kept and keys streamed: 1359 us.)
 template <typename T, int DP> constexpr int KEY_TILES = sizeof(T) * DP <= 256 ? 2 : 1;
 template <typename T, int DP, int MODE>
 __global__ void __launch_bounds__(256, sizeof(T) * DP <= 256 ? 2 : 1) paged_weights_rows_kernel(WeightArgs w) {
@@ -692,7 +692,7 @@ __global__ void __launch_bounds__(EVICT_THREADS) paged_evict_select_kernel(Evict
 }
 
 // K and V of the kept positions to their places: 16 bytes a lane, four rows of one key head on their way at once.  Bound by memory: 16 x 8 x 4096 rows of 256 bytes (475 MB read and written, rows in any order) in 100 us,
-// the rate of a large copy.
+// the rate of a large copy; in fp32 (931 MB) 201 us.
 template <int U>
 __global__ void __launch_bounds__(256) paged_evict_move_kernel(EvictArgs a, int chunks, int row_bytes) {
     const PagedView &pv = a.pv;

@@ -1,4 +1,4 @@
-// What the attention kernels of the paged cache (paged_attention.hip, paged_sparse.hip) share: tiles of keys in LDS, the two products with
+// What the attention kernels of the paged cache (paged_attention.hip, paged_sparse.hip) and the sums of their weights (paged_evict.hip) share: tiles of keys in LDS, the two products with
 // the online softmax between them, the sums of parts and their join.  The mathematics is described at the top of paged_attention.hip.
 #pragma once
 #include "paged.h"

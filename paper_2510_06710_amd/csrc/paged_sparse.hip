@@ -11,7 +11,7 @@ namespace {
 // ---- bounds ----------------------------------------------------------------------------------------------------------------
 // A workgroup for each (page, sequence): its lanes each hold eight dims of one key head (16 bytes of bf16, 32 of fp32).  Reads the keys
 // below kv_len of a page once and writes two rows a head; nothing is rounded.  Bound by memory: four prompts of up to 32,768 positions, 8 heads of 128, 181 MB in 38 us, 4.7 TB/s
-// (plain reads reach 6.1; the first workgroups' look-ups and the last ones' end are a fifth of it).
+// (plain reads reach 6.1; the first workgroups' look-ups and the last ones' end are a fifth of it); fp32, 362 MB, 76 us.
 template <typename T>
 __global__ void __launch_bounds__(256) paged_bounds_kernel(PagedView pv, T *bounds) {
     typedef T t8 __attribute__((ext_vector_type(8)));
@@ -75,10 +75,6 @@ __device__ __forceinline__ int page_of_row(const PagedView &pv, int row, int *s)
     return p < 0 ? -1 : p >> pv.page_log;
 }
 
-// A page's bounds are 2 d values of lo and hi, 16 bytes a lane: `lanes` lanes (a power of two, at most 64) hold a page, so a wave's load has 64 / lanes of them, and eight loads are on their way at once
-// (an fp32 page of more than 128 dims takes two loads a lane).  The parts of q that a lane multiplies by are the same for all pages.
-// Bound by the chain of look-ups before the first load where pages are few, else by the fp64 products: 8 x 2048 pages of 512 bytes 7.3 us; 32 ragged rows of up to 1024 pages of 8 heads, 67 MB,
-// 23 us.  (One wave a page and load, q again for every four pages: 12 and 81.)
 // Sum over 2^lanes_log neighbouring lanes, by lane moves (the value of lane ^ o, in halves).
 template <int CTRL> __device__ __forceinline__ double moved(double v) {
     const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
@@ -101,6 +97,11 @@ __device__ __forceinline__ double lanes_sum(double v, int lanes_log) {
     return v;
 }
 
+// A page's bounds are 2 d values of lo and hi, 16 bytes a lane: `lanes` lanes (a power of two, at most 64) hold a page, so a wave's load has 64 / lanes of them, and eight loads are on their way at once
+// (an fp32 page of more than 128 dims takes two loads a lane).  The parts of q that a lane multiplies by are the same for all pages.
+// Where pages are few it is the chain of look-ups before the first load: 8 x 2048 pages of 512 bytes 7.3 us.  32 ragged rows of up to 1024 pages of 8 heads, 67 MB, take 23 us, 11 of them at the rate of reads;
+// the rest is that chain and some 60 vector instructions a kilobyte, 8 of them products and 8 the bounds' widening to fp64, the others the bf16 values' unpacking and the sum over lanes.  In fp32 9.0 and 48 us.
+// (One wave a page and load, q again for every four pages: 12 and 81.)
 template <typename T>
 __global__ void __launch_bounds__(256) paged_score_kernel(SelectArgs a, int lanes_log, int per_block) {
     constexpr int E = 16 / sizeof(T), U = 8, R = sizeof(T) == 4 ? 2 : 1;          // values of a load; pages of a lane at once; loads of a page
@@ -235,6 +236,7 @@ struct SparseArgs {
 // Keys are taken 16 at a time (a page's run of them), two such runs to a tile of 32, through the same ring and products as paged_decode_kernel.
 // A workgroup is one wave: of one row and key head, up to 32 heads of its group, and a part of its list.  On a bf16 cache weights enter the product with v as a bf16 head and a bf16 tail (2^-16 of each is lost).
 // Bound by memory: 32 rows of 64 pages of 32 positions, 8 heads of 128, 268 MB in 54 us, 5.0 TB/s; one row of 64 pages of 64 (17 MB) 8.8 us, and 4.3 for the join of its 64 parts.
+// In fp32 168 us (3.2 TB/s; eight matrix instructions for one, most of whose columns are empty) and 17.4.
 template <typename T, int DP, int MODE>
 __global__ void __launch_bounds__(64) paged_sparse_kernel(SparseArgs x) {
     typedef Tile<T, DP> TL;

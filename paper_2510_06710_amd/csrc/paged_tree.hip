@@ -2,7 +2,7 @@
 //
 // A node's ancestors have smaller numbers, so a walk up from it meets them in descending order: the words of its row of bits are finished
 // one after the other, last first, by one thread.  Both kernels are chains of dependent reads of a few hundred bytes; the parents of a
-// sequence are read to LDS once, where a step of a walk costs 0.1 us and not a trip to memory.  Nothing is rounded: whole numbers and moved bits.
+// sequence are read to LDS once, where a step of a walk costs a quarter of a microsecond at most and not a trip to memory.  Nothing is rounded: whole numbers and moved bits.
 #include "paged.h"
 
 namespace {
@@ -10,6 +10,8 @@ namespace {
 // The parent of node i: below 0 for none.
 __device__ __forceinline__ int parent_of(const int32_t *parent, int i) { return parent[i] < i ? parent[i] : -1; }
 
+// A thread a node.  In a captured graph 8 nodes take 1.8 us, 32 sequences of 24 2.7; of 1024 nodes whose paths are up to some 400 long 111 us, for one sequence as for 64 (8.9 MB, 2 us at the
+// copy's rate): the longest walk, a quarter of a microsecond a node.
 __global__ void __launch_bounds__(256) paged_tree_kernel(PagedView pv, const int32_t *parent, int32_t *seen, int words, int32_t *position) {
     __shared__ int32_t up[VLA_TREE_ROWS];
     const PagedSeq sq = paged_seq(pv, blockIdx.x);
@@ -32,7 +34,8 @@ __global__ void __launch_bounds__(256) paged_tree_kernel(PagedView pv, const int
 // A workgroup for each sequence and run of (layer, key head) pairs of K or V; all of them follow the path (one wave, 64 nodes at a time), the first
 // writes it.  Of a path's rows only those move that leave their place.  A lane moves the same 16 bytes of every row, so what it writes
 // (place i) it has read before: sources ascend and lie behind their targets.  Eight rows are on their way at once.  One sequence of 8 nodes in 32 layers of 8 heads: 4.8 us, the
-// chain of the look-ups and the path; 64 sequences of up to 33 nodes, 16 layers of 32 heads: 44 us for 130 MB read and written, 2.9 TB/s (a copy: 4.75), its rows of 256 bytes behind that chain.
+// chain of the look-ups and the path; 64 sequences of up to 33 nodes, 16 layers of 32 heads: 44 us for 130 MB read and written, 2.9 TB/s (a copy: 4.75),
+// where a lane stores the rows of one unit before it loads those of the next; in fp32 92 us for 259 MB, 2.8 TB/s.
 struct AcceptArgs {
     PagedView pv;
     size_t layer_bytes;
